@@ -44,7 +44,10 @@ typedef enum {
     CPRUNE_ERR_BAD_DATA = 7   /* a weight was NaN/Inf or too large for the norm grid (reported by poll) */
 } cprune_status;
 
-enum { CPRUNE_ACT_NONE = 0, CPRUNE_ACT_RELU = 1, CPRUNE_ACT_RELU6 = 2 };
+/* SILU, z / (1 + exp(-z)), belongs to the group norm alone; everything else refuses it. */
+enum { CPRUNE_ACT_NONE = 0, CPRUNE_ACT_RELU = 1, CPRUNE_ACT_RELU6 = 2, CPRUNE_ACT_SILU = 3 };
+/* element types of the operators that take more than one: bf16 tensors have padded channels, float32 tensors have C */
+enum { CPRUNE_TYPE_BF16 = 0, CPRUNE_TYPE_F32 = 1 };
 /* max-pool applied to the activated conv result: 2x2 stride 2 (VGG blocks), or 3x3 stride 2 pad 1 (ResNet stem;
  * padding never wins the maximum) */
 enum { CPRUNE_POOL_NONE = 0, CPRUNE_POOL_MAX2X2 = 1, CPRUNE_POOL_MAX3X3S2 = 2 };
@@ -245,6 +248,33 @@ cprune_status cprune_global_avgpool(const void *x, int N, int H, int W, int C, v
 cprune_status cprune_fc_pack(const float *w, const float *b, int out, int in, void *w_packed, float *b_packed, void *stream);
 cprune_status cprune_fc(const void *x, int N, int in, const void *w_packed, const float *b_packed, int out, int act,
                         int out_is_f32, void *y, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Group norm with an activation, for networks whose normalisation does not fold into the convolution (small batches of the
+ * short training that the pruning loop gives a candidate, paper Algorithm 1 step 11):
+ *   y = act((x - mean) rstd gamma + beta + residual),   rstd = 1 / sqrt(variance + eps)
+ * with mean and biased variance over the pixels of one image and the C / groups neighbouring channels of one group; all of it
+ * in float32, rounded once to y's type.
+ *   type      CPRUNE_TYPE_BF16: x, y, residual bf16 [N][H][W][c_pad]; CPRUNE_TYPE_F32: float32 [N][H][W][C]
+ *   groups    divides C; C / groups may be any number (a pruned layer's channels need not fill vectors)
+ *   gamma, beta  float32 [C] or NULL (ones, zeros);   residual  as x, or NULL;   eps > 0
+ *   y         may be x or residual;   stats  float32 [N][groups][2], written: mean and rstd, which the gradients need
+ *   workspace cprune_group_norm_workspace_bytes (never 0 for arguments that are in order), 16-byte aligned
+ * A NaN in a group, or an infinity, makes its outputs NaN; the activations hand a NaN on.  Other groups keep their values.
+ *
+ * Gradients, given dy = dL/dy and the stats of the forward pass: dx, dgamma [C], dbeta [C] (either may be NULL) and
+ * dresidual (NULL, or wanted, with residual given).  The slope of relu is 0 at 0, of relu6 0 at 0 and at 6; it is taken of the
+ * z that x, stats, gamma, beta and residual give.  dx and dresidual may be dy or x, but not each other.
+ * Results do not depend on timing (no atomics).  bf16 tensors are 16-byte aligned, all others to their elements.
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (an image of 2^31 values or more, N > 65535, C > 2^20), CUDA.
+ * Enqueue only; at most four launches. */
+size_t cprune_group_norm_workspace_bytes(int type, int N, int H, int W, int C, int groups, int backward);
+cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, int C, int groups, const float *gamma, const float *beta,
+                                float eps, int act, const void *residual, void *y, float *stats, void *workspace, size_t workspace_bytes,
+                                void *stream);
+cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type, int N, int H, int W, int C, int groups, const float *stats,
+                                         const float *gamma, const float *beta, int act, const void *residual, void *dx, float *dgamma,
+                                         float *dbeta, void *dresidual, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Fused inverted-residual block (the MobileNetV2 / MnasNet building block of the paper's Sec. 4.1 models): the three

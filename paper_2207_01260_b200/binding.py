@@ -4,7 +4,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char_p, c_double, c_int, c_int32, c_longlong, c_size_t, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, c_void_p
 
 import torch
 
@@ -15,6 +15,7 @@ OK = 0
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "WORKSPACE_TOO_SMALL", 4: "CUDA", 5: "TIMEOUT",
                 6: "INTERNAL", 7: "BAD_DATA"}
 ACT = {"none": 0, "relu": 1, "relu6": 2}
+NORM_ACT = {**ACT, "silu": 3}              # of the group norm, which alone has silu
 POOL = {None: 0, "none": 0, "max2x2": 1, "max3x3s2": 2}
 KERNEL = {"auto": 0, "direct": 1, "tensor": 2, "depthwise": 3}
 KERNEL_NAMES = {v: k for k, v in KERNEL.items()}
@@ -32,7 +33,7 @@ EXPORTS = [
     "cprune_model_destroy", "cprune_poll_device_status", "cprune_select_shared", "cprune_prune_step",
     "cprune_task_estimate", "cprune_task_order", "cprune_model_task_table", "cprune_model_time_tasks",
     "cprune_selftest_wait_timeout", "cprune_block_plan", "cprune_block_query", "cprune_block_release", "cprune_block_pack",
-    "cprune_block_run", "cprune_model_reads_image",
+    "cprune_block_run", "cprune_model_reads_image", "cprune_group_norm_workspace_bytes", "cprune_group_norm", "cprune_group_norm_backward",
 ]
 
 
@@ -135,6 +136,10 @@ def lib():
         L.cprune_block_release.argtypes = [c_void_p]
         L.cprune_block_pack.argtypes = [c_void_p] * 10
         L.cprune_block_run.argtypes = [c_void_p] * 7
+        L.cprune_group_norm_workspace_bytes.restype = c_size_t
+        L.cprune_group_norm_workspace_bytes.argtypes = [c_int] * 7
+        L.cprune_group_norm.argtypes = [c_void_p] + [c_int] * 6 + [c_void_p, c_void_p, c_float, c_int] + [c_void_p] * 4 + [c_size_t, c_void_p]
+        L.cprune_group_norm_backward.argtypes = [c_void_p] * 2 + [c_int] * 6 + [c_void_p] * 3 + [c_int] + [c_void_p] * 6 + [c_size_t, c_void_p]
         _lib = L
     return _lib
 
@@ -454,6 +459,97 @@ def cprune_fc(x, in_features, w_packed, b_packed, out_features, activation="none
     return y
 
 
+# The operators below check what they are given before they hand addresses on: a tensor of another type, shape or device would be read out of
+# bounds.  What they allocate belongs to the stream that they run on, so that a workspace is not handed out again while it is in use there.
+TYPE = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _refuse(where, why):
+    raise CpruneError(1, where, why)
+
+
+def _checked(where, name, t, shape, dtype, device=None):
+    """`t`'s address; refuses anything but a contiguous tensor of this shape and type on the current device."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _refuse(where, "%s has to be a contiguous %s tensor of shape %s" % (name, dtype, tuple(shape)))
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _refuse(where, "%s is not on the current device" % name)
+    return t.data_ptr()
+
+
+def _empty(stream, shape, dtype, device):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _norm_input(where, x, C, groups, activation):
+    """(type, N, H, W, lanes) of an activation [N, H, W, lanes]."""
+    if x.dtype not in TYPE or x.dim() != 4 or C < 1:
+        _refuse(where, "x has to be a bf16 or float32 tensor [N, H, W, channels in memory]")
+    lanes = cprune_padded_channels(C) if x.dtype == torch.bfloat16 else C
+    if x.shape[3] != lanes:
+        _refuse(where, "x has %d channels in memory; %d channels take %d" % (x.shape[3], C, lanes))
+    if activation not in NORM_ACT:
+        _refuse(where, "unknown activation %r" % (activation,))
+    return (TYPE[x.dtype],) + tuple(x.shape[:3])
+
+
+def _norm_workspace(where, geometry, C, groups, backward, workspace, stream, device):
+    need = lib().cprune_group_norm_workspace_bytes(*geometry, C, groups, backward)
+    if workspace is None:
+        return _empty(stream, (need,), torch.uint8, device)
+    _checked(where, "workspace", workspace, (workspace.numel(),), torch.uint8)
+    return workspace
+
+
+def cprune_group_norm(x, C, groups, gamma=None, beta=None, eps=1e-5, activation="none", residual=None, y=None, stats=None, workspace=None, stream=None):
+    """Group norm of a channels-last activation x (bf16 [N, H, W, c_pad] or float32 [N, H, W, C]) with C channels in `groups` groups, its scale
+    and shift (float32 [C]), a tensor added to it and an activation (none, relu, relu6, silu).  Returns (y, stats); stats, float32
+    [N, groups, 2], holds mean and 1 / sqrt(variance + eps) for cprune_group_norm_backward.  y may be x."""
+    where = "cprune_group_norm"
+    geometry = _norm_input(where, x, C, groups, activation)
+    px, pr = _checked(where, "x", x, x.shape, x.dtype), _checked(where, "residual", residual, x.shape, x.dtype)
+    pg, pb = _checked(where, "gamma", gamma, (C,), torch.float32), _checked(where, "beta", beta, (C,), torch.float32)
+    if y is None:
+        y = _empty(stream, x.shape, x.dtype, x.device)
+    if stats is None:
+        stats = _empty(stream, (x.shape[0], max(groups, 0), 2), torch.float32, x.device)
+    workspace = _norm_workspace(where, geometry, C, groups, 0, workspace, stream, x.device)
+    _check(lib().cprune_group_norm(px, *geometry, C, groups, pg, pb, eps, NORM_ACT[activation], pr, _checked(where, "y", y, x.shape, x.dtype),
+                                   _checked(where, "stats", stats, (x.shape[0], groups, 2), torch.float32), workspace.data_ptr(), workspace.numel(),
+                                   _stream(stream)), where)
+    return y, stats
+
+
+def cprune_group_norm_backward(dy, x, C, groups, stats, gamma=None, beta=None, activation="none", residual=None, dx=None, dgamma=None, dbeta=None,
+                               dresidual=None, workspace=None, stream=None):
+    """Gradients of cprune_group_norm's y, given dy and the stats of the forward pass.  Returns (dx, dgamma, dbeta, dresidual); dresidual is None
+    where there is no residual."""
+    where = "cprune_group_norm_backward"
+    geometry = _norm_input(where, x, C, groups, activation)
+    px, pr, pdy = (_checked(where, n, t, x.shape, x.dtype) for n, t in (("x", x), ("residual", residual), ("dy", dy)))
+    pg, pb = _checked(where, "gamma", gamma, (C,), torch.float32), _checked(where, "beta", beta, (C,), torch.float32)
+    ps = _checked(where, "stats", stats, (x.shape[0], groups, 2), torch.float32)
+    if dx is None:
+        dx = _empty(stream, x.shape, x.dtype, x.device)
+    if dgamma is None:
+        dgamma = _empty(stream, (C,), torch.float32, x.device)
+    if dbeta is None:
+        dbeta = _empty(stream, (C,), torch.float32, x.device)
+    if dresidual is None and residual is not None:
+        dresidual = _empty(stream, x.shape, x.dtype, x.device)
+    workspace = _norm_workspace(where, geometry, C, groups, 1, workspace, stream, x.device)
+    _check(lib().cprune_group_norm_backward(pdy, px, *geometry, C, groups, ps, pg, pb, NORM_ACT[activation], pr, _checked(where, "dx", dx, x.shape, x.dtype),
+                                            _checked(where, "dgamma", dgamma, (C,), torch.float32), _checked(where, "dbeta", dbeta, (C,), torch.float32),
+                                            _checked(where, "dresidual", dresidual, x.shape, x.dtype), workspace.data_ptr(), workspace.numel(),
+                                            _stream(stream)), where)
+    return dx, dgamma, dbeta, dresidual
+
+
 class Model:
     """Handle of a cprune_model; keeps the plans and packed weights it borrows alive."""
 
@@ -548,4 +644,4 @@ def cprune_selftest_wait_timeout(stream=None):
 
 __all__ = [n for n in dir() if n.startswith("cprune_")] + ["Plan", "Model", "TaskDesc", "CpruneError", "lib",
                                                            "EXPORTS", "KERNEL_NAMES", "OP_CONV", "OP_MAXPOOL",
-                                                           "OP_GAP", "OP_FC", "OP_BLOCK", "CONV_WITH_NEXT", "Block"]
+                                                           "OP_GAP", "OP_FC", "OP_BLOCK", "CONV_WITH_NEXT", "Block", "NORM_ACT"]

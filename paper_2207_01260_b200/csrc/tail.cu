@@ -224,7 +224,7 @@ cprune_status cprune_global_avgpool(const void *x, int N, int H, int W, int C, v
 
 cprune_status cprune_fc(const void *x, int N, int in, const void *w_packed, const float *b_packed, int out, int act,
                         int out_is_f32, void *y, void *stream) {
-    if (!x || !w_packed || !b_packed || !y || N <= 0 || in <= 0 || out <= 0) return CPRUNE_ERR_INVALID_ARG;
+    if (!x || !w_packed || !b_packed || !y || N <= 0 || in <= 0 || out <= 0 || act == CPRUNE_ACT_SILU) return CPRUNE_ERR_INVALID_ARG;
     int in8 = cprune_padded_channels(in) / 8, out_pad = cprune_padded_channels(out);
     if ((long long)(out_pad >> 3) * ((N + 15) / 16) > 0x7fffffffLL) return CPRUNE_ERR_UNSUPPORTED;
     // One tile of 8 features per SM as long as there are SMs for them: one image 2.4 us.  Beyond that 16 features: 20 images of 1280

@@ -276,6 +276,22 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
                                          const float *gamma, const float *beta, int act, const void *residual, void *dx, float *dgamma,
                                          float *dbeta, void *dresidual, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Global norm of the gradients of many tensors and clipping to a largest norm (the same training):
+ *   norm = sqrt(sum of g^2 over all values of all tensors),   out = g min(1, max_norm / (norm + 1e-6))
+ * Sums in float64, in a fixed order; out is rounded once.  A NaN anywhere makes the norm and every result NaN, an infinity the
+ * norm infinite and the results 0 (NaN where the infinity was): look at *norm before an update.
+ *   grads   HOST array of n device addresses, counts and types (CPRUNE_TYPE_*) HOST arrays; a tensor is one run of counts[i]
+ *           values at any address of its type; no two of them overlap; n and counts may be 0
+ *   out     HOST array of n device addresses (types as grads), or NULL: in place.  out[i] is grads[i] or does not overlap any
+ *   norm    device float32 [1];   max_norm >= 0;   workspace  cprune_gradient_workspace_bytes(n), device, 16-byte aligned
+ * The arrays are read during the call (the list travels in kernel parameters); enqueue only, two launches for up to 512
+ * tensors, two more for every further 512.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^44 values), CUDA. */
+size_t cprune_gradient_workspace_bytes(int n);
+cprune_status cprune_gradient_norm(const void *const *grads, const unsigned long long *counts, const int *types, int n, float *norm,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+cprune_status cprune_clip_gradients(const void *const *grads, const unsigned long long *counts, const int *types, int n, float max_norm,
+                                    void *const *out, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Fused inverted-residual block (the MobileNetV2 / MnasNet building block of the paper's Sec. 4.1 models): the three
  * tasks 1x1 expand + activation, 3x3 depthwise (stride 1, pad 1) + activation, 1x1 project (+ the block's input as

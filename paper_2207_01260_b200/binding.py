@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, c_void_p
 
 import torch
@@ -34,6 +35,7 @@ EXPORTS = [
     "cprune_task_estimate", "cprune_task_order", "cprune_model_task_table", "cprune_model_time_tasks",
     "cprune_selftest_wait_timeout", "cprune_block_plan", "cprune_block_query", "cprune_block_release", "cprune_block_pack",
     "cprune_block_run", "cprune_model_reads_image", "cprune_group_norm_workspace_bytes", "cprune_group_norm", "cprune_group_norm_backward",
+    "cprune_gradient_workspace_bytes", "cprune_gradient_norm", "cprune_clip_gradients",
 ]
 
 
@@ -140,6 +142,10 @@ def lib():
         L.cprune_group_norm_workspace_bytes.argtypes = [c_int] * 7
         L.cprune_group_norm.argtypes = [c_void_p] + [c_int] * 6 + [c_void_p, c_void_p, c_float, c_int] + [c_void_p] * 4 + [c_size_t, c_void_p]
         L.cprune_group_norm_backward.argtypes = [c_void_p] * 2 + [c_int] * 6 + [c_void_p] * 3 + [c_int] + [c_void_p] * 6 + [c_size_t, c_void_p]
+        L.cprune_gradient_workspace_bytes.restype = c_size_t
+        L.cprune_gradient_workspace_bytes.argtypes = [c_int]
+        L.cprune_gradient_norm.argtypes = [c_void_p] * 3 + [c_int] + [c_void_p] * 2 + [c_size_t, c_void_p]
+        L.cprune_clip_gradients.argtypes = [c_void_p] * 3 + [c_int, c_float] + [c_void_p] * 3 + [c_size_t, c_void_p]
         _lib = L
     return _lib
 
@@ -548,6 +554,62 @@ def cprune_group_norm_backward(dy, x, C, groups, stats, gamma=None, beta=None, a
                                             _checked(where, "dresidual", dresidual, x.shape, x.dtype), workspace.data_ptr(), workspace.numel(),
                                             _stream(stream)), where)
     return dx, dgamma, dbeta, dresidual
+
+
+def _gradient_list(where, tensors):
+    """(addresses, counts, types) of a list of tensors, as arrays that the library reads."""
+    device = torch.cuda.current_device() if tensors else None
+    addresses, counts, types = array("Q"), array("Q"), array("i")
+    for t in tensors:
+        if t.dtype not in TYPE or not t.is_contiguous():
+            _refuse(where, "gradients have to be contiguous bf16 or float32 tensors")
+        if t.get_device() != device:
+            _refuse(where, "a gradient is not on the current device")
+        addresses.append(t.data_ptr())
+        counts.append(t.numel())
+        types.append(TYPE[t.dtype])
+    there = [a for a, n in zip(addresses, counts) if n]
+    if len(set(there)) != len(there):
+        _refuse(where, "a tensor is in the list twice")
+    return addresses, counts, types
+
+
+def _gradient_buffers(n, norm, workspace, where, stream):
+    if norm is None:
+        norm = _empty(stream, (1,), torch.float32, torch.device("cuda", torch.cuda.current_device()))
+    else:
+        _checked(where, "norm", norm, (1,), torch.float32)
+    if workspace is None:
+        workspace = _empty(stream, (lib().cprune_gradient_workspace_bytes(n),), torch.uint8, norm.device)
+    else:
+        _checked(where, "workspace", workspace, (workspace.numel(),), torch.uint8)
+    return norm, workspace
+
+
+def cprune_gradient_norm(grads, norm=None, workspace=None, stream=None):
+    """The global 2-norm of a list of contiguous bf16 or float32 tensors, as a float32 tensor [1]."""
+    where = "cprune_gradient_norm"
+    a, c, t = _gradient_list(where, grads)
+    norm, workspace = _gradient_buffers(len(a), norm, workspace, where, stream)
+    _check(lib().cprune_gradient_norm(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                      _stream(stream)), where)
+    return norm
+
+
+def cprune_clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
+    """Scales the gradients, a list of contiguous bf16 or float32 tensors, by min(1, max_norm / (norm + 1e-6)) with their global 2-norm: in place, or
+    into the tensors of `out` (same shapes and types).  Returns the norm before, a float32 tensor [1]."""
+    where = "cprune_clip_gradients"
+    a, c, t = _gradient_list(where, grads)
+    o = None
+    if out is not None:
+        o, oc, ot = _gradient_list(where, out)
+        if oc != c or ot != t:
+            _refuse(where, "out has to have the gradients' sizes and types")
+    norm, workspace = _gradient_buffers(len(a), norm, workspace, where, stream)
+    _check(lib().cprune_clip_gradients(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), max_norm, None if o is None else o.buffer_info()[0],
+                                       norm.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)), where)
+    return norm
 
 
 class Model:

@@ -74,6 +74,13 @@ cudaError_t launch_chained(void (*kernel)(KArgs...), dim3 grid, dim3 block, size
     return launch_chained_as(false, kernel, grid, block, smem, st, static_cast<Args &&>(args)...);
 }
 
+// The launches of one operator follow one another as a chain, whoever enqueues it: its first kernel waits before its successors may start.
+struct ChainScope {
+    const bool before = chain_launch_enabled();
+    void follow() { set_chain_launch(true); }
+    ~ChainScope() { set_chain_launch(before); }
+};
+
 inline int round_up(int v, int m) { return (v + m - 1) / m * m; }
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 

@@ -518,13 +518,6 @@ static cprune_status norm_check(int type, int N, int H, int W, int C, int groups
     return CPRUNE_OK;
 }
 
-// The launches of an operator follow one another as a chain, whoever enqueues it: the first waits before its successors may start.
-struct ChainScope {
-    const bool before = chain_launch_enabled();
-    void follow() { set_chain_launch(true); }
-    ~ChainScope() { set_chain_launch(before); }
-};
-
 // Which of the kernels for one, eight or four channels a vector
 template <typename F>
 static cprune_status by_kind(int kind, F f) {

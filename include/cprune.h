@@ -292,6 +292,35 @@ cprune_status cprune_gradient_norm(const void *const *grads, const unsigned long
 cprune_status cprune_clip_gradients(const void *const *grads, const unsigned long long *counts, const int *types, int n, float max_norm,
                                     void *const *out, float *norm, void *workspace, size_t workspace_bytes, void *stream);
 
+/* 4-bit values: the MXFP4 format of the OCP Microscaling specification, for the weights of fully connected and 1x1 layers (4.25 bits
+ * a weight) and, on the way into such a product, the activations.  Rows are rounded in blocks of 32 neighbouring channels:
+ *   scale = 2^(floor(log2 max |x|) - 2), not below 2^-127;   code = x / scale to the nearest of +-{0, .5, 1, 1.5, 2, 3, 4, 6}
+ * (ties to the even code, above 6 to 6).  A block that holds a NaN or an infinity has the scale NaN and stands for NaN.
+ *   codes   [rows][cprune_mx_blocks(C)][16 bytes], two to a byte, the lower channel in the low half; channels from C on are 0
+ *   scales  cprune_mx_scale_bytes(rows, C): exponent + 127, 255 for NaN, in tiles of 128 rows by 4 blocks as the tensor core takes
+ *           them: [rows / 128][blocks / 4][row % 32][row / 32 % 4][block % 4].  Blocks from C on are 0; rows from `rows` on stay as
+ *           they were.
+ *   x, values  CPRUNE_TYPE_BF16: bf16 [rows][c_pad], CPRUNE_TYPE_F32: float32 [rows][C]
+ * quantize writes the codes and scales (both or neither) and, unless NULL, the values that they stand for (what a layer sees in
+ * quantisation-aware training; may be x).  dequantize gives the values back.  Buffers of codes, scales and bf16: 16-byte aligned.
+ * pack: float32 weights [out][in] (the filters of a 1x1 layer are such) and biases [out] (NULL: zeros) -> codes, scales, float32
+ * [out_pad].
+ *
+ * Product:  y = act(q(x) W^T + b + residual), q the rounding above: float32 sums of exact products.
+ *   x  bf16 [rows][in_pad], a row per image or pixel;  residual  bf16 [rows][out_pad] or NULL;  act none, relu or relu6 (a NaN stays
+ *   one);  y  bf16 [rows][out_pad] (pad lanes zero) or float32 [rows][out] when out_is_f32; it may be residual, not x
+ *   workspace  cprune_mx_fc_workspace_bytes, device, 16-byte aligned
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (more than 2^20 - 16 rows of a product, 2^40 rows of a rounding, 2^24 channels),
+ * CUDA.  Enqueue only; at most three launches. */
+int cprune_mx_blocks(int C);
+size_t cprune_mx_scale_bytes(size_t rows, int C);
+cprune_status cprune_mx_quantize(const void *x, int type, size_t rows, int C, void *codes, void *scales, void *values, void *stream);
+cprune_status cprune_mx_dequantize(const void *codes, const void *scales, size_t rows, int C, int type, void *values, void *stream);
+cprune_status cprune_mx_pack(const float *w, const float *b, int out, int in, void *codes, void *scales, float *b_packed, void *stream);
+size_t cprune_mx_fc_workspace_bytes(size_t rows, int in, int out);
+cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes, const void *scales, const float *b_packed, int out, int act,
+                           const void *residual, int out_is_f32, void *y, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Fused inverted-residual block (the MobileNetV2 / MnasNet building block of the paper's Sec. 4.1 models): the three
  * tasks 1x1 expand + activation, 3x3 depthwise (stride 1, pad 1) + activation, 1x1 project (+ the block's input as

@@ -36,6 +36,8 @@ EXPORTS = [
     "cprune_selftest_wait_timeout", "cprune_block_plan", "cprune_block_query", "cprune_block_release", "cprune_block_pack",
     "cprune_block_run", "cprune_model_reads_image", "cprune_group_norm_workspace_bytes", "cprune_group_norm", "cprune_group_norm_backward",
     "cprune_gradient_workspace_bytes", "cprune_gradient_norm", "cprune_clip_gradients",
+    "cprune_mx_blocks", "cprune_mx_scale_bytes", "cprune_mx_quantize", "cprune_mx_dequantize", "cprune_mx_pack", "cprune_mx_fc_workspace_bytes",
+    "cprune_mx_fc",
 ]
 
 
@@ -146,6 +148,15 @@ def lib():
         L.cprune_gradient_workspace_bytes.argtypes = [c_int]
         L.cprune_gradient_norm.argtypes = [c_void_p] * 3 + [c_int] + [c_void_p] * 2 + [c_size_t, c_void_p]
         L.cprune_clip_gradients.argtypes = [c_void_p] * 3 + [c_int, c_float] + [c_void_p] * 3 + [c_size_t, c_void_p]
+        L.cprune_mx_blocks.argtypes = [c_int]
+        L.cprune_mx_scale_bytes.restype = c_size_t
+        L.cprune_mx_scale_bytes.argtypes = [c_size_t, c_int]
+        L.cprune_mx_quantize.argtypes = [c_void_p, c_int, c_size_t, c_int] + [c_void_p] * 4
+        L.cprune_mx_dequantize.argtypes = [c_void_p, c_void_p, c_size_t, c_int, c_int, c_void_p, c_void_p]
+        L.cprune_mx_pack.argtypes = [c_void_p, c_void_p, c_int, c_int] + [c_void_p] * 4
+        L.cprune_mx_fc_workspace_bytes.restype = c_size_t
+        L.cprune_mx_fc_workspace_bytes.argtypes = [c_size_t, c_int, c_int]
+        L.cprune_mx_fc.argtypes = [c_void_p, c_size_t, c_int] + [c_void_p] * 3 + [c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         _lib = L
     return _lib
 
@@ -610,6 +621,94 @@ def cprune_clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, 
     _check(lib().cprune_clip_gradients(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), max_norm, None if o is None else o.buffer_info()[0],
                                        norm.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)), where)
     return norm
+
+
+def _mx_rows(where, x, C):
+    """(rows, type) of x, a tensor [..., channels in memory]."""
+    if x.dtype not in TYPE or x.dim() < 1 or C < 1:
+        _refuse(where, "x has to be a bf16 or float32 tensor [..., channels in memory]")
+    lanes = cprune_padded_channels(C) if x.dtype == torch.bfloat16 else C
+    if x.shape[-1] != lanes:
+        _refuse(where, "x has %d channels in memory; %d channels take %d" % (x.shape[-1], C, lanes))
+    return x.numel() // lanes, TYPE[x.dtype]
+
+
+def _mx_shapes(rows, C):
+    """Shapes of the codes and of the scales."""
+    blocks = -(-C // 32)
+    return (rows, blocks * 16), (-(-rows // 128), -(-blocks // 4), 32, 4, 4)
+
+
+def cprune_mx_quantize(x, C, codes=None, scales=None, values=False, stream=None):
+    """x (bf16 [..., c_pad] or float32 [..., C]) rounded to MXFP4 along its channels.  Returns (codes uint8 [rows, blocks * 16], scales uint8
+    [rows / 128, blocks / 4, 32, 4, 4], values): values is None, or with values=True (or a tensor like x, which may be x) what the codes
+    stand for, in the form of x."""
+    where = "cprune_mx_quantize"
+    rows, typ = _mx_rows(where, x, C)
+    shape_c, shape_s = _mx_shapes(rows, C)
+    px = _checked(where, "x", x, x.shape, x.dtype)
+    if codes is None:
+        codes = _empty(stream, shape_c, torch.uint8, x.device)
+    if scales is None:
+        scales = _empty(stream, shape_s, torch.uint8, x.device)
+    values = None if values is False else _empty(stream, x.shape, x.dtype, x.device) if values is True else values
+    _check(lib().cprune_mx_quantize(px, typ, rows, C, _checked(where, "codes", codes, shape_c, torch.uint8), _checked(where, "scales", scales, shape_s, torch.uint8),
+                                    _checked(where, "values", values, x.shape, x.dtype), _stream(stream)), where)
+    return codes, scales, values
+
+
+def cprune_mx_dequantize(codes, scales, C, dtype=torch.float32, stream=None):
+    """The values [rows, channels in memory] that codes and scales of C channels stand for."""
+    where = "cprune_mx_dequantize"
+    if dtype not in TYPE or codes.dim() != 2 or C < 1:
+        _refuse(where, "codes have to be a tensor [rows, blocks * 16], dtype bf16 or float32")
+    rows = codes.shape[0]
+    shape_c, shape_s = _mx_shapes(rows, C)
+    pc, ps = _checked(where, "codes", codes, shape_c, torch.uint8), _checked(where, "scales", scales, shape_s, torch.uint8)
+    values = _empty(stream, (rows, cprune_padded_channels(C) if dtype == torch.bfloat16 else C), dtype, codes.device)
+    _check(lib().cprune_mx_dequantize(pc, ps, rows, C, TYPE[dtype], values.data_ptr(), _stream(stream)), where)
+    return values
+
+
+def cprune_mx_pack(w, b=None, stream=None):
+    """Weights float32 [out, in] (or the filters [out, in, 1, 1] of a 1x1 layer) and biases -> (codes, scales, bias padded to the channels in memory)
+    for cprune_mx_fc."""
+    where = "cprune_mx_pack"
+    if w.dim() not in (2, 4) or w[0].numel() != w.shape[1]:
+        _refuse(where, "w has to be [out, in] or [out, in, 1, 1]")
+    out, inn = w.shape[:2]
+    pw, pb = _checked(where, "w", w, w.shape, torch.float32), _checked(where, "b", b, (out,), torch.float32)
+    shape_c, shape_s = _mx_shapes(out, inn)
+    codes, scales = _empty(stream, shape_c, torch.uint8, w.device), _empty(stream, shape_s, torch.uint8, w.device)
+    bp = _empty(stream, (cprune_padded_channels(out),), torch.float32, w.device)
+    _check(lib().cprune_mx_pack(pw, pb, out, inn, codes.data_ptr(), scales.data_ptr(), bp.data_ptr(), _stream(stream)), where)
+    return codes, scales, bp
+
+
+def cprune_mx_fc(x, in_features, codes, scales, b_packed, out_features, activation="none", residual=None, out_f32=False, y=None, workspace=None, stream=None):
+    """act(q(x) W^T + b + residual): x bf16 [..., in_pad], a row per image or pixel, rounded to MXFP4 on the way in; W and b from cprune_mx_pack;
+    residual bf16 [..., out_pad].  Returns y, bf16 [..., out_pad] or float32 [..., out_features]; y may be residual."""
+    where = "cprune_mx_fc"
+    if x.dtype != torch.bfloat16:
+        _refuse(where, "x has to be bf16")
+    if activation not in ACT:
+        _refuse(where, "unknown activation %r" % (activation,))
+    if out_features < 1:
+        _refuse(where, "no output features")
+    rows, _ = _mx_rows(where, x, in_features)
+    out_pad = cprune_padded_channels(out_features)
+    shape_c, shape_s = _mx_shapes(out_features, in_features)
+    px = _checked(where, "x", x, x.shape, torch.bfloat16)
+    pc, ps = _checked(where, "codes", codes, shape_c, torch.uint8), _checked(where, "scales", scales, shape_s, torch.uint8)
+    pb, pr = _checked(where, "b_packed", b_packed, (out_pad,), torch.float32), _checked(where, "residual", residual, x.shape[:-1] + (out_pad,), torch.bfloat16)
+    shape, dtype = (x.shape[:-1] + (out_features,), torch.float32) if out_f32 else (x.shape[:-1] + (out_pad,), torch.bfloat16)
+    if y is None:
+        y = _empty(stream, shape, dtype, x.device)
+    if workspace is None:
+        workspace = _empty(stream, (lib().cprune_mx_fc_workspace_bytes(rows, in_features, out_features),), torch.uint8, x.device)
+    _check(lib().cprune_mx_fc(px, rows, in_features, pc, ps, pb, out_features, ACT[activation], pr, 1 if out_f32 else 0, _checked(where, "y", y, shape, dtype),
+                              _checked(where, "workspace", workspace, (workspace.numel(),), torch.uint8), workspace.numel(), _stream(stream)), where)
+    return y
 
 
 class Model:

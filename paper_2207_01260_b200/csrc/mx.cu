@@ -1,0 +1,354 @@
+// Rounding to MXFP4 and back, and the product with weights kept in it.
+//
+//   rounding   block by block of 32 channels: scale = 2^(floor(log2 max |x|) - 2), code = x / scale to the nearest E2M1 value.
+//              Both are exact but for the one rounding: the scale is a power of two.
+//   product    y = act(q(x) W^T + b + residual), q the rounding above: 4-bit values on both sides, whose products are exact; float32 sums.
+#include <cmath>
+
+#include "common.cuh"
+#include "mx.cuh"
+
+namespace cprune {
+
+// ------------------------------------------------------------------------------------------------------- rounding
+
+// Where the eight values that begin at channel c of a row come from.  TYPE 0: bf16 rows of c_pad channels; 1: float32 rows on 16-byte boundaries;
+// 2: float32 rows at any address.  Channels from C on are zeros.
+template <int TYPE>
+__device__ __forceinline__ void read_eight(const void *x, size_t row, int c, int C, int pitch, float *f) {
+    if (TYPE == 0) {
+        bf16x8 v = {{0u, 0u, 0u, 0u}};
+        if (c < pitch) v = ldg8((const bf16x8 *)((const __nv_bfloat16 *)x + row * pitch + c));
+        unpack8(v, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i >= C) f[i] = 0.f;
+    } else {
+        const float *p = (const float *)x + row * pitch + c;
+        if (TYPE == 1) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (c + 4 * h < C) v = __ldg((const float4 *)p + h);       // (C is a multiple of 4)
+                f[4 * h] = v.x; f[4 * h + 1] = v.y; f[4 * h + 2] = v.z; f[4 * h + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = c + i < C ? __ldg(p + i) : 0.f;
+        }
+    }
+}
+
+// The exact values of codes, in the form of x (pad lanes zero)
+template <int TYPE>
+__device__ __forceinline__ void write_eight(void *y, size_t row, int c, int C, int pitch, float *f) {
+    if (TYPE == 0) {
+        if (c >= pitch) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i >= C) f[i] = 0.f;
+        *(bf16x8 *)((__nv_bfloat16 *)y + row * pitch + c) = pack8(f);
+    } else {
+        float *p = (float *)y + row * pitch + c;
+        if (TYPE == 1) {
+            if (c < C) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+            if (c + 4 < C) *((float4 *)p + 1) = make_float4(f[4], f[5], f[6], f[7]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < C) p[i] = f[i];
+        }
+    }
+}
+
+constexpr int MX_T = 256;
+
+// 16 threads take four blocks (128 channels) of a row, eight values each: loads and stores of neighbouring threads adjoin, and the four scales are
+// one word of a tile of scales.  FORM 0: codes and scales (either both or neither), values as x; 1: the values in blocks, bf16 [rows][blocks * 32], in
+// the order 0 4 1 5 2 6 3 7 of every eight (the order in which mx_pair takes codes apart).
+template <int TYPE, int FORM>
+__global__ void __launch_bounds__(MX_T) mx_quantize_kernel(const void *__restrict__ x, unsigned long long rows, int C, int pitch, int tiles4, uint32_t *__restrict__ codes,
+                                                           uint8_t *__restrict__ scales, void *__restrict__ values) {
+    pdl_wait();
+    pdl_trigger();
+    const int blocks = (C + MX_BLOCK - 1) / MX_BLOCK, sub = threadIdx.x & 15;
+    const unsigned long long units = rows * tiles4;
+    // (whole warps go round: the shuffles below need all lanes)
+    for (unsigned long long u0 = ((unsigned long long)blockIdx.x * MX_T + (threadIdx.x & ~31)) / 16; u0 < units; u0 += (unsigned long long)gridDim.x * (MX_T / 16)) {
+        const unsigned long long u = u0 + ((threadIdx.x >> 4) & 1);
+        const bool in = u < units;
+        const size_t row = in ? u / tiles4 : 0;
+        const int tile = in ? (int)(u - row * tiles4) : 0, c = tile * 128 + sub * 8, block = tile * 4 + (sub >> 2);
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 0.f;
+        if (in && block < blocks) read_eight<TYPE>(x, row, c, C, pitch, f);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const uint32_t code = mx_scale_code(top);
+        const float inverse = mx_inverse(code);
+        float q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = code == MX_NAN ? 0.f : f[i] * inverse;
+        const uint32_t w = mx_codes(q);
+        if (FORM == 0 && codes) {
+            const uint32_t s0 = __shfl_sync(0xffffffffu, code, threadIdx.x & 16), s1 = __shfl_sync(0xffffffffu, code, (threadIdx.x & 16) + 4);
+            const uint32_t s2 = __shfl_sync(0xffffffffu, code, (threadIdx.x & 16) + 8), s3 = __shfl_sync(0xffffffffu, code, (threadIdx.x & 16) + 12);
+            if (in && block < blocks) codes[(row * blocks + block) * 4 + (sub & 3)] = w;
+            if (in && sub == 0) *(uint32_t *)(scales + mx_scale_at((long long)row, tile * 4, tiles4)) = s0 | s1 << 8 | s2 << 16 | s3 << 24;
+        }
+        if (values && in && block < blocks) {
+            mx_values(w, mx_scale(code), f);
+            if (FORM == 0) write_eight<TYPE>(values, row, c, C, pitch, f);
+            else {
+                const float g[8] = {f[0], f[4], f[1], f[5], f[2], f[6], f[3], f[7]};
+                *(bf16x8 *)((__nv_bfloat16 *)values + row * ((size_t)blocks * MX_BLOCK) + c) = pack8(g);
+            }
+        }
+    }
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(MX_T) mx_dequantize_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales, unsigned long long rows, int C, int pitch,
+                                                             int tiles4, void *__restrict__ values) {
+    pdl_wait();
+    pdl_trigger();
+    const int eights = TYPE == 0 ? pitch / 8 : (C + 7) / 8, blocks = (C + MX_BLOCK - 1) / MX_BLOCK;
+    const unsigned long long total = rows * eights;
+    for (unsigned long long e = (unsigned long long)blockIdx.x * MX_T + threadIdx.x; e < total; e += (unsigned long long)gridDim.x * MX_T) {
+        const size_t row = e / eights;
+        const int c = (int)(e - row * eights) * 8, block = c / MX_BLOCK;
+        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (block < blocks) mx_values(__ldg(codes + (row * blocks + block) * 4 + (c & 31) / 8), mx_scale(__ldg(scales + mx_scale_at((long long)row, block, tiles4))), f);
+        write_eight<TYPE>(values, row, c, C, pitch, f);
+    }
+}
+
+__global__ void mx_pad_bias_kernel(const float *__restrict__ b, int n, int n_pad, float *__restrict__ out) {
+    pdl_wait();
+    pdl_trigger();
+    const int k = blockIdx.x * blockDim.x + threadIdx.x;
+    if (k < n_pad) out[k] = (b && k < n) ? b[k] : 0.f;
+}
+
+// --------------------------------------------------------------------------------------------- product, few rows
+
+// A block takes 16 rows and 16 features; its eight warps share out the channels, and their sums meet in shared memory.  A thread reads
+// a whole block of 32 codes of a feature (16 bytes), makes bf16 values of them, which hold 4-bit values times any power of two exactly, and
+// takes the same 32 channels of its two rows: eight MMA steps, in an order of the channels that both sides share.
+// The tensor core truncates where it adds to an accumulator; four steps start from zero and are added to the running sum by a rounded
+// addition, and the warps' sums meet in float64.
+constexpr int MXF_WARPS = 8, MXF_NT = 2, MXF_AHEAD = 2;
+
+struct MxProduct {
+    const uint4 *codes;                    // weights [out][blocks] of 16 bytes
+    const uint8_t *scales;
+    const float *bias;
+    const __nv_bfloat16 *res;
+    void *y;
+    unsigned long long rows;
+    int blocks, tiles4, out, out_pad, act, out_is_f32;
+};
+
+// (one float32 of y, in its form)
+__device__ __forceinline__ void mx_store(const MxProduct &p, unsigned long long n, int o, float v) {
+    if (p.out_is_f32) {
+        if (o < p.out) ((float *)p.y)[n * p.out + o] = v;
+    } else ((__nv_bfloat16 *)p.y)[n * p.out_pad + o] = __float2bfloat16_rn(o < p.out ? v : 0.f);
+}
+
+// relu and relu6 that keep a NaN
+__device__ __forceinline__ float mx_act(float v, int act) {
+    if (act == CPRUNE_ACT_NONE) return v;
+    v = v < 0.f ? 0.f : v;
+    return act == CPRUNE_ACT_RELU6 && v > 6.f ? 6.f : v;
+}
+
+__global__ void __launch_bounds__(MXF_WARPS * 32) mx_few_rows_kernel(const bf16x8 *__restrict__ x, const MxProduct p) {
+    __shared__ float part[MXF_WARPS][16][MXF_NT * 8 + 1];
+    pdl_trigger();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int o0 = blockIdx.x * (MXF_NT * 8);
+    const unsigned long long n0 = (unsigned long long)blockIdx.y * 16;
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    struct Piece { uint4 w; uint32_t scale; };
+    auto load_w = [&](int c, Piece *v) {
+        const int b = c * 4 + t;
+#pragma unroll
+        for (int f = 0; f < MXF_NT; ++f) {
+            const int o = o0 + f * 8 + g;
+            const bool in = b < p.blocks && o < p.out;
+            v[f].w = in ? __ldg(p.codes + (size_t)o * p.blocks + b) : none;
+            v[f].scale = in ? __ldg(p.scales + mx_scale_at(o, b, p.tiles4)) : 127;
+        }
+    };
+    const int chunks = (p.blocks + 3) / 4;
+    Piece wq[MXF_AHEAD][MXF_NT];
+#pragma unroll
+    for (int i = 0; i < MXF_AHEAD; ++i) load_w(warp + i * MXF_WARPS, wq[i]);
+    pdl_wait();
+    float acc[MXF_NT][4];
+#pragma unroll
+    for (int f = 0; f < MXF_NT; ++f)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[f][j] = 0.f;
+    const bf16x8 zero = {{0u, 0u, 0u, 0u}};
+    for (int c0 = warp; c0 < chunks; c0 += MXF_AHEAD * MXF_WARPS) {
+#pragma unroll
+        for (int i = 0; i < MXF_AHEAD; ++i) {
+            const int c = c0 + i * MXF_WARPS, b = c * 4 + t;
+            if (c >= chunks) break;
+            bf16x8 xq[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned long long n = n0 + h * 8 + g;
+                const bool in = n < p.rows && b < p.blocks;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) xq[h][q] = in ? ldg8(x + (n * p.blocks + b) * 4 + q) : zero;
+            }
+#pragma unroll
+            for (int f = 0; f < MXF_NT; ++f) {
+                const uint32_t code = wq[i][f].scale;
+                // 2^126 and the scale in one factor, but for scales above 2 (whose factor would leave the type)
+                const uint32_t top = min(code, 128u);
+                const uint32_t lifted = code == MX_NAN ? 0x7fffu : (top + 126u) << 7, above = code > 128u && code != MX_NAN ? (code - 1u) << 7 : 0x3f80u;
+                uint32_t m1 = lifted * 0x10001u, m2 = above * 0x10001u;
+                const bool two = code > 128u && code != MX_NAN;
+                auto value = [&](uint32_t v) {
+                    __nv_bfloat162 r = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&v), *reinterpret_cast<__nv_bfloat162 *>(&m1));
+                    if (two) r = __hmul2(r, *reinterpret_cast<__nv_bfloat162 *>(&m2));
+                    return *reinterpret_cast<uint32_t *>(&r);
+                };
+                const uint32_t words[4] = {wq[i][f].w.x, wq[i][f].w.y, wq[i][f].w.z, wq[i][f].w.w};
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int q = 2 * hh; q < 2 * hh + 2; ++q) {
+                        mma_16816(s, xq[0][q].w[0], xq[1][q].w[0], xq[0][q].w[1], xq[1][q].w[1], value(mx_pair<0>(words[q])), value(mx_pair<1>(words[q])));
+                        mma_16816(s, xq[0][q].w[2], xq[1][q].w[2], xq[0][q].w[3], xq[1][q].w[3], value(mx_pair<2>(words[q])), value(mx_pair<3>(words[q])));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[f][j] += s[j];
+                }
+            }
+            load_w(c + MXF_AHEAD * MXF_WARPS, wq[i]);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < MXF_NT; ++f)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[warp][(j >> 1) * 8 + g][f * 8 + t * 2 + (j & 1)] = acc[f][j];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * MXF_NT * 8; e += MXF_WARPS * 32) {
+        const int r = e / (MXF_NT * 8), c = e % (MXF_NT * 8), o = o0 + c;
+        const unsigned long long n = n0 + r;
+        if (n >= p.rows || o >= p.out_pad) continue;
+        double s = 0.0;
+#pragma unroll
+        for (int q = 0; q < MXF_WARPS; ++q) s += part[q][r][c];
+        float v = o < p.out ? (float)(s + (double)p.bias[o]) : 0.f;
+        if (p.res && o < p.out) v += __bfloat162float(p.res[n * p.out_pad + o]);
+        mx_store(p, n, o, mx_act(v, p.act));
+    }
+}
+
+static unsigned mx_grid(unsigned long long units, int per_block) {
+    const unsigned long long b = (units + per_block - 1) / per_block;
+    return (unsigned)(b < 1 ? 1 : b < 148 * 16 ? b : 148 * 16);
+}
+
+static int mx_type(int type, int C, uintptr_t addresses) { return type == CPRUNE_TYPE_BF16 ? 0 : C % 4 == 0 && !(addresses & 15) ? 1 : 2; }
+
+}  // namespace cprune
+
+using namespace cprune;
+
+extern "C" {
+
+int cprune_mx_blocks(int C) { return C > 0 ? mx_blocks(C) : 0; }
+
+size_t cprune_mx_scale_bytes(size_t rows, int C) { return C > 0 ? (rows + 127) / 128 * (size_t)((mx_blocks(C) + 3) / 4) * 512 : 0; }
+
+static cprune_status mx_check(const void *x, int type, size_t rows, int C, const void *codes, const void *scales) {
+    if (!x || (type != CPRUNE_TYPE_BF16 && type != CPRUNE_TYPE_F32) || rows == 0 || C <= 0 || !codes != !scales) return CPRUNE_ERR_INVALID_ARG;
+    if (((uintptr_t)codes | (uintptr_t)scales) & 15 || (uintptr_t)x & (type == CPRUNE_TYPE_BF16 ? 15 : 3)) return CPRUNE_ERR_INVALID_ARG;
+    if (rows >> 40 || C > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
+    return CPRUNE_OK;
+}
+
+cprune_status cprune_mx_quantize(const void *x, int type, size_t rows, int C, void *codes, void *scales, void *values, void *stream) {
+    const cprune_status c = mx_check(x, type, rows, C, codes, scales);
+    if (c != CPRUNE_OK) return c;
+    if ((!codes && !values) || (uintptr_t)values & (type == CPRUNE_TYPE_BF16 ? 15 : 3)) return CPRUNE_ERR_INVALID_ARG;
+    const int tiles4 = (mx_blocks(C) + 3) / 4, pitch = type == CPRUNE_TYPE_BF16 ? cprune_padded_channels(C) : C;
+    const unsigned grid = mx_grid(rows * tiles4, MX_T / 16);
+    auto launch = [&](auto kernel) {
+        return launch_chained(kernel, dim3(grid), dim3(MX_T), 0, (cudaStream_t)stream, x, (unsigned long long)rows, C, pitch, tiles4, (uint32_t *)codes, (uint8_t *)scales, values);
+    };
+    switch (mx_type(type, C, (uintptr_t)x | (uintptr_t)values)) {
+        case 0: CPRUNE_CUDA_CHECK(launch(mx_quantize_kernel<0, 0>)); break;
+        case 1: CPRUNE_CUDA_CHECK(launch(mx_quantize_kernel<1, 0>)); break;
+        default: CPRUNE_CUDA_CHECK(launch(mx_quantize_kernel<2, 0>));
+    }
+    return CPRUNE_OK;
+}
+
+cprune_status cprune_mx_dequantize(const void *codes, const void *scales, size_t rows, int C, int type, void *values, void *stream) {
+    if (!codes) return CPRUNE_ERR_INVALID_ARG;
+    const cprune_status c = mx_check(values, type, rows, C, codes, scales);
+    if (c != CPRUNE_OK) return c;
+    const int tiles4 = (mx_blocks(C) + 3) / 4, pitch = type == CPRUNE_TYPE_BF16 ? cprune_padded_channels(C) : C;
+    const unsigned grid = mx_grid(rows * ((pitch + 7) / 8), MX_T);
+    auto launch = [&](auto kernel) {
+        return launch_chained(kernel, dim3(grid), dim3(MX_T), 0, (cudaStream_t)stream, (const uint32_t *)codes, (const uint8_t *)scales, (unsigned long long)rows, C, pitch, tiles4,
+                              values);
+    };
+    switch (mx_type(type, C, (uintptr_t)values)) {
+        case 0: CPRUNE_CUDA_CHECK(launch(mx_dequantize_kernel<0>)); break;
+        case 1: CPRUNE_CUDA_CHECK(launch(mx_dequantize_kernel<1>)); break;
+        default: CPRUNE_CUDA_CHECK(launch(mx_dequantize_kernel<2>));
+    }
+    return CPRUNE_OK;
+}
+
+cprune_status cprune_mx_pack(const float *w, const float *b, int out, int in, void *codes, void *scales, float *b_packed, void *stream) {
+    if (!codes || !b_packed || out <= 0 || ((uintptr_t)b | (uintptr_t)b_packed) & 3) return CPRUNE_ERR_INVALID_ARG;
+    ChainScope chain;
+    const cprune_status s = cprune_mx_quantize(w, CPRUNE_TYPE_F32, out, in, codes, scales, nullptr, stream);
+    if (s != CPRUNE_OK) return s;
+    chain.follow();
+    const int out_pad = cprune_padded_channels(out);
+    CPRUNE_CUDA_CHECK(launch_chained(mx_pad_bias_kernel, dim3((out_pad + 255) / 256), dim3(256), 0, (cudaStream_t)stream, b, out, out_pad, b_packed));
+    return CPRUNE_OK;
+}
+
+size_t cprune_mx_fc_workspace_bytes(size_t rows, int in, int out) {
+    if (rows == 0 || in <= 0 || out <= 0) return 0;
+    return rows * (size_t)mx_blocks(in) * MX_BLOCK * 2;
+}
+
+cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes, const void *scales, const float *b_packed, int out, int act, const void *residual,
+                           int out_is_f32, void *y, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!x || !codes || !scales || !b_packed || !y || rows == 0 || in <= 0 || out <= 0 || act < CPRUNE_ACT_NONE || act > CPRUNE_ACT_RELU6) return CPRUNE_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)residual | (uintptr_t)workspace) & 15 || (uintptr_t)b_packed & 3) return CPRUNE_ERR_INVALID_ARG;
+    if ((uintptr_t)y & (out_is_f32 ? 3 : 15)) return CPRUNE_ERR_INVALID_ARG;
+    if (rows > 16ull * 65535 || in > (1 << 24) || out > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
+    if (!workspace || workspace_bytes < cprune_mx_fc_workspace_bytes(rows, in, out)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    cudaStream_t st = (cudaStream_t)stream;
+    MxProduct p = {};
+    p.codes = (const uint4 *)codes; p.scales = (const uint8_t *)scales; p.bias = b_packed; p.res = (const __nv_bfloat16 *)residual; p.y = y; p.rows = rows;
+    p.blocks = mx_blocks(in); p.tiles4 = (p.blocks + 3) / 4; p.out = out; p.out_pad = cprune_padded_channels(out); p.act = act; p.out_is_f32 = out_is_f32;
+    ChainScope chain;
+    CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 1>, dim3(mx_grid(rows * p.tiles4, MX_T / 16)), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
+                                     cprune_padded_channels(in), p.tiles4, (uint32_t *)nullptr, (uint8_t *)nullptr, workspace));
+    chain.follow();
+    const dim3 grid((p.out_pad + MXF_NT * 8 - 1) / (MXF_NT * 8), (unsigned)((rows + 15) / 16));
+    CPRUNE_CUDA_CHECK(launch_chained(mx_few_rows_kernel, grid, dim3(MXF_WARPS * 32), 0, st, (const bf16x8 *)workspace, p));
+    return CPRUNE_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,65 @@
+// 4-bit values of the OCP Microscaling formats (MXFP4): E2M1 codes in blocks of 32 along the channels, an E8M0 scale to a block.
+#pragma once
+
+#include "common.cuh"
+
+namespace cprune {
+
+constexpr int MX_BLOCK = 32;
+constexpr uint32_t MX_NAN = 255;          // the scale of a block without a value
+
+inline int mx_blocks(int C) { return (C + MX_BLOCK - 1) / MX_BLOCK; }
+
+// Where the scale of a row's block lies: tiles of 128 rows by 4 blocks (512 bytes, the order in which the tensor core takes them),
+// [rows / 128][blocks / 4][row % 32][row / 32 % 4][block % 4]
+__host__ __device__ __forceinline__ size_t mx_scale_at(long long row, int block, int tiles4) {
+    return ((size_t)(row >> 7) * tiles4 + (block >> 2)) * 512 + (size_t)((row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3));
+}
+
+// The scale's code of a block whose largest magnitude has these bits (of the absolute values: a NaN's are the largest).
+// 2^(floor(log2 top) - 2), the two being the exponent of the format's largest value 6; not below 2^-127
+__device__ __forceinline__ uint32_t mx_scale_code(uint32_t top) {
+    const int e = (int)(top >> 23);
+    return e == 255 ? MX_NAN : (uint32_t)max(e - 2, 0);
+}
+__device__ __forceinline__ float mx_scale(uint32_t code) {
+    return __uint_as_float(code == MX_NAN ? 0x7fffffffu : code == 0 ? 0x00400000u : code << 23);
+}
+// 1 / scale (a power of two: products with it are exact)
+__device__ __forceinline__ float mx_inverse(uint32_t code) { return code == MX_NAN ? 0.f : __uint_as_float((254u - code) << 23); }
+
+// Eight values, already divided by the scale, to the nearest codes (ties to the even code, above 6 to 6); value i in bits 4 i
+__device__ __forceinline__ uint32_t mx_codes(const float *f) {
+    uint32_t r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r)
+        : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
+    return r;
+}
+
+// A code's bits s ee m are those of a bf16 with exponent field ee, which is the code's value times 2^-126 (subnormal codes included).
+// Codes i and i + 4 of a word as such bf16:
+template <int I>
+__device__ __forceinline__ uint32_t mx_pair(uint32_t w) {
+    const uint32_t s = I < 3 ? w << (12 - 4 * I) : w >> (4 * I - 12);
+    const uint32_t e = I == 0 ? w << 6 : I == 1 ? w << 2 : I == 2 ? w >> 2 : w >> 6;
+    return (s & 0x80008000u) | (e & 0x01C001C0u);
+}
+
+// Eight codes to float32 (times the scale)
+__device__ __forceinline__ void mx_values(uint32_t w, float scale, float *f) {
+    const uint32_t p[4] = {mx_pair<0>(w), mx_pair<1>(w), mx_pair<2>(w), mx_pair<3>(w)};
+    const float up = __uint_as_float(253u << 23);      // 2^126
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = __uint_as_float(p[i] << 16) * up * scale;
+        f[i + 4] = __uint_as_float(p[i] & 0xffff0000u) * up * scale;
+    }
+}
+
+}  // namespace cprune

@@ -15,7 +15,10 @@
 // The variance is never a difference of large sums: a thread takes the deviations from its own mean, and means and deviations are put
 // together pairwise (Chan, Golub, LeVeque 1979), in float32.
 #include <cmath>
+#include <mutex>
+#include <set>
 #include <type_traits>
+#include <utility>
 
 #include "common.cuh"
 #include "sm100_ptx.cuh"
@@ -24,32 +27,58 @@ namespace cprune {
 
 // ------------------------------------------------------------------------------------------------ vectors of channels
 
+// Two float32 in one register pair: additions and fused multiply-adds of such pairs are one instruction
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 two(float lo, float hi) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 one_by_one(f2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// L channels of a vector as NP pairs (a single channel: with a zero)
 template <int KIND> struct Lanes;       // 0: 8 bf16, 1: 4 float32, 2: one float32
 template <> struct Lanes<0> {
-    static constexpr int L = 8;
+    static constexpr int L = 8, NP = 4;
     using Raw = bf16x8;
-    static __device__ __forceinline__ void unpack(const Raw &r, float *f) { unpack8(r, f); }
+    static __device__ __forceinline__ void unpack(const Raw &r, f2 *f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = two(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u));
+    }
     static __device__ __forceinline__ Raw pack(const float *f) { return pack8(f); }
 };
 template <> struct Lanes<1> {
-    static constexpr int L = 4;
+    static constexpr int L = 4, NP = 2;
     using Raw = float4;
-    static __device__ __forceinline__ void unpack(const Raw &r, float *f) { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
+    static __device__ __forceinline__ void unpack(const Raw &r, f2 *f) { f[0] = two(r.x, r.y); f[1] = two(r.z, r.w); }
     static __device__ __forceinline__ Raw pack(const float *f) { return make_float4(f[0], f[1], f[2], f[3]); }
 };
 template <> struct Lanes<2> {
-    static constexpr int L = 1;
+    static constexpr int L = 1, NP = 1;
     using Raw = float;
-    static __device__ __forceinline__ void unpack(const Raw &r, float *f) { f[0] = r; }
+    static __device__ __forceinline__ void unpack(const Raw &r, f2 *f) { f[0] = two(r, 0.f); }
     static __device__ __forceinline__ Raw pack(const float *f) { return f[0]; }
 };
-
-// An activation that keeps NaN (apply_act's maximum would drop it), and its slope: 0 on the borders of relu and relu6.
-__device__ __forceinline__ float norm_act(float z, int act) {
-    if (act == CPRUNE_ACT_NONE) return z;
-    if (act == CPRUNE_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
-    z = z < 0.f ? 0.f : z;
-    return act == CPRUNE_ACT_RELU6 && z > 6.f ? 6.f : z;
+template <int KIND>
+__device__ __forceinline__ void unpack_floats(const typename Lanes<KIND>::Raw &r, float *f) {
+    f2 v[Lanes<KIND>::NP];
+    Lanes<KIND>::unpack(r, v);
+#pragma unroll
+    for (int l = 0; l < Lanes<KIND>::L; ++l) f[l] = l % 2 ? one_by_one(v[l / 2]).y : one_by_one(v[l / 2]).x;
 }
 
 struct NormParams {
@@ -66,172 +95,304 @@ struct NormParams {
     int rows;                           // R: pixels that the block's threads hold side by side
     int per;                            // pixels of a block (on chip: of a rank; else: of a chunk)
     int chunks;
+    int gs, data_bytes;                 // on chip: groups of a slice, bytes of a tensor's share of a block
     int act;
     float eps;
 };
 
-// The side of relu's and relu6's borders on which z lies decides about a whole gradient, so next to a border it is taken in 64 bits.
-__device__ __noinline__ float slope_64(float x, float mean, float rstd, float gamma, float beta, float res, int act) {
-    const double z = ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)beta + (double)res;
-    return z > 0.0 && (act != CPRUNE_ACT_RELU6 || z < 6.0) ? 1.f : (z == z ? 0.f : (float)z);
+__device__ __forceinline__ float sigmoid(float z) {
+    float e, r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+    return r;
 }
 
-// act'(z)
-__device__ __forceinline__ float norm_slope(float x, float mean, float rstd, float gamma, float beta, float res, float xhat, int act) {
-    if (act == CPRUNE_ACT_NONE) return 1.f;
-    const float t = xhat * gamma, z = t + beta + res;
-    if (act == CPRUNE_ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + __expf(-z));
-        return s * (1.f + z * (1.f - s));
-    }
-    // x - mean, its products with rstd and gamma and the two sums are rounded: five times 2^-24 of the largest term bounds the error of z
-    const float near = 4e-7f * (fabsf(t) + fabsf(beta) + fabsf(res));
-    if (fabsf(z) <= near || (act == CPRUNE_ACT_RELU6 && fabsf(z - 6.f) <= near)) return slope_64(x, mean, rstd, gamma, beta, res, act);
-    return z > 0.f && (act != CPRUNE_ACT_RELU6 || z < 6.f) ? 1.f : (z == z ? 0.f : z);
-}
-
-// What a thread needs of the channels of its column
-template <int L> struct Column {
-    float mean[L], rstd[L], gamma[L], beta[L];
-    __device__ __forceinline__ void load_affine(const NormParams &p, int c0) {
+// The activation of a vector, and its form in memory.  relu and relu6 keep a NaN (apply_act's maximum would drop it); 0 and 6 are bf16 values, so that a
+// bf16 result is clamped after its rounding, two at a time.
+template <int KIND, int ACT>
+__device__ __forceinline__ typename Lanes<KIND>::Raw finish(const f2 *z) {
+    constexpr int NP = Lanes<KIND>::NP;
+    float f[2 * NP];
 #pragma unroll
-        for (int l = 0; l < L; ++l) {
-            const bool in = c0 + l < p.C;
-            gamma[l] = in ? (p.gamma ? __ldg(p.gamma + c0 + l) : 1.f) : 0.f;
-            beta[l] = in && p.beta ? __ldg(p.beta + c0 + l) : 0.f;
-            mean[l] = rstd[l] = 0.f;
+    for (int i = 0; i < NP; ++i) {
+        const float2 v = one_by_one(z[i]);
+        f[2 * i] = v.x;
+        f[2 * i + 1] = v.y;
+    }
+    if (ACT == CPRUNE_ACT_SILU) {
+#pragma unroll
+        for (int l = 0; l < 2 * NP; ++l) f[l] *= sigmoid(f[l]);
+    }
+    if (KIND != 0 && (ACT == CPRUNE_ACT_RELU || ACT == CPRUNE_ACT_RELU6)) {
+#pragma unroll
+        for (int l = 0; l < 2 * NP; ++l) {
+            asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(f[l]));
+            if (ACT == CPRUNE_ACT_RELU6) asm("min.NaN.f32 %0, %0, 0f40C00000;" : "+f"(f[l]));
         }
     }
+    typename Lanes<KIND>::Raw r = Lanes<KIND>::pack(f);
+    if constexpr (KIND == 0 && (ACT == CPRUNE_ACT_RELU || ACT == CPRUNE_ACT_RELU6)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(r.w[i]) : "r"(0u));
+            if (ACT == CPRUNE_ACT_RELU6) asm("min.NaN.bf16x2 %0, %0, %1;" : "+r"(r.w[i]) : "r"(0x40C040C0u));
+        }
+    }
+    return r;
+}
+
+// What a thread needs of the channels of its column: z = (x - mean) a + beta with a = rstd gamma.  (x - mean is taken first: multiplied out, a mean far
+// from zero would cancel.)  Lanes behind the last channel have zeros everywhere.
+template <int NP> struct Column {
+    f2 minus_mean[NP], a[NP], beta[NP];
+    float most;                         // the largest |beta|
 };
 
-template <int KIND>
-__device__ __forceinline__ void apply_one(const NormParams &p, const Column<Lanes<KIND>::L> &k, int c0, const typename Lanes<KIND>::Raw &x, size_t at) {
+// f(l) -> (-mean, rstd gamma, beta) of lane l of the column
+template <int KIND, typename F>
+__device__ __forceinline__ void fill_column(Column<Lanes<KIND>::NP> &k, F of) {
     constexpr int L = Lanes<KIND>::L;
-    using Raw = typename Lanes<KIND>::Raw;
-    float f[L], r[L];
-    Lanes<KIND>::unpack(x, f);
-    if (p.res) Lanes<KIND>::unpack(((const Raw *)p.res)[at], r);
+    float3 v[2 * Lanes<KIND>::NP];
+    k.most = 0.f;
 #pragma unroll
-    for (int l = 0; l < L; ++l) {
-        float z = (f[l] - k.mean[l]) * k.rstd[l] * k.gamma[l] + k.beta[l];
-        if (p.res) z += r[l];
-        f[l] = c0 + l < p.C ? norm_act(z, p.act) : 0.f;
+    for (int l = 0; l < 2 * Lanes<KIND>::NP; ++l) {
+        v[l] = l < L ? of(l) : make_float3(0.f, 0.f, 0.f);
+        k.most = fmaxf(k.most, fabsf(v[l].z));
     }
-    ((Raw *)p.out)[at] = Lanes<KIND>::pack(f);
+#pragma unroll
+    for (int i = 0; i < Lanes<KIND>::NP; ++i) {
+        k.minus_mean[i] = two(v[2 * i].x, v[2 * i + 1].x);
+        k.a[i] = two(v[2 * i].y, v[2 * i + 1].y);
+        k.beta[i] = two(v[2 * i].z, v[2 * i + 1].z);
+    }
+}
+// from global memory
+template <int KIND>
+__device__ __forceinline__ void load_column(const NormParams &p, Column<Lanes<KIND>::NP> &k, int n, int c0) {
+    fill_column<KIND>(k, [&](int l) {
+        const int c = c0 + l;
+        if (c >= p.C) return make_float3(0.f, 0.f, 0.f);
+        const float2 s = __ldcg((const float2 *)p.stats + (size_t)n * p.G + c / p.cpg);
+        return make_float3(-s.x, s.y * (p.gamma ? __ldg(p.gamma + c) : 1.f), p.beta ? __ldg(p.beta + c) : 0.f);
+    });
 }
 
-// dz and xhat of a vector
+// x - mean, and z
 template <int KIND>
-__device__ __forceinline__ void gradient_one(const NormParams &p, const Column<Lanes<KIND>::L> &k, const typename Lanes<KIND>::Raw &x,
-                                             const typename Lanes<KIND>::Raw &dy, const typename Lanes<KIND>::Raw &res, float *dz, float *xhat) {
+__device__ __forceinline__ void affine(const NormParams &p, const Column<Lanes<KIND>::NP> &k, const typename Lanes<KIND>::Raw &x, const typename Lanes<KIND>::Raw &res, f2 *d, f2 *z) {
+    constexpr int NP = Lanes<KIND>::NP;
+    Lanes<KIND>::unpack(x, d);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        d[i] = add2(d[i], k.minus_mean[i]);
+        z[i] = fma2(d[i], k.a[i], k.beta[i]);
+    }
+    if (p.res) {
+        f2 r[NP];
+        Lanes<KIND>::unpack(res, r);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) z[i] = add2(z[i], r[i]);
+    }
+}
+
+template <int KIND, int ACT>
+__device__ __forceinline__ void apply_one(const NormParams &p, const Column<Lanes<KIND>::NP> &k, const typename Lanes<KIND>::Raw &x, const typename Lanes<KIND>::Raw &res, size_t at) {
+    f2 d[Lanes<KIND>::NP], z[Lanes<KIND>::NP];
+    affine<KIND>(p, k, x, res, d, z);
+    ((typename Lanes<KIND>::Raw *)p.out)[at] = finish<KIND, ACT>(z);
+}
+
+// The side of relu's and relu6's borders on which z lies decides about a whole gradient, so next to a border z is taken in 64 bits: a bit
+// for each lane of the vector that is inside the borders, from what its z is made of.
+template <int KIND>
+__device__ __noinline__ uint32_t inside_64(const NormParams &p, typename Lanes<KIND>::Raw x, typename Lanes<KIND>::Raw res, int n, int c0) {
     constexpr int L = Lanes<KIND>::L;
     float f[L], r[L];
-    Lanes<KIND>::unpack(x, f);
+    unpack_floats<KIND>(x, f);
+    if (p.res) unpack_floats<KIND>(res, r);
+    uint32_t inside = 0;
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+        if (c0 + l >= p.C) continue;
+        const float2 s = __ldcg((const float2 *)p.stats + (size_t)n * p.G + (c0 + l) / p.cpg);
+        const double gamma = p.gamma ? __ldg(p.gamma + c0 + l) : 1.f, beta = p.beta ? __ldg(p.beta + c0 + l) : 0.f;
+        const double z = ((double)f[l] - (double)s.x) * (double)s.y * gamma + beta + (p.res ? (double)r[l] : 0.0);
+        if (z > 0.0 && (p.act != CPRUNE_ACT_RELU6 || z < 6.0)) inside |= 1u << l;
+    }
+    return inside;
+}
+
+// x - mean and dz of a vector of image n
+template <int KIND, int ACT>
+__device__ __forceinline__ void gradient_one(const NormParams &p, const Column<Lanes<KIND>::NP> &k, int n, int c0, const typename Lanes<KIND>::Raw &x,
+                                             const typename Lanes<KIND>::Raw &dy, const typename Lanes<KIND>::Raw &res, f2 *d, f2 *dz) {
+    constexpr int NP = Lanes<KIND>::NP, L = Lanes<KIND>::L;
+    f2 z[NP];
+    affine<KIND>(p, k, x, res, d, z);
     Lanes<KIND>::unpack(dy, dz);
-    if (p.res) Lanes<KIND>::unpack(res, r);
+    if (ACT == CPRUNE_ACT_NONE) return;
+    float f[2 * NP], g[2 * NP];
 #pragma unroll
-    for (int l = 0; l < L; ++l) {
-        xhat[l] = (f[l] - k.mean[l]) * k.rstd[l];
-        dz[l] *= norm_slope(f[l], k.mean[l], k.rstd[l], k.gamma[l], k.beta[l], p.res ? r[l] : 0.f, xhat[l], p.act);
+    for (int i = 0; i < NP; ++i) {
+        const float2 v = one_by_one(z[i]), w = one_by_one(dz[i]);
+        f[2 * i] = v.x; f[2 * i + 1] = v.y;
+        g[2 * i] = w.x; g[2 * i + 1] = w.y;
     }
+    if (ACT == CPRUNE_ACT_SILU) {
+#pragma unroll
+        for (int l = 0; l < L; ++l) {
+            const float s = sigmoid(f[l]), t = s * f[l];
+            g[l] *= fmaf(t, 1.f - s, s);
+        }
+    } else {
+        // Where z is next to 0, |(x - mean) a| is next to |beta + residual|; it is off by two roundings of 2^-24, the sums by one each
+        float r[2 * NP];
+        if (p.res) unpack_floats<KIND>(res, r);
+        const float near = 4e-7f * k.most, top = 6.f;
+        bool close = false;
+#pragma unroll
+        for (int l = 0; l < L; ++l) {
+            const float e = p.res ? fmaf(4e-7f, fabsf(r[l]), near) : near;
+            close |= fabsf(f[l]) < e || (ACT == CPRUNE_ACT_RELU6 && fabsf(f[l] - top) < e + 2.4e-6f);
+        }
+        if (close) {
+            const uint32_t inside = inside_64<KIND>(p, x, res, n, c0);
+#pragma unroll
+            for (int l = 0; l < L; ++l) f[l] = inside >> l & 1 ? 1.f : -1.f;
+        }
+#pragma unroll
+        for (int l = 0; l < L; ++l) g[l] = f[l] > 0.f && (ACT != CPRUNE_ACT_RELU6 || f[l] < top) ? g[l] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) dz[i] = two(g[2 * i], g[2 * i + 1]);
 }
 
-// ---------------------------------------------------------------------------------------------------- three launches
+// dx = a dz + c0 + c1 (x - mean),  c0 = -rstd m1, c1 = -rstd^2 m2
+template <int KIND>
+__device__ __forceinline__ void store_gradient(const NormParams &p, const Column<Lanes<KIND>::NP> &k, const f2 *k0, const f2 *k1, const f2 *d, const f2 *dz, size_t at) {
+    constexpr int NP = Lanes<KIND>::NP;
+    float f[2 * NP], g[2 * NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const float2 v = one_by_one(fma2(k.a[i], dz[i], fma2(d[i], k1[i], k0[i]))), w = one_by_one(dz[i]);
+        f[2 * i] = v.x; f[2 * i + 1] = v.y;
+        g[2 * i] = w.x; g[2 * i + 1] = w.y;
+    }
+    ((typename Lanes<KIND>::Raw *)p.out)[at] = Lanes<KIND>::pack(f);
+    if (p.dres) ((typename Lanes<KIND>::Raw *)p.dres)[at] = Lanes<KIND>::pack(g);
+}
+
+// f(l) -> (-rstd m1, -rstd^2 m2) of lane l of the column
+template <int KIND, typename F>
+__device__ __forceinline__ void fill_means(f2 *k0, f2 *k1, F of) {
+    constexpr int NP = Lanes<KIND>::NP;
+    float2 v[2 * NP];
+#pragma unroll
+    for (int l = 0; l < 2 * NP; ++l) v[l] = l < Lanes<KIND>::L ? of(l) : make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) { k0[i] = two(v[2 * i].x, v[2 * i + 1].x); k1[i] = two(v[2 * i].y, v[2 * i + 1].y); }
+}
+
+// ---------------------------------------------------------------------------------------------------- sums of a block
 
 constexpr int NORM_T = 256;
+constexpr int NORM_PITCH = NORM_T + 4;  // floats between the rows of sums per thread, one row per lane: neighbouring lanes in different banks
 constexpr int NORM_AHEAD = 4;           // vectors of a thread in flight
-
-// Sums over the R rows of a block: v[a][l * T + thread] -> done(column lane, the A sums).  `sub` neighbouring threads share a lane of channels.
-template <int L, int A, int T, typename F>
-__device__ __forceinline__ void sum_rows(const float *v, int sv, int rows, F done) {
-    const int lanes = sv * L;
-    int sub = 1;
-    while (sub < 32 && lanes * sub * 2 <= T) sub *= 2;
-    const int sl = threadIdx.x % sub;
-    for (int q0 = 0; q0 < lanes; q0 += T / sub) {
-        const int q = q0 + threadIdx.x / sub;
-        float s[A];
-#pragma unroll
-        for (int a = 0; a < A; ++a) s[a] = 0.f;
-        if (q < lanes)
-            for (int r = sl; r < rows; r += sub)
-#pragma unroll
-                for (int a = 0; a < A; ++a) s[a] += v[(a * L + q % L) * T + r * sv + q / L];
-        for (int o = sub / 2; o > 0; o /= 2)
-#pragma unroll
-            for (int a = 0; a < A; ++a) s[a] += __shfl_xor_sync(0xffffffffu, s[a], o);
-        if (q < lanes && sl == 0) done(q, s);
-    }
-}
 
 // Number of the pixels r, r + R, ... below n
 __device__ __forceinline__ int pixels_of(int n, int r, int rows) { return r < n ? (n - r + rows - 1) / rows : 0; }
 
-// Mean and squared deviations of a chunk of pixels, channel by channel
-template <int KIND>
-__global__ void __launch_bounds__(NORM_T) norm_partial_kernel(const NormParams p) {
-    constexpr int L = Lanes<KIND>::L;
-    using Raw = typename Lanes<KIND>::Raw;
-    __shared__ float v[2 * L * NORM_T];
-    __shared__ float mean_s[L * NORM_T];
-    pdl_wait();
-    pdl_trigger();
-    const int v0 = blockIdx.y * p.sv, sv = min(p.sv, p.pv - v0);
-    const int rows = NORM_T / sv, r = threadIdx.x / sv, col = threadIdx.x - r * sv;
-    const int p0 = blockIdx.x * p.per, n = min(p.per, p.HW - p0);
-    const int cnt = r < rows ? pixels_of(n, r, rows) : 0;
-    const size_t base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
-    float mean[L], m2[L];
-#pragma unroll
-    for (int l = 0; l < L; ++l) mean[l] = m2[l] = 0.f;
-    // running mean and deviations of groups of NORM_AHEAD vectors
-    for (int i0 = 0; i0 < cnt; i0 += NORM_AHEAD) {
-        Raw raw[NORM_AHEAD];
-#pragma unroll
-        for (int i = 0; i < NORM_AHEAD; ++i)
-            if (i0 + i < cnt) raw[i] = ((const Raw *)p.x)[base + (size_t)(i0 + i) * rows * p.pv];
-        const float m = (float)min(NORM_AHEAD, cnt - i0), total = i0 + m, share = m / total;
-        float f[NORM_AHEAD][L];
-#pragma unroll
-        for (int i = 0; i < NORM_AHEAD; ++i) Lanes<KIND>::unpack(raw[i], f[i]);
-#pragma unroll
-        for (int l = 0; l < L; ++l) {
-            float s = 0.f, q = 0.f;
-#pragma unroll
-            for (int i = 0; i < NORM_AHEAD; ++i) s += i0 + i < cnt ? f[i][l] : 0.f;
-            s /= m;
-#pragma unroll
-            for (int i = 0; i < NORM_AHEAD; ++i) {
-                const float d = i0 + i < cnt ? f[i][l] - s : 0.f;
-                q += d * d;
-            }
-            const float d = s - mean[l];
-            mean[l] += d * share;
-            m2[l] += q + d * d * (float)i0 * share;
-        }
-    }
-    if (r < rows) {
-#pragma unroll
-        for (int l = 0; l < L; ++l) {
-            v[l * NORM_T + threadIdx.x] = mean[l] * (float)cnt;
-            v[(L + l) * NORM_T + threadIdx.x] = m2[l];
-        }
-    }
-    __syncthreads();
-    const float inv = 1.f / (float)n;
-    sum_rows<L, 1, NORM_T>(v, sv, rows, [&](int q, const float *s) { mean_s[q] = s[0] * inv; });
-    __syncthreads();
-    if (r < rows && cnt > 0) {
-#pragma unroll
-        for (int l = 0; l < L; ++l) {
-            const float d = mean[l] - mean_s[col * L + l];
-            v[(L + l) * NORM_T + threadIdx.x] += d * d * (float)cnt;
-        }
-    }
-    __syncthreads();
-    float2 *part = p.part + ((size_t)blockIdx.z * p.chunks + blockIdx.x) * p.pv * L + v0 * L;
-    sum_rows<L, 1, NORM_T>(v + L * NORM_T, sv, rows, [&](int q, const float *s) { part[q] = make_float2(mean_s[q], s[0]); });
+// Threads that share a lane of channels when sums over the R rows of a block are taken
+__device__ __forceinline__ int sharers(int lanes) {
+    int sub = 1;
+    while (sub < 32 && lanes * sub * 2 <= NORM_T) sub *= 2;
+    return sub;
 }
+__device__ __forceinline__ float sum_sharers(float s, int sub) {
+    for (int o = sub / 2; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+}
+
+// A sums over the rows: v[(a L + lane % L) PITCH + thread], handed to done(lane, sums)
+template <int L, int A, typename F>
+__device__ __forceinline__ void sum_rows(const float *v, int sv, int rows, F done) {
+    const int lanes = sv * L, sub = sharers(lanes), sl = threadIdx.x % sub;
+    for (int q0 = 0; q0 < lanes; q0 += NORM_T / sub) {
+        const int q = q0 + threadIdx.x / sub;
+        float s[A];
+#pragma unroll
+        for (int a = 0; a < A; ++a) s[a] = 0.f;
+        const float *w = v + q % L * NORM_PITCH + q / L;
+        if (q < lanes)
+#pragma unroll 4
+            for (int r = sl; r < rows; r += sub)
+#pragma unroll
+                for (int a = 0; a < A; ++a) s[a] += w[a * L * NORM_PITCH + r * sv];
+#pragma unroll
+        for (int a = 0; a < A; ++a) s[a] = sum_sharers(s[a], sub);
+        if (q < lanes && sl == 0) done(q, s);
+    }
+}
+
+// Means and squared deviations of the rows' values put together per lane: v holds every thread's sum and its deviations from its own mean over
+// its `n / rows`, or one more, pixels
+template <int L, typename F>
+__device__ __forceinline__ void combine_rows(const float *v, int sv, int rows, int n, F done) {
+    const int lanes = sv * L, sub = sharers(lanes), sl = threadIdx.x % sub;
+    const int few = n / rows, more = n - few * rows;           // rows below `more` have few + 1 pixels
+    const float inv = n > 0 ? 1.f / (float)n : 0.f, inv_few = few > 0 ? 1.f / (float)few : 0.f, inv_more = 1.f / (float)(few + 1);
+    const int used = few > 0 ? rows : more;
+    for (int q0 = 0; q0 < lanes; q0 += NORM_T / sub) {
+        const int q = q0 + threadIdx.x / sub;
+        const float *w = v + q % L * NORM_PITCH + q / L;
+        float s = 0.f, m2 = 0.f;
+        if (q < lanes)
+#pragma unroll 4
+            for (int r = sl; r < used; r += sub) s += w[r * sv];
+        const float mean = sum_sharers(s, sub) * inv;
+        if (q < lanes)
+#pragma unroll 4
+            for (int r = sl; r < used; r += sub) {
+                const float d = w[r * sv] * (r < more ? inv_more : inv_few) - mean;
+                m2 += w[L * NORM_PITCH + r * sv] + d * d * (float)(r < more ? few + 1 : few);
+            }
+        m2 = sum_sharers(m2, sub);
+        if (q < lanes && sl == 0) done(q, mean, m2);
+    }
+}
+
+// A thread's sum and squared deviations, value by value.  The shift is its first value: a value that lies D from the mean of n has itself D^2 of the deviations
+// and leaves D^2 / (n - 1) to the others, so that n D^2, which the shift adds to the squares, is at most n - 1 times what is wanted.
+template <int NP> struct Spread {
+    f2 minus_shift[NP], s[NP], q[NP];
+    __device__ __forceinline__ void begin(const f2 *first) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            minus_shift[i] = two(-one_by_one(first[i]).x, -one_by_one(first[i]).y);
+            s[i] = q[i] = 0ull;
+        }
+    }
+    __device__ __forceinline__ void add(const f2 *f) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const f2 d = add2(f[i], minus_shift[i]);
+            s[i] = add2(s[i], d);
+            q[i] = fma2(d, d, q[i]);
+        }
+    }
+    // sums and deviations from the means of n values, per lane
+    template <int L> __device__ __forceinline__ void store(float *v, int n) const {
+        const float inv = n > 0 ? 1.f / (float)n : 0.f;
+#pragma unroll
+        for (int l = 0; l < L; ++l) {
+            const float2 k = one_by_one(minus_shift[l / 2]), a = one_by_one(s[l / 2]), b = one_by_one(q[l / 2]);
+            const float shift = l % 2 ? k.y : k.x, sum = l % 2 ? a.y : a.x, square = l % 2 ? b.y : b.x;
+            const float dev = square - sum * (sum * inv);
+            v[l * NORM_PITCH + threadIdx.x] = n > 0 ? sum - shift * (float)n : 0.f;
+            v[(L + l) * NORM_PITCH + threadIdx.x] = n > 0 ? (dev < 0.f ? 0.f : dev) : 0.f;         // (a NaN stays one: no maximum)
+        }
+    }
+};
 
 // Sum over the threads of a team (a warp or a block), the same for all of them and in a fixed order
 template <int TEAM>
@@ -249,9 +410,63 @@ __device__ __forceinline__ float team_sum(float s, float *scratch) {
     return s;
 }
 
+// ---------------------------------------------------------------------------------------------------- three launches
+
+// The pixels and columns of a block
+struct Chunk {
+    int v0, sv, rows, r, col, n, cnt;
+    size_t base, step;
+    __device__ __forceinline__ Chunk(const NormParams &p) {
+        v0 = blockIdx.y * p.sv;
+        sv = min(p.sv, p.pv - v0);
+        rows = NORM_T / sv;
+        r = threadIdx.x / sv;
+        col = threadIdx.x - r * sv;
+        const int p0 = blockIdx.x * p.per;
+        n = min(p.per, p.HW - p0);
+        cnt = r < rows ? pixels_of(n, r, rows) : 0;
+        base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
+        step = (size_t)rows * p.pv;
+    }
+};
+
+// Mean and squared deviations of a chunk of pixels, channel by channel
+template <int KIND>
+__global__ void __launch_bounds__(NORM_T) norm_partial_kernel(const __grid_constant__ NormParams p) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
+    using Raw = typename Lanes<KIND>::Raw;
+    __shared__ float v[2 * L * NORM_PITCH];
+    pdl_wait();
+    pdl_trigger();
+    const Chunk c(p);
+    Spread<NP> own;
+    if (c.cnt > 0) {
+        f2 f[NP];
+        Lanes<KIND>::unpack(((const Raw *)p.x)[c.base], f);
+        own.begin(f);
+    }
+    for (int i0 = 0; i0 < c.cnt; i0 += NORM_AHEAD) {
+        Raw raw[NORM_AHEAD];
+#pragma unroll
+        for (int i = 0; i < NORM_AHEAD; ++i)
+            if (i0 + i < c.cnt) raw[i] = ((const Raw *)p.x)[c.base + (i0 + i) * c.step];
+#pragma unroll
+        for (int i = 0; i < NORM_AHEAD; ++i)
+            if (i0 + i < c.cnt) {
+                f2 f[NP];
+                Lanes<KIND>::unpack(raw[i], f);
+                own.add(f);
+            }
+    }
+    if (c.r < c.rows) own.template store<L>(v, c.cnt);
+    __syncthreads();
+    float2 *part = p.part + ((size_t)blockIdx.z * p.chunks + blockIdx.x) * p.pv * L + c.v0 * L;
+    combine_rows<L>(v, c.sv, c.rows, c.n, [&](int q, float mean, float m2) { part[q] = make_float2(mean, m2); });
+}
+
 // Chunks and channels of a group put together: mean and rstd
 template <int TEAM>
-__global__ void __launch_bounds__(NORM_T) norm_combine_kernel(const NormParams p, int lanes) {
+__global__ void __launch_bounds__(NORM_T) norm_combine_kernel(const __grid_constant__ NormParams p, int lanes) {
     __shared__ float scratch[NORM_T / 32];
     pdl_wait();
     pdl_trigger();
@@ -277,96 +492,97 @@ __global__ void __launch_bounds__(NORM_T) norm_combine_kernel(const NormParams p
     if (t == 0) ((float2 *)p.stats)[id] = make_float2(mean, 1.f / sqrtf(var + p.eps));
 }
 
-template <int L>
-__device__ __forceinline__ void load_stats(const NormParams &p, Column<L> &k, int n, int c0) {
-    k.load_affine(p, c0);
-#pragma unroll
-    for (int l = 0; l < L; ++l)
-        if (c0 + l < p.C) {
-            const float2 s = __ldcg((const float2 *)p.stats + (size_t)n * p.G + (c0 + l) / p.cpg);
-            k.mean[l] = s.x;
-            k.rstd[l] = s.y;
-        }
-}
-
-template <int KIND>
-__global__ void __launch_bounds__(NORM_T) norm_apply_kernel(const NormParams p) {
-    constexpr int L = Lanes<KIND>::L;
+template <int KIND, int ACT>
+__global__ void __launch_bounds__(NORM_T) norm_apply_kernel(const __grid_constant__ NormParams p) {
     using Raw = typename Lanes<KIND>::Raw;
     pdl_wait();
     pdl_trigger();
-    const int v0 = blockIdx.y * p.sv, sv = min(p.sv, p.pv - v0);
-    const int rows = NORM_T / sv, r = threadIdx.x / sv, col = threadIdx.x - r * sv;
-    const int p0 = blockIdx.x * p.per, n = min(p.per, p.HW - p0);
-    if (r >= rows) return;
-    const int cnt = pixels_of(n, r, rows), c0 = (v0 + col) * L;
-    const size_t base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
-    Column<L> k;
-    load_stats<L>(p, k, blockIdx.z, c0);
-    for (int i0 = 0; i0 < cnt; i0 += NORM_AHEAD) {
-        Raw raw[NORM_AHEAD];
+    const Chunk c(p);
+    if (c.cnt == 0) return;
+    Column<Lanes<KIND>::NP> k;
+    load_column<KIND>(p, k, blockIdx.z, (c.v0 + c.col) * Lanes<KIND>::L);
+    for (int i0 = 0; i0 < c.cnt; i0 += NORM_AHEAD) {
+        Raw raw[NORM_AHEAD], res[NORM_AHEAD];
 #pragma unroll
         for (int i = 0; i < NORM_AHEAD; ++i)
-            if (i0 + i < cnt) raw[i] = ((const Raw *)p.x)[base + (size_t)(i0 + i) * rows * p.pv];
+            if (i0 + i < c.cnt) {
+                raw[i] = ((const Raw *)p.x)[c.base + (i0 + i) * c.step];
+                if (p.res) res[i] = ((const Raw *)p.res)[c.base + (i0 + i) * c.step];
+            }
 #pragma unroll
         for (int i = 0; i < NORM_AHEAD; ++i)
-            if (i0 + i < cnt) apply_one<KIND>(p, k, c0, raw[i], base + (size_t)(i0 + i) * rows * p.pv);
+            if (i0 + i < c.cnt) apply_one<KIND, ACT>(p, k, raw[i], res[i], c.base + (i0 + i) * c.step);
     }
 }
 
+// Sums of dz and dz (x - mean) of a thread
+template <int NP> struct GradientSums {
+    f2 a[NP], b[NP];
+    __device__ __forceinline__ GradientSums() {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) a[i] = b[i] = 0ull;
+    }
+    __device__ __forceinline__ void add(const f2 *d, const f2 *dz) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            a[i] = add2(a[i], dz[i]);
+            b[i] = fma2(dz[i], d[i], b[i]);
+        }
+    }
+    template <int L> __device__ __forceinline__ void store(float *v) const {
+#pragma unroll
+        for (int l = 0; l < L; ++l) {
+            v[l * NORM_PITCH + threadIdx.x] = l % 2 ? one_by_one(a[l / 2]).y : one_by_one(a[l / 2]).x;
+            v[(L + l) * NORM_PITCH + threadIdx.x] = l % 2 ? one_by_one(b[l / 2]).y : one_by_one(b[l / 2]).x;
+        }
+    }
+};
+
 // Sums of dz and dz xhat over a chunk of pixels, channel by channel
-template <int KIND>
-__global__ void __launch_bounds__(NORM_T) norm_grad_partial_kernel(const NormParams p) {
-    constexpr int L = Lanes<KIND>::L;
+template <int KIND, int ACT>
+__global__ void __launch_bounds__(NORM_T) norm_grad_partial_kernel(const __grid_constant__ NormParams p) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
     using Raw = typename Lanes<KIND>::Raw;
-    __shared__ float v[2 * L * NORM_T];
+    __shared__ float v[2 * L * NORM_PITCH];
     pdl_wait();
     pdl_trigger();
-    const int v0 = blockIdx.y * p.sv, sv = min(p.sv, p.pv - v0);
-    const int rows = NORM_T / sv, r = threadIdx.x / sv, col = threadIdx.x - r * sv;
-    const int p0 = blockIdx.x * p.per, n = min(p.per, p.HW - p0);
-    const int cnt = r < rows ? pixels_of(n, r, rows) : 0, c0 = (v0 + col) * L;
-    const size_t base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
-    float a[L], b[L];
-#pragma unroll
-    for (int l = 0; l < L; ++l) a[l] = b[l] = 0.f;
-    if (cnt > 0) {
-        Column<L> k;
-        load_stats<L>(p, k, blockIdx.z, c0);
-        for (int i0 = 0; i0 < cnt; i0 += 2) {
+    const Chunk c(p);
+    const int c0 = (c.v0 + c.col) * L;
+    const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
+    GradientSums<NP> sums;
+    if (c.cnt > 0) {
+        Column<NP> k;
+        load_column<KIND>(p, k, blockIdx.z, c0);
+        for (int i0 = 0; i0 < c.cnt; i0 += 2) {
             Raw x[2], dy[2], res[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (i0 + i < cnt) {
-                    const size_t at = base + (size_t)(i0 + i) * rows * p.pv;
+                if (i0 + i < c.cnt) {
+                    const size_t at = c.base + (i0 + i) * c.step;
                     x[i] = ((const Raw *)p.x)[at];
                     dy[i] = ((const Raw *)p.dy)[at];
                     if (p.res) res[i] = ((const Raw *)p.res)[at];
                 }
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (i0 + i < cnt) {
-                    float dz[L], xhat[L];
-                    gradient_one<KIND>(p, k, x[i], dy[i], res[i], dz, xhat);
-#pragma unroll
-                    for (int l = 0; l < L; ++l) { a[l] += dz[l]; b[l] += dz[l] * xhat[l]; }
+                if (i0 + i < c.cnt) {
+                    f2 d[NP], dz[NP];
+                    gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], d, dz);
+                    sums.add(d, dz);
                 }
         }
     }
-    if (r < rows) {
-#pragma unroll
-        for (int l = 0; l < L; ++l) {
-            v[l * NORM_T + threadIdx.x] = a[l];
-            v[(L + l) * NORM_T + threadIdx.x] = b[l];
-        }
-    }
+    if (c.r < c.rows) sums.template store<L>(v);
     __syncthreads();
-    float2 *part = p.part + ((size_t)blockIdx.z * p.chunks + blockIdx.x) * p.pv * L + v0 * L;
-    sum_rows<L, 2, NORM_T>(v, sv, rows, [&](int q, const float *s) { part[q] = make_float2(s[0], s[1]); });
+    float2 *part = p.part + ((size_t)blockIdx.z * p.chunks + blockIdx.x) * p.pv * L + c.v0 * L;
+    sum_rows<L, 2>(v, c.sv, c.rows, [&](int q, const float *s) {
+        const int ch = c.v0 * L + q;
+        part[q] = make_float2(s[0], ch < p.C ? s[1] * __ldcg(stats + ch / p.cpg).y : 0.f);
+    });
 }
 
 template <int TEAM>
-__global__ void __launch_bounds__(NORM_T) norm_grad_combine_kernel(const NormParams p, int lanes) {
+__global__ void __launch_bounds__(NORM_T) norm_grad_combine_kernel(const __grid_constant__ NormParams p, int lanes) {
     __shared__ float scratch[NORM_T / 32];
     pdl_wait();
     pdl_trigger();
@@ -390,18 +606,20 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_combine_kernel(const NormPar
 }
 
 // dgamma and dbeta of 32 channels: the partial sums of all images and chunks, eight at a time, in a fixed order; their total in 64 bits
-__device__ __forceinline__ void parameter_gradients(const NormParams &p, int block, int lanes) {
+__global__ void __launch_bounds__(NORM_T) norm_parameter_gradients_kernel(const __grid_constant__ NormParams p, int lanes) {
     __shared__ double tot[2][8][33];
-    const int cl = threadIdx.x & 31, k = threadIdx.x >> 5, c = block * 32 + cl;
+    pdl_wait();
+    pdl_trigger();
+    const int cl = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + cl;
     double a = 0.0, b = 0.0;
     const long long entries = (long long)p.N * p.chunks;
     if (c < p.C)
-        for (long long e0 = k; e0 < entries; e0 += 32) {
-            float2 v[4];
+        for (long long e0 = k; e0 < entries; e0 += 64) {
+            float2 v[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = e0 + 8 * i < entries ? __ldcg(p.part + (size_t)(e0 + 8 * i) * lanes + c) : make_float2(0.f, 0.f);
+            for (int i = 0; i < 8; ++i) v[i] = e0 + 8 * i < entries ? __ldcg(p.part + (size_t)(e0 + 8 * i) * lanes + c) : make_float2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { a += v[i].x; b += v[i].y; }
+            for (int i = 0; i < 8; ++i) { a += v[i].x; b += v[i].y; }
         }
     tot[0][k][cl] = a;
     tot[1][k][cl] = b;
@@ -414,70 +632,398 @@ __device__ __forceinline__ void parameter_gradients(const NormParams &p, int blo
     }
 }
 
-__global__ void __launch_bounds__(NORM_T) norm_parameter_gradients_kernel(const NormParams p, int lanes) {
-    pdl_wait();
-    pdl_trigger();
-    parameter_gradients(p, blockIdx.x, lanes);
-}
-
-template <int KIND>
-__device__ __forceinline__ void store_gradient(const NormParams &p, const Column<Lanes<KIND>::L> &k, const float *m1, const float *m2, int c0, const float *dz,
-                                               const float *xhat, size_t at) {
-    constexpr int L = Lanes<KIND>::L;
-    using Raw = typename Lanes<KIND>::Raw;
-    float f[L], g[L];
-#pragma unroll
-    for (int l = 0; l < L; ++l) {
-        const bool in = c0 + l < p.C;
-        f[l] = in ? k.rstd[l] * (k.gamma[l] * dz[l] - m1[l] - xhat[l] * m2[l]) : 0.f;
-        g[l] = in ? dz[l] : 0.f;
-    }
-    ((Raw *)p.out)[at] = Lanes<KIND>::pack(f);
-    if (p.dres) ((Raw *)p.dres)[at] = Lanes<KIND>::pack(g);
-}
-
-template <int KIND>
-__global__ void __launch_bounds__(NORM_T) norm_grad_apply_kernel(const NormParams p, int lanes) {
-    constexpr int L = Lanes<KIND>::L;
+template <int KIND, int ACT>
+__global__ void __launch_bounds__(NORM_T) norm_grad_apply_kernel(const __grid_constant__ NormParams p, int lanes) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
     using Raw = typename Lanes<KIND>::Raw;
     pdl_wait();
     pdl_trigger();
-    const int v0 = blockIdx.y * p.sv, sv = min(p.sv, p.pv - v0);
-    const int rows = NORM_T / sv, r = threadIdx.x / sv, col = threadIdx.x - r * sv;
-    const int p0 = blockIdx.x * p.per, n = min(p.per, p.HW - p0);
-    if (r >= rows) return;
-    const int cnt = pixels_of(n, r, rows), c0 = (v0 + col) * L;
-    const size_t base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
-    Column<L> k;
-    load_stats<L>(p, k, blockIdx.z, c0);
-    float m1[L], m2[L];
-#pragma unroll
-    for (int l = 0; l < L; ++l) {
-        const float2 m = c0 + l < p.C ? __ldcg(p.means + (size_t)blockIdx.z * p.G + (c0 + l) / p.cpg) : make_float2(0.f, 0.f);
-        m1[l] = m.x;
-        m2[l] = m.y;
-    }
-    for (int i0 = 0; i0 < cnt; i0 += 2) {
+    const Chunk c(p);
+    if (c.cnt == 0) return;
+    const int c0 = (c.v0 + c.col) * L;
+    const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G, *means = p.means + (size_t)blockIdx.z * p.G;
+    Column<NP> k;
+    f2 k0[NP], k1[NP];
+    load_column<KIND>(p, k, blockIdx.z, c0);
+    fill_means<KIND>(k0, k1, [&](int l) {
+        if (c0 + l >= p.C) return make_float2(0.f, 0.f);
+        const float2 m = __ldcg(means + (c0 + l) / p.cpg);
+        const float rstd = __ldcg(stats + (c0 + l) / p.cpg).y;
+        return make_float2(-rstd * m.x, -rstd * rstd * m.y);
+    });
+    for (int i0 = 0; i0 < c.cnt; i0 += 2) {
         Raw x[2], dy[2], res[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (i0 + i < cnt) {
-                const size_t at = base + (size_t)(i0 + i) * rows * p.pv;
+            if (i0 + i < c.cnt) {
+                const size_t at = c.base + (i0 + i) * c.step;
                 x[i] = ((const Raw *)p.x)[at];
                 dy[i] = ((const Raw *)p.dy)[at];
                 if (p.res) res[i] = ((const Raw *)p.res)[at];
             }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (i0 + i < cnt) {
-                float dz[L], xhat[L];
-                gradient_one<KIND>(p, k, x[i], dy[i], res[i], dz, xhat);
-                store_gradient<KIND>(p, k, m1, m2, c0, dz, xhat, base + (size_t)(i0 + i) * rows * p.pv);
+            if (i0 + i < c.cnt) {
+                f2 d[NP], dz[NP];
+                gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], d, dz);
+                store_gradient<KIND>(p, k, k0, k1, d, dz, c.base + (i0 + i) * c.step);
             }
     }
 }
 
+// ------------------------------------------------------------------------------------------------------- on chip
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// two floats in the shared memory of a block of the cluster
+__device__ __forceinline__ float2 remote_float2(const float2 *own, int rank) {
+    uint32_t a;
+    float2 v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(own)), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+    return v;
+}
+template <typename Raw>
+__device__ __forceinline__ void copy_in(Raw *dst, const Raw *src) {
+    if constexpr (sizeof(Raw) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+// What a block works on: pixels p0 .. p0 + n of an image, columns v0 .. v0 + sv, groups g0 .. g0 + sg
+struct Share {
+    int v0, sv, g0, sg, p0, n, rows, r, col, cnt;
+    size_t base, step;
+    __device__ __forceinline__ Share(const NormParams &p, int L, int rank) {
+        g0 = blockIdx.y * p.gs;
+        sg = min(p.gs, p.G - g0);
+        v0 = g0 * p.cpg / L;
+        sv = (g0 + sg == p.G ? p.pv : (g0 + sg) * p.cpg / L) - v0;
+        p0 = rank * p.per;
+        n = max(0, min(p.per, p.HW - p0));
+        rows = NORM_T / sv;
+        r = threadIdx.x / sv;
+        col = threadIdx.x - r * sv;
+        cnt = r < rows ? pixels_of(n, r, rows) : 0;
+        base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
+        step = (size_t)rows * p.pv;
+    }
+};
+
+// f(group, rank's values of lane `rank`) for the groups of the slice: 16 threads a group, thread i with rank i's pair (zeros from `ranks` on)
+template <typename F>
+__device__ __forceinline__ void over_ranks(const float2 *group, int sg, int ranks, F f) {
+    const int q = threadIdx.x & 15;
+    for (int g0 = 0; g0 < sg; g0 += NORM_T / 16) {           // (whole warps go round)
+        const int g = g0 + threadIdx.x / 16;
+        f(g, g < sg && q < ranks ? remote_float2(group + g, q) : make_float2(0.f, 0.f));
+    }
+}
+__device__ __forceinline__ float sum16(float s) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+}
+
+// Dynamic shared memory: the data ([pixel of a thread][thread] per tensor), sums per thread (afterwards: what a column needs of its channels), results per
+// group and of the image's groups, results per channel, scale and shift.  What a channel needs is worked out once for all threads.
+__host__ __device__ __forceinline__ size_t norm_sums_bytes(int L, int sv) { return 16 * (size_t)L * (sv > NORM_PITCH / 2 ? sv : NORM_PITCH / 2); }
+struct NormSmem {
+    unsigned char *data;
+    float *v;
+    float4 *constants;                  // over v: -mean, rstd gamma, beta
+    float2 *group, *image, *channel, *affine;
+    template <int L> __device__ __forceinline__ NormSmem(unsigned char *base, const NormParams &p, int tensors, std::integral_constant<int, L>) {
+        data = base;
+        v = (float *)(base + (size_t)p.data_bytes * tensors);
+        constants = (float4 *)v;
+        group = (float2 *)((char *)v + norm_sums_bytes(L, p.sv));
+        image = group + p.gs;
+        channel = image + p.gs;
+        affine = channel + p.sv * L;
+    }
+};
+
+// scale and shift of the slice's channels: read early, needed late
+template <int L>
+__device__ __forceinline__ void fetch_affine(const NormParams &p, const Share &s, float2 *to) {
+    for (int q = threadIdx.x; q < s.sv * L; q += NORM_T) {
+        const int c = s.v0 * L + q;
+        const bool in = c < p.C;
+        to[q] = make_float2(in ? (p.gamma ? __ldg(p.gamma + c) : 1.f) : 0.f, in && p.beta ? __ldg(p.beta + c) : 0.f);
+    }
+}
+
+template <int KIND, int ACT>
+__global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_constant__ NormParams p) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
+    using Raw = typename Lanes<KIND>::Raw;
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    const int ranks = gridDim.x, rank = (int)cluster_rank(), t = threadIdx.x;
+    const Share s(p, L, rank);
+    const NormSmem m(norm_smem, p, 1, std::integral_constant<int, L>());
+    Raw *data = (Raw *)m.data;
+    pdl_wait();
+    pdl_trigger();
+#pragma unroll 4
+    for (int i = 0; i < s.cnt; ++i) copy_in(data + i * NORM_T + t, (const Raw *)p.x + s.base + i * s.step);
+    fetch_affine<L>(p, s, m.affine);
+    copy_wait();
+    Spread<NP> own;
+    if (s.cnt > 0) {
+        f2 f[NP];
+        Lanes<KIND>::unpack(data[t], f);
+        own.begin(f);
+    }
+#pragma unroll 4
+    for (int i = 1; i < s.cnt; ++i) {
+        f2 f[NP];
+        Lanes<KIND>::unpack(data[i * NORM_T + t], f);
+        own.add(f);
+    }
+    if (s.r < s.rows) own.template store<L>(m.v, s.cnt);
+    __syncthreads();
+    combine_rows<L>(m.v, s.sv, s.rows, s.n, [&](int q, float mean, float m2) { m.channel[q] = make_float2(mean, m2); });
+    __syncthreads();
+    // channels to groups: a warp per group
+    const int lane = t & 31;
+    const float inv_cpg = 1.f / (float)p.cpg, inv_hw = 1.f / (float)p.HW;
+    for (int g = t >> 5; g < s.sg; g += NORM_T / 32) {
+        const float2 *c = m.channel + (s.g0 + g) * p.cpg - s.v0 * L;
+        float a = 0.f, b = 0.f;
+        for (int j = lane; j < p.cpg; j += 32) a += c[j].x;
+        a = team_sum<32>(a, nullptr) * inv_cpg;
+        for (int j = lane; j < p.cpg; j += 32) {
+            const float d = c[j].x - a;
+            b += c[j].y + d * d * (float)s.n;
+        }
+        b = team_sum<32>(b, nullptr);
+        if (lane == 0) m.group[g] = make_float2(a, b);
+    }
+    cluster_arrive();
+    cluster_wait();
+    // the ranks' groups to the image's
+    const float pixels = (float)max(0, min(p.per, p.HW - (t & 15) * p.per));
+    over_ranks(m.group, s.sg, ranks, [&](int g, float2 w) {
+        const float mean = sum16(w.x * pixels) * inv_hw, d = w.x - mean;
+        const float m2 = sum16(w.y + d * d * pixels * (float)p.cpg);
+        if (g < s.sg && (t & 15) == 0) {
+            const float2 result = make_float2(mean, 1.f / sqrtf(m2 * inv_hw * inv_cpg + p.eps));
+            m.image[g] = result;
+            if (rank == 0) ((float2 *)p.stats)[(size_t)blockIdx.z * p.G + s.g0 + g] = result;
+        }
+    });
+    cluster_arrive();                                          // (its wait, at the end: no block leaves while others read its groups)
+    __syncthreads();
+    for (int q = t; q < s.sv * L; q += NORM_T) {
+        const float2 w = s.v0 * L + q < p.C ? m.image[(s.v0 * L + q) / p.cpg - s.g0] : make_float2(0.f, 0.f), k = m.affine[q];
+        m.constants[q] = make_float4(-w.x, w.y * k.x, k.y, 0.f);
+    }
+    __syncthreads();
+    if (s.cnt > 0) {
+        Column<NP> k;
+        fill_column<KIND>(k, [&](int l) {
+            const float4 c = m.constants[s.col * L + l];
+            return make_float3(c.x, c.y, c.z);
+        });
+        for (int i0 = 0; i0 < s.cnt; i0 += NORM_AHEAD) {
+            Raw raw[NORM_AHEAD], res[NORM_AHEAD];
+#pragma unroll
+            for (int i = 0; i < NORM_AHEAD; ++i)
+                if (i0 + i < s.cnt) {
+                    raw[i] = data[(i0 + i) * NORM_T + t];
+                    if (p.res) res[i] = ((const Raw *)p.res)[s.base + (i0 + i) * s.step];
+                }
+#pragma unroll
+            for (int i = 0; i < NORM_AHEAD; ++i)
+                if (i0 + i < s.cnt) apply_one<KIND, ACT>(p, k, raw[i], res[i], s.base + (i0 + i) * s.step);
+        }
+    }
+    cluster_wait();
+}
+
+// part: the sums of every rank's channels, [N][ranks][lanes], for the parameters' gradients
+template <int KIND, int ACT>
+__global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_constant__ NormParams p, int lanes) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
+    using Raw = typename Lanes<KIND>::Raw;
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    const int ranks = gridDim.x, rank = (int)cluster_rank(), t = threadIdx.x;
+    const Share s(p, L, rank);
+    const NormSmem m(norm_smem, p, p.res ? 3 : 2, std::integral_constant<int, L>());
+    Raw *x = (Raw *)m.data, *dy = (Raw *)(m.data + p.data_bytes), *res = p.res ? (Raw *)(m.data + 2 * (size_t)p.data_bytes) : x;
+    const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
+    pdl_wait();
+    pdl_trigger();
+#pragma unroll 4
+    for (int i = 0; i < s.cnt; ++i) {
+        copy_in(x + i * NORM_T + t, (const Raw *)p.x + s.base + i * s.step);
+        copy_in(dy + i * NORM_T + t, (const Raw *)p.dy + s.base + i * s.step);
+        if (p.res) copy_in(res + i * NORM_T + t, (const Raw *)p.res + s.base + i * s.step);
+    }
+    fetch_affine<L>(p, s, m.affine);
+    for (int q = t; q < s.sv * L; q += NORM_T) {
+        const float2 w = s.v0 * L + q < p.C ? __ldcg(stats + (s.v0 * L + q) / p.cpg) : make_float2(0.f, 0.f), k = m.affine[q];
+        m.constants[q] = make_float4(-w.x, w.y * k.x, k.y, w.y);
+        m.channel[q].x = w.y;
+    }
+    __syncthreads();
+    Column<NP> k;
+    fill_column<KIND>(k, [&](int l) {
+        const float4 c = m.constants[s.col * L + l];
+        return make_float3(c.x, c.y, c.z);
+    });
+    copy_wait();
+    GradientSums<NP> sums;
+#pragma unroll 2
+    for (int i = 0; i < s.cnt; ++i) {
+        f2 d[NP], dz[NP];
+        gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], d, dz);
+        sums.add(d, dz);
+    }
+    __syncthreads();                                           // (the constants make room for the sums)
+    if (s.r < s.rows) sums.template store<L>(m.v);
+    __syncthreads();
+    sum_rows<L, 2>(m.v, s.sv, s.rows, [&](int q, const float *w) {
+        const float2 c = make_float2(w[0], w[1] * m.channel[q].x);
+        p.part[((size_t)blockIdx.z * ranks + rank) * lanes + s.v0 * L + q] = c;
+        // rstd stays where it is; the sums, weighted, take the shift's and the scale's place
+        m.affine[q] = make_float2(m.affine[q].x * c.x, m.affine[q].x * c.y);
+    });
+    __syncthreads();
+    const int lane = t & 31;
+    for (int g = t >> 5; g < s.sg; g += NORM_T / 32) {
+        const float2 *c = m.affine + (s.g0 + g) * p.cpg - s.v0 * L;
+        float s1 = 0.f, s2 = 0.f;
+        for (int j = lane; j < p.cpg; j += 32) {
+            s1 += c[j].x;
+            s2 += c[j].y;
+        }
+        s1 = team_sum<32>(s1, nullptr);
+        s2 = team_sum<32>(s2, nullptr);
+        if (lane == 0) m.group[g] = make_float2(s1, s2);
+    }
+    cluster_arrive();
+    cluster_wait();
+    const float inv = 1.f / ((float)p.HW * (float)p.cpg);
+    over_ranks(m.group, s.sg, ranks, [&](int g, float2 w) {
+        const float m1 = sum16(w.x) * inv, m2 = sum16(w.y) * inv;
+        if (g < s.sg && (t & 15) == 0) m.image[g] = make_float2(m1, m2);
+    });
+    cluster_arrive();
+    __syncthreads();
+    for (int q = t; q < s.sv * L; q += NORM_T) {
+        const float2 w = s.v0 * L + q < p.C ? m.image[(s.v0 * L + q) / p.cpg - s.g0] : make_float2(0.f, 0.f);
+        const float rstd = m.channel[q].x;
+        m.affine[q] = make_float2(-rstd * w.x, -rstd * rstd * w.y);
+    }
+    __syncthreads();
+    if (s.cnt > 0) {
+        f2 k0[NP], k1[NP];
+        fill_means<KIND>(k0, k1, [&](int l) { return m.affine[s.col * L + l]; });
+#pragma unroll 2
+        for (int i = 0; i < s.cnt; ++i) {
+            f2 d[NP], dz[NP];
+            gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], d, dz);
+            store_gradient<KIND>(p, k, k0, k1, d, dz, s.base + i * s.step);
+        }
+    }
+    cluster_wait();
+}
+
 // ------------------------------------------------------------------------------------------------------------- host
+
+// How the on-chip kernels share out an image; ranks == 0: they do not take it
+struct NormCluster {
+    int ranks = 0, gs = 0, slices = 0, per = 0, widest = 0;
+    size_t data_bytes = 0, smem = 0;
+};
+
+constexpr size_t NORM_SMEM = 227 * 1024;
+
+static NormCluster norm_cluster(int kind, int N, int HW, int C, int G, int tensors) {
+    NormCluster best;
+    const int L = kind == 0 ? 8 : kind == 1 ? 4 : 1, lanes = kind == 0 ? cprune_padded_channels(C) : C, pv = lanes / L, cpg = C / G;
+    int granule = 1;                       // groups that begin at a vector's boundary
+    while ((long long)granule * cpg % L) ++granule;
+    auto plan = [&](int gs, int ranks) {
+        NormCluster c;
+        int widest = 0;
+        for (int g0 = 0; g0 < G; g0 += gs) {
+            const int v1 = g0 + gs >= G ? pv : (g0 + gs) * cpg / L, sv = v1 - g0 * cpg / L;
+            widest = sv > widest ? sv : widest;
+        }
+        if (widest > NORM_T) return c;
+        c.widest = widest;
+        c.gs = gs;
+        c.slices = (G + gs - 1) / gs;
+        c.per = (HW + ranks - 1) / ranks;
+        const int rows = NORM_T / widest;
+        c.data_bytes = (size_t)((c.per + rows - 1) / rows) * NORM_T * (kind == 2 ? 4 : 16);
+        c.smem = c.data_bytes * tensors + norm_sums_bytes(L, widest) + (size_t)gs * 16 + (size_t)widest * L * 16;
+        c.ranks = c.smem <= NORM_SMEM ? ranks : 0;
+        return c;
+    };
+    // the widest slices of whole granules that a block's threads span
+    int gs = (G + granule - 1) / granule * granule;
+    while (gs > granule && !plan(gs, 16).ranks) gs = (gs / granule + 1) / 2 * granule;
+    const size_t caps[3] = {72 * 1024, 110 * 1024, NORM_SMEM};
+    for (int k = 0; k < 3 && !best.ranks; ++k)
+        for (int ranks = 1; ranks <= 16; ranks *= 2) {
+            const NormCluster c = plan(gs, ranks);
+            if (c.ranks && c.smem <= caps[k]) { best = c; break; }
+        }
+    if (!best.ranks) return best;
+    // few images: more blocks, as long as each keeps two pixels a thread
+    while ((long long)N * best.slices * best.ranks < 148 && best.ranks < 16 && best.data_bytes > 2u * NORM_T * (kind == 2 ? 4 : 16)) {
+        const NormCluster c = plan(best.gs, best.ranks * 2);
+        if (!c.ranks) break;
+        best = c;
+    }
+    if (best.slices > 65535) best.ranks = 0;
+    return best;
+}
+
+template <typename K>
+static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaStream_t st, const NormParams &p, int lanes) {
+    int dev = 0;
+    CPRUNE_CUDA_CHECK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) return CPRUNE_ERR_UNSUPPORTED;
+    static std::mutex mu;
+    static std::set<std::pair<int, const void *>> ready;        // the limits of a kernel are attributes of a device
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!ready.count({dev, (const void *)kernel})) {
+            CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_SMEM));
+            CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            ready.insert({dev, (const void *)kernel});
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(c.ranks, c.slices, N);
+    cfg.blockDim = dim3(NORM_T);
+    cfg.dynamicSmemBytes = c.smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = c.ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+    if (chain_launch_enabled()) {
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.numAttrs = 2;
+    }
+    if constexpr (std::is_invocable_v<K, NormParams, int>) CPRUNE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, p, lanes));
+    else CPRUNE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, p));
+    return CPRUNE_OK;
+}
 
 struct NormTiling {
     int lanes;          // per pixel
@@ -505,9 +1051,10 @@ static NormTiling norm_tiling(int kind, int HW, int C) {
     return t;
 }
 
+// (the on-chip kernels have one chunk to a rank)
 static size_t norm_part_bytes(int N, int HW, int C, int kind) {
     const NormTiling t = norm_tiling(kind, HW, C);
-    return ((size_t)N * t.chunks * t.lanes * sizeof(float2) + 255) / 256 * 256;
+    return ((size_t)N * (t.chunks > 16 ? t.chunks : 16) * t.lanes * sizeof(float2) + 255) / 256 * 256;
 }
 
 static cprune_status norm_check(int type, int N, int H, int W, int C, int groups, int act) {
@@ -518,14 +1065,18 @@ static cprune_status norm_check(int type, int N, int H, int W, int C, int groups
     return CPRUNE_OK;
 }
 
-// Which of the kernels for one, eight or four channels a vector
+// f(kind, activation) with both as constants
 template <typename F>
-static cprune_status by_kind(int kind, F f) {
-    switch (kind) {
-        case 0: return f(std::integral_constant<int, 0>());
-        case 1: return f(std::integral_constant<int, 1>());
-        default: return f(std::integral_constant<int, 2>());
-    }
+static cprune_status by_kind(int kind, int act, F f) {
+    auto with = [&](auto k) -> cprune_status {
+        switch (act) {
+            case CPRUNE_ACT_RELU: return f(k, std::integral_constant<int, CPRUNE_ACT_RELU>());
+            case CPRUNE_ACT_RELU6: return f(k, std::integral_constant<int, CPRUNE_ACT_RELU6>());
+            case CPRUNE_ACT_SILU: return f(k, std::integral_constant<int, CPRUNE_ACT_SILU>());
+            default: return f(k, std::integral_constant<int, CPRUNE_ACT_NONE>());
+        }
+    };
+    return kind == 0 ? with(std::integral_constant<int, 0>()) : kind == 1 ? with(std::integral_constant<int, 1>()) : with(std::integral_constant<int, 2>());
 }
 
 static NormParams norm_params(int kind, int N, int H, int W, int C, int groups, int act) {
@@ -570,8 +1121,13 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
     p.part = (float2 *)workspace;
     const NormTiling t = norm_tiling(kind, p.HW, C);
     cudaStream_t st = (cudaStream_t)stream;
-    return by_kind(kind, [&](auto k) -> cprune_status {
-        constexpr int K = decltype(k)::value;
+    const NormCluster c = norm_cluster(kind, N, p.HW, C, groups, 1);
+    return by_kind(kind, act, [&](auto k, auto a) -> cprune_status {
+        constexpr int K = decltype(k)::value, A = decltype(a)::value;
+        if (c.ranks) {
+            p.gs = c.gs; p.sv = c.widest; p.per = c.per; p.data_bytes = (int)c.data_bytes;
+            return launch_cluster(norm_cluster_kernel<K, A>, c, N, st, p, t.lanes);
+        }
         const dim3 grid(t.chunks, t.slices, N);
         ChainScope chain;
         CPRUNE_CUDA_CHECK(launch_chained(norm_partial_kernel<K>, grid, dim3(NORM_T), 0, st, p));
@@ -579,7 +1135,7 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
         const long long ids = (long long)N * groups;
         if ((long long)t.chunks * p.cpg > NORM_TEAM_ENTRIES) CPRUNE_CUDA_CHECK(launch_chained(norm_combine_kernel<NORM_T>, dim3((unsigned)ids), dim3(NORM_T), 0, st, p, t.lanes));
         else CPRUNE_CUDA_CHECK(launch_chained(norm_combine_kernel<32>, dim3((unsigned)ceil_div(ids, NORM_T / 32)), dim3(NORM_T), 0, st, p, t.lanes));
-        CPRUNE_CUDA_CHECK(launch_chained(norm_apply_kernel<K>, grid, dim3(NORM_T), 0, st, p));
+        CPRUNE_CUDA_CHECK(launch_chained(norm_apply_kernel<K, A>, grid, dim3(NORM_T), 0, st, p));
         return CPRUNE_OK;
     });
 }
@@ -603,18 +1159,27 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
     p.means = (float2 *)((char *)workspace + part_bytes);
     const NormTiling t = norm_tiling(kind, p.HW, C);
     cudaStream_t st = (cudaStream_t)stream;
-    return by_kind(kind, [&](auto k) -> cprune_status {
-        constexpr int K = decltype(k)::value;
-        const dim3 grid(t.chunks, t.slices, N);
+    const NormCluster c = norm_cluster(kind, N, p.HW, C, groups, residual ? 3 : 2);
+    return by_kind(kind, act, [&](auto k, auto a) -> cprune_status {
+        constexpr int K = decltype(k)::value, A = decltype(a)::value;
         ChainScope chain;
-        CPRUNE_CUDA_CHECK(launch_chained(norm_grad_partial_kernel<K>, grid, dim3(NORM_T), 0, st, p));
+        if (c.ranks) {
+            p.gs = c.gs; p.sv = c.widest; p.per = c.per; p.data_bytes = (int)c.data_bytes; p.chunks = c.ranks;
+            const cprune_status e = launch_cluster(norm_grad_cluster_kernel<K, A>, c, N, st, p, t.lanes);
+            if (e != CPRUNE_OK || !(dgamma || dbeta)) return e;
+            chain.follow();
+            CPRUNE_CUDA_CHECK(launch_chained(norm_parameter_gradients_kernel, dim3((C + 31) / 32), dim3(NORM_T), 0, st, p, t.lanes));
+            return CPRUNE_OK;
+        }
+        const dim3 grid(t.chunks, t.slices, N);
+        CPRUNE_CUDA_CHECK(launch_chained(norm_grad_partial_kernel<K, A>, grid, dim3(NORM_T), 0, st, p));
         chain.follow();
         const long long ids = (long long)N * groups;
         if ((long long)t.chunks * p.cpg > NORM_TEAM_ENTRIES)
             CPRUNE_CUDA_CHECK(launch_chained(norm_grad_combine_kernel<NORM_T>, dim3((unsigned)ids), dim3(NORM_T), 0, st, p, t.lanes));
         else CPRUNE_CUDA_CHECK(launch_chained(norm_grad_combine_kernel<32>, dim3((unsigned)ceil_div(ids, NORM_T / 32)), dim3(NORM_T), 0, st, p, t.lanes));
         if (dgamma || dbeta) CPRUNE_CUDA_CHECK(launch_chained(norm_parameter_gradients_kernel, dim3((C + 31) / 32), dim3(NORM_T), 0, st, p, t.lanes));
-        CPRUNE_CUDA_CHECK(launch_chained(norm_grad_apply_kernel<K>, grid, dim3(NORM_T), 0, st, p, t.lanes));
+        CPRUNE_CUDA_CHECK(launch_chained(norm_grad_apply_kernel<K, A>, grid, dim3(NORM_T), 0, st, p, t.lanes));
         return CPRUNE_OK;
     });
 }

@@ -246,8 +246,10 @@ def test_more_than_32_bits_of_bytes(cp):
     one = activation(cp, 18, 2, hw, hw, C, "bf16").cuda()
     x[-2:] = one
     y, stats = cp.cprune_group_norm(x, C, 8, activation="relu", y=x)
-    want, wstats = cp.cprune_group_norm(one, C, 8, activation="relu")
-    assert torch.equal(y[-2:], want) and torch.equal(stats[-2:], wstats)
+    # (how an image is shared out, and with it the order of its sums, may depend on the batch: the bounds are those against the definition)
+    want, mean, rstd, _, _, size = reference(one.cpu(), C, 8, torch.ones(C), torch.zeros(C), "relu", None)
+    close("rstd", stats[-2:, :, 1].cpu(), rstd, UNITS * rstd)
+    close("y", y[-2:].cpu(), want, STEP["bf16"] * want.abs() + UNITS * size)
     assert not y[:2].any()
 
 

@@ -205,32 +205,35 @@ __device__ __forceinline__ void apply_one(const NormParams &p, const Column<Lane
 // The side of relu's and relu6's borders on which z lies decides about a whole gradient, so next to a border z is taken in 64 bits: a bit
 // for each lane of the vector that is inside the borders, from what its z is made of.
 template <int KIND>
-__device__ __noinline__ uint32_t inside_64(const NormParams &p, typename Lanes<KIND>::Raw x, typename Lanes<KIND>::Raw res, int n, int c0) {
-    constexpr int L = Lanes<KIND>::L;
-    float f[L], r[L];
-    unpack_floats<KIND>(x, f);
-    if (p.res) unpack_floats<KIND>(res, r);
+__device__ __forceinline__ float lane_of(const typename Lanes<KIND>::Raw *v, int l) {
+    if constexpr (KIND == 0) return __bfloat162float(((const __nv_bfloat16 *)v)[l]);
+    else return ((const float *)v)[l];
+}
+template <int KIND, int ACT>
+__device__ __forceinline__ uint32_t inside_64(const NormParams &p, const typename Lanes<KIND>::Raw *x, const typename Lanes<KIND>::Raw *res, int n, int c0) {
     uint32_t inside = 0;
-#pragma unroll
-    for (int l = 0; l < L; ++l) {
-        if (c0 + l >= p.C) continue;
+#pragma unroll 1
+    for (int l = 0; l < Lanes<KIND>::L && c0 + l < p.C; ++l) {
         const float2 s = __ldcg((const float2 *)p.stats + (size_t)n * p.G + (c0 + l) / p.cpg);
-        const double gamma = p.gamma ? __ldg(p.gamma + c0 + l) : 1.f, beta = p.beta ? __ldg(p.beta + c0 + l) : 0.f;
-        const double z = ((double)f[l] - (double)s.x) * (double)s.y * gamma + beta + (p.res ? (double)r[l] : 0.0);
-        if (z > 0.0 && (p.act != CPRUNE_ACT_RELU6 || z < 6.0)) inside |= 1u << l;
+        double z = ((double)lane_of<KIND>(x, l) - (double)s.x) * (double)s.y;
+        if (p.gamma) z *= __ldg(p.gamma + c0 + l);
+        if (p.beta) z += __ldg(p.beta + c0 + l);
+        if (p.res) z += lane_of<KIND>(res, l);
+        if (z > 0.0 && (ACT != CPRUNE_ACT_RELU6 || z < 6.0)) inside |= 1u << l;
     }
     return inside;
 }
 
-// x - mean and dz of a vector of image n
+// x - mean and dz of a vector of image n (x_at, res_at: where it lies)
 template <int KIND, int ACT>
 __device__ __forceinline__ void gradient_one(const NormParams &p, const Column<Lanes<KIND>::NP> &k, int n, int c0, const typename Lanes<KIND>::Raw &x,
-                                             const typename Lanes<KIND>::Raw &dy, const typename Lanes<KIND>::Raw &res, f2 *d, f2 *dz) {
+                                             const typename Lanes<KIND>::Raw &dy, const typename Lanes<KIND>::Raw &res, const typename Lanes<KIND>::Raw *x_at,
+                                             const typename Lanes<KIND>::Raw *res_at, f2 *d, f2 *dz) {
     constexpr int NP = Lanes<KIND>::NP, L = Lanes<KIND>::L;
     f2 z[NP];
     affine<KIND>(p, k, x, res, d, z);
     Lanes<KIND>::unpack(dy, dz);
-    if (ACT == CPRUNE_ACT_NONE) return;
+    if constexpr (ACT != CPRUNE_ACT_NONE) {
     float f[2 * NP], g[2 * NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
@@ -256,7 +259,7 @@ __device__ __forceinline__ void gradient_one(const NormParams &p, const Column<L
             close |= fabsf(f[l]) < e || (ACT == CPRUNE_ACT_RELU6 && fabsf(f[l] - top) < e + 2.4e-6f);
         }
         if (close) {
-            const uint32_t inside = inside_64<KIND>(p, x, res, n, c0);
+            const uint32_t inside = inside_64<KIND, ACT>(p, x_at, res_at, n, c0);
 #pragma unroll
             for (int l = 0; l < L; ++l) f[l] = inside >> l & 1 ? 1.f : -1.f;
         }
@@ -265,6 +268,7 @@ __device__ __forceinline__ void gradient_one(const NormParams &p, const Column<L
     }
 #pragma unroll
     for (int i = 0; i < NP; ++i) dz[i] = two(g[2 * i], g[2 * i + 1]);
+    }
 }
 
 // dx = a dz + c0 + c1 (x - mean),  c0 = -rstd m1, c1 = -rstd^2 m2
@@ -299,26 +303,28 @@ constexpr int NORM_T = 256;
 constexpr int NORM_PITCH = NORM_T + 4;  // floats between the rows of sums per thread, one row per lane: neighbouring lanes in different banks
 constexpr int NORM_AHEAD = 4;           // vectors of a thread in flight
 
-// Number of the pixels r, r + R, ... below n
-__device__ __forceinline__ int pixels_of(int n, int r, int rows) { return r < n ? (n - r + rows - 1) / rows : 0; }
-
-// Threads that share a lane of channels when sums over the R rows of a block are taken
-__device__ __forceinline__ int sharers(int lanes) {
-    int sub = 1;
-    while (sub < 32 && lanes * sub * 2 <= NORM_T) sub *= 2;
-    return sub;
+// 1 / n, to one unit in the last place
+__device__ __forceinline__ float inverse(int n) {
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"((float)n));
+    return r;
 }
-__device__ __forceinline__ float sum_sharers(float s, int sub) {
-    for (int o = sub / 2; o > 0; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+
+// 2^k threads share a lane of channels when sums over the R rows of a block are taken
+__device__ __forceinline__ int sharers_log2(int lanes) { return lanes > NORM_T ? 0 : min(5, 31 - __clz(NORM_T / lanes)); }
+__device__ __forceinline__ float sum_sharers(float s, int log2) {
+#pragma unroll
+    for (int k = 0; k < 5; ++k)
+        if (k < log2) s += __shfl_xor_sync(0xffffffffu, s, 1 << k);
     return s;
 }
 
 // A sums over the rows: v[(a L + lane % L) PITCH + thread], handed to done(lane, sums)
 template <int L, int A, typename F>
 __device__ __forceinline__ void sum_rows(const float *v, int sv, int rows, F done) {
-    const int lanes = sv * L, sub = sharers(lanes), sl = threadIdx.x % sub;
-    for (int q0 = 0; q0 < lanes; q0 += NORM_T / sub) {
-        const int q = q0 + threadIdx.x / sub;
+    const int lanes = sv * L, log2 = sharers_log2(lanes), sub = 1 << log2, sl = threadIdx.x & (sub - 1);
+    for (int q0 = 0; q0 < lanes; q0 += NORM_T >> log2) {
+        const int q = q0 + (threadIdx.x >> log2);
         float s[A];
 #pragma unroll
         for (int a = 0; a < A; ++a) s[a] = 0.f;
@@ -329,34 +335,34 @@ __device__ __forceinline__ void sum_rows(const float *v, int sv, int rows, F don
 #pragma unroll
                 for (int a = 0; a < A; ++a) s[a] += w[a * L * NORM_PITCH + r * sv];
 #pragma unroll
-        for (int a = 0; a < A; ++a) s[a] = sum_sharers(s[a], sub);
+        for (int a = 0; a < A; ++a) s[a] = sum_sharers(s[a], log2);
         if (q < lanes && sl == 0) done(q, s);
     }
 }
 
 // Means and squared deviations of the rows' values put together per lane: v holds every thread's sum and its deviations from its own mean over
-// its `n / rows`, or one more, pixels
+// its `few`, or one more, of the n pixels
 template <int L, typename F>
-__device__ __forceinline__ void combine_rows(const float *v, int sv, int rows, int n, F done) {
-    const int lanes = sv * L, sub = sharers(lanes), sl = threadIdx.x % sub;
-    const int few = n / rows, more = n - few * rows;           // rows below `more` have few + 1 pixels
-    const float inv = n > 0 ? 1.f / (float)n : 0.f, inv_few = few > 0 ? 1.f / (float)few : 0.f, inv_more = 1.f / (float)(few + 1);
+__device__ __forceinline__ void combine_rows(const float *v, int sv, int rows, int n, int few, F done) {
+    const int lanes = sv * L, log2 = sharers_log2(lanes), sub = 1 << log2, sl = threadIdx.x & (sub - 1);
+    const int more = n - few * rows;                           // rows below `more` have few + 1 pixels
+    const float inv = n > 0 ? inverse(n) : 0.f, inv_few = few > 0 ? inverse(few) : 0.f, inv_more = inverse(few + 1);
     const int used = few > 0 ? rows : more;
-    for (int q0 = 0; q0 < lanes; q0 += NORM_T / sub) {
-        const int q = q0 + threadIdx.x / sub;
+    for (int q0 = 0; q0 < lanes; q0 += NORM_T >> log2) {
+        const int q = q0 + (threadIdx.x >> log2);
         const float *w = v + q % L * NORM_PITCH + q / L;
         float s = 0.f, m2 = 0.f;
         if (q < lanes)
 #pragma unroll 4
             for (int r = sl; r < used; r += sub) s += w[r * sv];
-        const float mean = sum_sharers(s, sub) * inv;
+        const float mean = sum_sharers(s, log2) * inv;
         if (q < lanes)
 #pragma unroll 4
             for (int r = sl; r < used; r += sub) {
                 const float d = w[r * sv] * (r < more ? inv_more : inv_few) - mean;
                 m2 += w[L * NORM_PITCH + r * sv] + d * d * (float)(r < more ? few + 1 : few);
             }
-        m2 = sum_sharers(m2, sub);
+        m2 = sum_sharers(m2, log2);
         if (q < lanes && sl == 0) done(q, mean, m2);
     }
 }
@@ -382,7 +388,7 @@ template <int NP> struct Spread {
     }
     // sums and deviations from the means of n values, per lane
     template <int L> __device__ __forceinline__ void store(float *v, int n) const {
-        const float inv = n > 0 ? 1.f / (float)n : 0.f;
+        const float inv = n > 0 ? inverse(n) : 0.f;
 #pragma unroll
         for (int l = 0; l < L; ++l) {
             const float2 k = one_by_one(minus_shift[l / 2]), a = one_by_one(s[l / 2]), b = one_by_one(q[l / 2]);
@@ -414,7 +420,7 @@ __device__ __forceinline__ float team_sum(float s, float *scratch) {
 
 // The pixels and columns of a block
 struct Chunk {
-    int v0, sv, rows, r, col, n, cnt;
+    int v0, sv, rows, r, col, n, few, cnt;
     size_t base, step;
     __device__ __forceinline__ Chunk(const NormParams &p) {
         v0 = blockIdx.y * p.sv;
@@ -424,7 +430,8 @@ struct Chunk {
         col = threadIdx.x - r * sv;
         const int p0 = blockIdx.x * p.per;
         n = min(p.per, p.HW - p0);
-        cnt = r < rows ? pixels_of(n, r, rows) : 0;
+        few = n / rows;
+        cnt = r < rows ? few + (r < n - few * rows) : 0;
         base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
         step = (size_t)rows * p.pv;
     }
@@ -461,7 +468,7 @@ __global__ void __launch_bounds__(NORM_T) norm_partial_kernel(const __grid_const
     if (c.r < c.rows) own.template store<L>(v, c.cnt);
     __syncthreads();
     float2 *part = p.part + ((size_t)blockIdx.z * p.chunks + blockIdx.x) * p.pv * L + c.v0 * L;
-    combine_rows<L>(v, c.sv, c.rows, c.n, [&](int q, float mean, float m2) { part[q] = make_float2(mean, m2); });
+    combine_rows<L>(v, c.sv, c.rows, c.n, c.few, [&](int q, float mean, float m2) { part[q] = make_float2(mean, m2); });
 }
 
 // Chunks and channels of a group put together: mean and rstd
@@ -567,7 +574,7 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_partial_kernel(const __grid_
             for (int i = 0; i < 2; ++i)
                 if (i0 + i < c.cnt) {
                     f2 d[NP], dz[NP];
-                    gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], d, dz);
+                    gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], (const Raw *)p.x + c.base + (i0 + i) * c.step, (const Raw *)p.res + c.base + (i0 + i) * c.step, d, dz);
                     sums.add(d, dz);
                 }
         }
@@ -665,7 +672,7 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_apply_kernel(const __grid_co
         for (int i = 0; i < 2; ++i)
             if (i0 + i < c.cnt) {
                 f2 d[NP], dz[NP];
-                gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], d, dz);
+                gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], (const Raw *)p.x + c.base + (i0 + i) * c.step, (const Raw *)p.res + c.base + (i0 + i) * c.step, d, dz);
                 store_gradient<KIND>(p, k, k0, k1, d, dz, c.base + (i0 + i) * c.step);
             }
     }
@@ -680,13 +687,11 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// two floats in the shared memory of a block of the cluster
-__device__ __forceinline__ float2 remote_float2(const float2 *own, int rank) {
+// writes two floats into the shared memory of a block of the cluster, at the place that `own` has in this one's
+__device__ __forceinline__ void push_float2(const float2 *own, int rank, float2 v) {
     uint32_t a;
-    float2 v;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(own)), "r"(rank));
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
-    return v;
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(v.x), "f"(v.y) : "memory");
 }
 template <typename Raw>
 __device__ __forceinline__ void copy_in(Raw *dst, const Raw *src) {
@@ -697,7 +702,7 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" 
 
 // What a block works on: pixels p0 .. p0 + n of an image, columns v0 .. v0 + sv, groups g0 .. g0 + sg
 struct Share {
-    int v0, sv, g0, sg, p0, n, rows, r, col, cnt;
+    int v0, sv, g0, sg, p0, n, rows, r, col, few, cnt;
     size_t base, step;
     __device__ __forceinline__ Share(const NormParams &p, int L, int rank) {
         g0 = blockIdx.y * p.gs;
@@ -709,19 +714,26 @@ struct Share {
         rows = NORM_T / sv;
         r = threadIdx.x / sv;
         col = threadIdx.x - r * sv;
-        cnt = r < rows ? pixels_of(n, r, rows) : 0;
+        few = n / rows;
+        cnt = r < rows ? few + (r < n - few * rows) : 0;
         base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
         step = (size_t)rows * p.pv;
     }
 };
 
-// f(group, rank's values of lane `rank`) for the groups of the slice: 16 threads a group, thread i with rank i's pair (zeros from `ranks` on)
+// f(group, thread of its team, team, log2 of it) for the groups of the slice (and for numbers behind the last: whole warps go round)
 template <typename F>
-__device__ __forceinline__ void over_ranks(const float2 *group, int sg, int ranks, F f) {
+__device__ __forceinline__ void by_group(int sg, int cpg, F f) {
+    const int log2 = cpg <= 16 ? 4 : 5, team = 1 << log2;
+    for (int g0 = 0; g0 < sg; g0 += NORM_T >> log2) f(g0 + (int)(threadIdx.x >> log2), (int)(threadIdx.x & (team - 1)), team, log2);
+}
+// f(group, pair) for the groups of the slice: 16 threads a group, thread i with what rank i sent (zeros from `ranks` on)
+template <typename F>
+__device__ __forceinline__ void over_ranks(const float2 *inbox, int gs, int sg, int ranks, F f) {
     const int q = threadIdx.x & 15;
     for (int g0 = 0; g0 < sg; g0 += NORM_T / 16) {           // (whole warps go round)
         const int g = g0 + threadIdx.x / 16;
-        f(g, g < sg && q < ranks ? remote_float2(group + g, q) : make_float2(0.f, 0.f));
+        f(g, g < sg && q < ranks ? inbox[q * gs + g] : make_float2(0.f, 0.f));
     }
 }
 __device__ __forceinline__ float sum16(float s) {
@@ -730,24 +742,28 @@ __device__ __forceinline__ float sum16(float s) {
     return s;
 }
 
-// Dynamic shared memory: the data ([pixel of a thread][thread] per tensor), sums per thread (afterwards: what a column needs of its channels), results per
-// group and of the image's groups, results per channel, scale and shift.  What a channel needs is worked out once for all threads.
+// Dynamic shared memory: the data ([pixel of a thread][thread] per tensor), sums per thread (afterwards: what a column needs of its channels), what every
+// rank sends of its groups, the image's groups, results per channel, scale and shift.  What a channel needs is worked out once for all threads.
 __host__ __device__ __forceinline__ size_t norm_sums_bytes(int L, int sv) { return 16 * (size_t)L * (sv > NORM_PITCH / 2 ? sv : NORM_PITCH / 2); }
 struct NormSmem {
     unsigned char *data;
     float *v;
     float4 *constants;                  // over v: -mean, rstd gamma, beta
-    float2 *group, *image, *channel, *affine;
+    float2 *inbox, *image, *channel, *affine;
     template <int L> __device__ __forceinline__ NormSmem(unsigned char *base, const NormParams &p, int tensors, std::integral_constant<int, L>) {
         data = base;
         v = (float *)(base + (size_t)p.data_bytes * tensors);
         constants = (float4 *)v;
-        group = (float2 *)((char *)v + norm_sums_bytes(L, p.sv));
-        image = group + p.gs;
+        inbox = (float2 *)((char *)v + norm_sums_bytes(L, p.sv));
+        image = inbox + p.gs * gridDim.x;
         channel = image + p.gs;
         affine = channel + p.sv * L;
     }
 };
+
+// Where a channel's constants lie: lane by lane, so that threads of neighbouring columns read neighbouring ones
+template <int L>
+__device__ __forceinline__ int slot(int q, int sv) { return q % L * sv + q / L; }
 
 // scale and shift of the slice's channels: read early, needed late
 template <int L>
@@ -768,6 +784,7 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
     const Share s(p, L, rank);
     const NormSmem m(norm_smem, p, 1, std::integral_constant<int, L>());
     Raw *data = (Raw *)m.data;
+    cluster_arrive();                                          // (waited for before the first write into another block)
     pdl_wait();
     pdl_trigger();
 #pragma unroll 4
@@ -788,28 +805,30 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
     }
     if (s.r < s.rows) own.template store<L>(m.v, s.cnt);
     __syncthreads();
-    combine_rows<L>(m.v, s.sv, s.rows, s.n, [&](int q, float mean, float m2) { m.channel[q] = make_float2(mean, m2); });
+    combine_rows<L>(m.v, s.sv, s.rows, s.n, s.few, [&](int q, float mean, float m2) { m.channel[q] = make_float2(mean, m2); });
     __syncthreads();
-    // channels to groups: a warp per group
-    const int lane = t & 31;
-    const float inv_cpg = 1.f / (float)p.cpg, inv_hw = 1.f / (float)p.HW;
-    for (int g = t >> 5; g < s.sg; g += NORM_T / 32) {
+    // channels to groups: 16 or 32 threads a group
+    const float inv_cpg = inverse(p.cpg), inv_hw = inverse(p.HW);
+    cluster_wait();
+    by_group(s.sg, p.cpg, [&](int g, int i, int team, int log2) {
         const float2 *c = m.channel + (s.g0 + g) * p.cpg - s.v0 * L;
         float a = 0.f, b = 0.f;
-        for (int j = lane; j < p.cpg; j += 32) a += c[j].x;
-        a = team_sum<32>(a, nullptr) * inv_cpg;
-        for (int j = lane; j < p.cpg; j += 32) {
-            const float d = c[j].x - a;
-            b += c[j].y + d * d * (float)s.n;
-        }
-        b = team_sum<32>(b, nullptr);
-        if (lane == 0) m.group[g] = make_float2(a, b);
-    }
+        if (g < s.sg)
+            for (int j = i; j < p.cpg; j += team) a += c[j].x;
+        a = sum_sharers(a, log2) * inv_cpg;
+        if (g < s.sg)
+            for (int j = i; j < p.cpg; j += team) {
+                const float d = c[j].x - a;
+                b += c[j].y + d * d * (float)s.n;
+            }
+        b = sum_sharers(b, log2);
+        if (g < s.sg && i < ranks) push_float2(m.inbox + rank * p.gs + g, i, make_float2(a, b));
+    });
     cluster_arrive();
     cluster_wait();
     // the ranks' groups to the image's
     const float pixels = (float)max(0, min(p.per, p.HW - (t & 15) * p.per));
-    over_ranks(m.group, s.sg, ranks, [&](int g, float2 w) {
+    over_ranks(m.inbox, p.gs, s.sg, ranks, [&](int g, float2 w) {
         const float mean = sum16(w.x * pixels) * inv_hw, d = w.x - mean;
         const float m2 = sum16(w.y + d * d * pixels * (float)p.cpg);
         if (g < s.sg && (t & 15) == 0) {
@@ -818,17 +837,16 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
             if (rank == 0) ((float2 *)p.stats)[(size_t)blockIdx.z * p.G + s.g0 + g] = result;
         }
     });
-    cluster_arrive();                                          // (its wait, at the end: no block leaves while others read its groups)
     __syncthreads();
     for (int q = t; q < s.sv * L; q += NORM_T) {
         const float2 w = s.v0 * L + q < p.C ? m.image[(s.v0 * L + q) / p.cpg - s.g0] : make_float2(0.f, 0.f), k = m.affine[q];
-        m.constants[q] = make_float4(-w.x, w.y * k.x, k.y, 0.f);
+        m.constants[slot<L>(q, s.sv)] = make_float4(-w.x, w.y * k.x, k.y, 0.f);
     }
     __syncthreads();
     if (s.cnt > 0) {
         Column<NP> k;
         fill_column<KIND>(k, [&](int l) {
-            const float4 c = m.constants[s.col * L + l];
+            const float4 c = m.constants[l * s.sv + s.col];
             return make_float3(c.x, c.y, c.z);
         });
         for (int i0 = 0; i0 < s.cnt; i0 += NORM_AHEAD) {
@@ -844,7 +862,6 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
                 if (i0 + i < s.cnt) apply_one<KIND, ACT>(p, k, raw[i], res[i], s.base + (i0 + i) * s.step);
         }
     }
-    cluster_wait();
 }
 
 // part: the sums of every rank's channels, [N][ranks][lanes], for the parameters' gradients
@@ -858,6 +875,7 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_
     const NormSmem m(norm_smem, p, p.res ? 3 : 2, std::integral_constant<int, L>());
     Raw *x = (Raw *)m.data, *dy = (Raw *)(m.data + p.data_bytes), *res = p.res ? (Raw *)(m.data + 2 * (size_t)p.data_bytes) : x;
     const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
+    cluster_arrive();
     pdl_wait();
     pdl_trigger();
 #pragma unroll 4
@@ -869,13 +887,13 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_
     fetch_affine<L>(p, s, m.affine);
     for (int q = t; q < s.sv * L; q += NORM_T) {
         const float2 w = s.v0 * L + q < p.C ? __ldcg(stats + (s.v0 * L + q) / p.cpg) : make_float2(0.f, 0.f), k = m.affine[q];
-        m.constants[q] = make_float4(-w.x, w.y * k.x, k.y, w.y);
+        m.constants[slot<L>(q, s.sv)] = make_float4(-w.x, w.y * k.x, k.y, 0.f);
         m.channel[q].x = w.y;
     }
     __syncthreads();
     Column<NP> k;
     fill_column<KIND>(k, [&](int l) {
-        const float4 c = m.constants[s.col * L + l];
+        const float4 c = m.constants[l * s.sv + s.col];
         return make_float3(c.x, c.y, c.z);
     });
     copy_wait();
@@ -883,7 +901,7 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_
 #pragma unroll 2
     for (int i = 0; i < s.cnt; ++i) {
         f2 d[NP], dz[NP];
-        gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], d, dz);
+        gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
         sums.add(d, dz);
     }
     __syncthreads();                                           // (the constants make room for the sums)
@@ -896,44 +914,43 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_
         m.affine[q] = make_float2(m.affine[q].x * c.x, m.affine[q].x * c.y);
     });
     __syncthreads();
-    const int lane = t & 31;
-    for (int g = t >> 5; g < s.sg; g += NORM_T / 32) {
+    cluster_wait();
+    by_group(s.sg, p.cpg, [&](int g, int i, int team, int log2) {
         const float2 *c = m.affine + (s.g0 + g) * p.cpg - s.v0 * L;
         float s1 = 0.f, s2 = 0.f;
-        for (int j = lane; j < p.cpg; j += 32) {
-            s1 += c[j].x;
-            s2 += c[j].y;
-        }
-        s1 = team_sum<32>(s1, nullptr);
-        s2 = team_sum<32>(s2, nullptr);
-        if (lane == 0) m.group[g] = make_float2(s1, s2);
-    }
+        if (g < s.sg)
+            for (int j = i; j < p.cpg; j += team) {
+                s1 += c[j].x;
+                s2 += c[j].y;
+            }
+        s1 = sum_sharers(s1, log2);
+        s2 = sum_sharers(s2, log2);
+        if (g < s.sg && i < ranks) push_float2(m.inbox + rank * p.gs + g, i, make_float2(s1, s2));
+    });
     cluster_arrive();
     cluster_wait();
     const float inv = 1.f / ((float)p.HW * (float)p.cpg);
-    over_ranks(m.group, s.sg, ranks, [&](int g, float2 w) {
+    over_ranks(m.inbox, p.gs, s.sg, ranks, [&](int g, float2 w) {
         const float m1 = sum16(w.x) * inv, m2 = sum16(w.y) * inv;
         if (g < s.sg && (t & 15) == 0) m.image[g] = make_float2(m1, m2);
     });
-    cluster_arrive();
     __syncthreads();
     for (int q = t; q < s.sv * L; q += NORM_T) {
         const float2 w = s.v0 * L + q < p.C ? m.image[(s.v0 * L + q) / p.cpg - s.g0] : make_float2(0.f, 0.f);
         const float rstd = m.channel[q].x;
-        m.affine[q] = make_float2(-rstd * w.x, -rstd * rstd * w.y);
+        ((float2 *)m.v)[slot<L>(q, s.sv)] = make_float2(-rstd * w.x, -rstd * rstd * w.y);
     }
     __syncthreads();
     if (s.cnt > 0) {
         f2 k0[NP], k1[NP];
-        fill_means<KIND>(k0, k1, [&](int l) { return m.affine[s.col * L + l]; });
+        fill_means<KIND>(k0, k1, [&](int l) { return ((const float2 *)m.v)[l * s.sv + s.col]; });
 #pragma unroll 2
         for (int i = 0; i < s.cnt; ++i) {
             f2 d[NP], dz[NP];
-            gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], d, dz);
+            gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
             store_gradient<KIND>(p, k, k0, k1, d, dz, s.base + i * s.step);
         }
     }
-    cluster_wait();
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -965,7 +982,7 @@ static NormCluster norm_cluster(int kind, int N, int HW, int C, int G, int tenso
         c.per = (HW + ranks - 1) / ranks;
         const int rows = NORM_T / widest;
         c.data_bytes = (size_t)((c.per + rows - 1) / rows) * NORM_T * (kind == 2 ? 4 : 16);
-        c.smem = c.data_bytes * tensors + norm_sums_bytes(L, widest) + (size_t)gs * 16 + (size_t)widest * L * 16;
+        c.smem = c.data_bytes * tensors + norm_sums_bytes(L, widest) + (size_t)gs * 8 * (ranks + 1) + (size_t)widest * L * 16;
         c.ranks = c.smem <= NORM_SMEM ? ranks : 0;
         return c;
     };

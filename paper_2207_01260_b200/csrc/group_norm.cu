@@ -81,13 +81,14 @@ __device__ __forceinline__ void unpack_floats(const typename Lanes<KIND>::Raw &r
     for (int l = 0; l < Lanes<KIND>::L; ++l) f[l] = l % 2 ? one_by_one(v[l / 2]).y : one_by_one(v[l / 2]).x;
 }
 
+constexpr int L_of(int kind) { return kind == 0 ? 8 : kind == 1 ? 4 : 1; }
+
 struct NormParams {
     const void *x, *dy, *res;
     void *out, *dres;                   // y, or dx and dresidual
     const float *gamma, *beta;
     float *stats;                       // [N][G][2]: mean, rstd
     float2 *part;                       // partial results of chunks of pixels, [N][chunks][lanes]
-    float2 *means;                      // backward: m1, m2 [N][G]
     float *dgamma, *dbeta;
     int N, HW, C, G, cpg;
     int pv;                             // vectors per pixel
@@ -96,6 +97,7 @@ struct NormParams {
     int per;                            // pixels of a block (on chip: of a rank; else: of a chunk)
     int chunks;
     int gs, data_bytes;                 // on chip: groups of a slice, bytes of a tensor's share of a block
+    int range, room, ring_bytes;        // two passes: groups that a slice touches at most, channels of these or of the slice (both even), bytes of the ring
     int act;
     float eps;
 };
@@ -178,8 +180,8 @@ __device__ __forceinline__ void load_column(const NormParams &p, Column<Lanes<KI
 }
 
 // x - mean, and z
-template <int KIND>
-__device__ __forceinline__ void affine(const NormParams &p, const Column<Lanes<KIND>::NP> &k, const typename Lanes<KIND>::Raw &x, const typename Lanes<KIND>::Raw &res, f2 *d, f2 *z) {
+template <int KIND, bool RES>
+__device__ __forceinline__ void affine(const Column<Lanes<KIND>::NP> &k, const typename Lanes<KIND>::Raw &x, const typename Lanes<KIND>::Raw &res, f2 *d, f2 *z) {
     constexpr int NP = Lanes<KIND>::NP;
     Lanes<KIND>::unpack(x, d);
 #pragma unroll
@@ -187,7 +189,7 @@ __device__ __forceinline__ void affine(const NormParams &p, const Column<Lanes<K
         d[i] = add2(d[i], k.minus_mean[i]);
         z[i] = fma2(d[i], k.a[i], k.beta[i]);
     }
-    if (p.res) {
+    if (RES) {
         f2 r[NP];
         Lanes<KIND>::unpack(res, r);
 #pragma unroll
@@ -195,10 +197,10 @@ __device__ __forceinline__ void affine(const NormParams &p, const Column<Lanes<K
     }
 }
 
-template <int KIND, int ACT>
+template <int KIND, int ACT, bool RES>
 __device__ __forceinline__ void apply_one(const NormParams &p, const Column<Lanes<KIND>::NP> &k, const typename Lanes<KIND>::Raw &x, const typename Lanes<KIND>::Raw &res, size_t at) {
     f2 d[Lanes<KIND>::NP], z[Lanes<KIND>::NP];
-    affine<KIND>(p, k, x, res, d, z);
+    affine<KIND, RES>(k, x, res, d, z);
     ((typename Lanes<KIND>::Raw *)p.out)[at] = finish<KIND, ACT>(z);
 }
 
@@ -209,7 +211,7 @@ __device__ __forceinline__ float lane_of(const typename Lanes<KIND>::Raw *v, int
     if constexpr (KIND == 0) return __bfloat162float(((const __nv_bfloat16 *)v)[l]);
     else return ((const float *)v)[l];
 }
-template <int KIND, int ACT>
+template <int KIND, int ACT, bool RES>
 __device__ __forceinline__ uint32_t inside_64(const NormParams &p, const typename Lanes<KIND>::Raw *x, const typename Lanes<KIND>::Raw *res, int n, int c0) {
     uint32_t inside = 0;
 #pragma unroll 1
@@ -218,20 +220,20 @@ __device__ __forceinline__ uint32_t inside_64(const NormParams &p, const typenam
         double z = ((double)lane_of<KIND>(x, l) - (double)s.x) * (double)s.y;
         if (p.gamma) z *= __ldg(p.gamma + c0 + l);
         if (p.beta) z += __ldg(p.beta + c0 + l);
-        if (p.res) z += lane_of<KIND>(res, l);
+        if (RES) z += lane_of<KIND>(res, l);
         if (z > 0.0 && (ACT != CPRUNE_ACT_RELU6 || z < 6.0)) inside |= 1u << l;
     }
     return inside;
 }
 
 // x - mean and dz of a vector of image n (x_at, res_at: where it lies)
-template <int KIND, int ACT>
+template <int KIND, int ACT, bool RES>
 __device__ __forceinline__ void gradient_one(const NormParams &p, const Column<Lanes<KIND>::NP> &k, int n, int c0, const typename Lanes<KIND>::Raw &x,
                                              const typename Lanes<KIND>::Raw &dy, const typename Lanes<KIND>::Raw &res, const typename Lanes<KIND>::Raw *x_at,
                                              const typename Lanes<KIND>::Raw *res_at, f2 *d, f2 *dz) {
     constexpr int NP = Lanes<KIND>::NP, L = Lanes<KIND>::L;
     f2 z[NP];
-    affine<KIND>(p, k, x, res, d, z);
+    affine<KIND, RES>(k, x, res, d, z);
     Lanes<KIND>::unpack(dy, dz);
     if constexpr (ACT != CPRUNE_ACT_NONE) {
     float f[2 * NP], g[2 * NP];
@@ -250,16 +252,16 @@ __device__ __forceinline__ void gradient_one(const NormParams &p, const Column<L
     } else {
         // Where z is next to 0, |(x - mean) a| is next to |beta + residual|; it is off by two roundings of 2^-24, the sums by one each
         float r[2 * NP];
-        if (p.res) unpack_floats<KIND>(res, r);
+        if (RES) unpack_floats<KIND>(res, r);
         const float near = 4e-7f * k.most, top = 6.f;
         bool close = false;
 #pragma unroll
         for (int l = 0; l < L; ++l) {
-            const float e = p.res ? fmaf(4e-7f, fabsf(r[l]), near) : near;
+            const float e = RES ? fmaf(4e-7f, fabsf(r[l]), near) : near;
             close |= fabsf(f[l]) < e || (ACT == CPRUNE_ACT_RELU6 && fabsf(f[l] - top) < e + 2.4e-6f);
         }
         if (close) {
-            const uint32_t inside = inside_64<KIND, ACT>(p, x_at, res_at, n, c0);
+            const uint32_t inside = inside_64<KIND, ACT, RES>(p, x_at, res_at, n, c0);
 #pragma unroll
             for (int l = 0; l < L; ++l) f[l] = inside >> l & 1 ? 1.f : -1.f;
         }
@@ -400,23 +402,32 @@ template <int NP> struct Spread {
     }
 };
 
-// Sum over the threads of a team (a warp or a block), the same for all of them and in a fixed order
-template <int TEAM>
-__device__ __forceinline__ float team_sum(float s, float *scratch) {
+__device__ __forceinline__ float sum16(float s) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (TEAM > 32) {
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = s;
-        __syncthreads();
-        s = 0.f;
-#pragma unroll
-        for (int i = 0; i < TEAM / 32; ++i) s += scratch[i];
-    }
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     return s;
 }
+// f(group, thread of its team, team, log2 of it) for `sg` groups (and for numbers behind the last: whole warps go round); 16 or 32 threads a group
+template <typename F>
+__device__ __forceinline__ void by_group(int sg, int entries, F f) {
+    const int log2 = entries <= 16 ? 4 : 5, team = 1 << log2;
+    for (int g0 = 0; g0 < sg; g0 += NORM_T >> log2) f(g0 + (int)(threadIdx.x >> log2), (int)(threadIdx.x & (team - 1)), team, log2);
+}
 
-// ---------------------------------------------------------------------------------------------------- three launches
+// ------------------------------------------------------------------------------------------------------- two passes
+
+// Asynchronous copies of 16 (or 4) bytes into the thread's own places of shared memory: nothing but the thread's own wait orders them
+template <typename Raw>
+__device__ __forceinline__ void copy_in(Raw *dst, const Raw *src) {
+    if constexpr (sizeof(Raw) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// pixels of a thread under way: 48 to 64 KB a block, three blocks to an SM
+__host__ __device__ constexpr int ring_of(int tensors) { return tensors == 1 ? 12 : tensors == 2 ? 8 : 5; }
 
 // The pixels and columns of a block
 struct Chunk {
@@ -435,6 +446,43 @@ struct Chunk {
         base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
         step = (size_t)rows * p.pv;
     }
+    __device__ __forceinline__ size_t at(int i) const { return base + i * step; }
+};
+
+// A thread's pixels of T tensors, first to last or last to first, through a ring in shared memory
+template <typename Raw, int T, bool BACK> struct Stream {
+    static constexpr int RING = ring_of(T);
+    Raw *ring;
+    const Chunk &c;
+    const Raw *from[T];
+    __device__ __forceinline__ Stream(void *smem, const Chunk &chunk, const void *a, const void *b = nullptr, const void *d = nullptr) : ring((Raw *)smem + threadIdx.x), c(chunk) {
+        from[0] = (const Raw *)a;
+        if (T > 1) from[T > 1 ? 1 : 0] = (const Raw *)b;
+        if (T > 2) from[T > 2 ? 2 : 0] = (const Raw *)d;
+    }
+    __device__ __forceinline__ void issue(int i, int place) {
+        if (i < c.cnt) {
+            const size_t at = c.at(BACK ? c.cnt - 1 - i : i);
+#pragma unroll
+            for (int k = 0; k < T; ++k) copy_in(ring + (place * T + k) * NORM_T, from[k] + at);
+        }
+        copy_commit();
+    }
+    __device__ __forceinline__ void begin() {
+#pragma unroll
+        for (int i = 0; i < RING - 1; ++i) issue(i, i);
+    }
+    // f(pixel, places of its vectors, NORM_T apart)
+    template <typename F> __device__ __forceinline__ void run(F f) {
+#pragma unroll 1
+        for (int i = 0, place = 0; i < c.cnt; ++i) {
+            copy_wait_but<RING - 2>();
+            f(BACK ? c.cnt - 1 - i : i, ring + place * T * NORM_T);
+            issue(i + RING - 1, place ? place - 1 : RING - 1);
+            if (++place == RING) place = 0;
+        }
+        copy_wait();
+    }
 };
 
 // Mean and squared deviations of a chunk of pixels, channel by channel
@@ -442,84 +490,121 @@ template <int KIND>
 __global__ void __launch_bounds__(NORM_T) norm_partial_kernel(const __grid_constant__ NormParams p) {
     constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
     using Raw = typename Lanes<KIND>::Raw;
-    __shared__ float v[2 * L * NORM_PITCH];
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    float *v = (float *)norm_smem;      // afterwards
+    const Chunk c(p);
     pdl_wait();
     pdl_trigger();
-    const Chunk c(p);
+    Stream<Raw, 1, false> x(norm_smem, c, p.x);
+    x.begin();
     Spread<NP> own;
-    if (c.cnt > 0) {
+    x.run([&](int i, const Raw *at) {
         f2 f[NP];
-        Lanes<KIND>::unpack(((const Raw *)p.x)[c.base], f);
-        own.begin(f);
-    }
-    for (int i0 = 0; i0 < c.cnt; i0 += NORM_AHEAD) {
-        Raw raw[NORM_AHEAD];
-#pragma unroll
-        for (int i = 0; i < NORM_AHEAD; ++i)
-            if (i0 + i < c.cnt) raw[i] = ((const Raw *)p.x)[c.base + (i0 + i) * c.step];
-#pragma unroll
-        for (int i = 0; i < NORM_AHEAD; ++i)
-            if (i0 + i < c.cnt) {
-                f2 f[NP];
-                Lanes<KIND>::unpack(raw[i], f);
-                own.add(f);
-            }
-    }
+        Lanes<KIND>::unpack(*at, f);
+        if (i == 0) own.begin(f);
+        own.add(f);                    // (its first value adds nothing)
+    });
+    __syncthreads();
     if (c.r < c.rows) own.template store<L>(v, c.cnt);
     __syncthreads();
     float2 *part = p.part + ((size_t)blockIdx.z * p.chunks + blockIdx.x) * p.pv * L + c.v0 * L;
     combine_rows<L>(v, c.sv, c.rows, c.n, c.few, [&](int q, float mean, float m2) { part[q] = make_float2(mean, m2); });
 }
 
-// Chunks and channels of a group put together: mean and rstd
-template <int TEAM>
-__global__ void __launch_bounds__(NORM_T) norm_combine_kernel(const __grid_constant__ NormParams p, int lanes) {
-    __shared__ float scratch[NORM_T / 32];
-    pdl_wait();
-    pdl_trigger();
-    const long long id = (long long)blockIdx.x * (NORM_T / TEAM) + threadIdx.x / TEAM;
-    if (id >= (long long)p.N * p.G) return;          // (whole teams)
-    const int n = (int)(id / p.G), g = (int)(id - (long long)n * p.G), t = threadIdx.x % TEAM;
-    const float2 *part = p.part + (size_t)n * p.chunks * lanes + (size_t)g * p.cpg;
-    const int entries = p.chunks * p.cpg;
-    float s = 0.f;
-    for (int e = t; e < entries; e += TEAM) {
-        const int k = e / p.cpg, j = e - k * p.cpg;
-        s += __ldcg(part + (size_t)k * lanes + j).x * (float)min(p.per, p.HW - k * p.per);
+// The groups that a slice touches
+struct GroupRange {
+    int g0, n;
+    __device__ __forceinline__ GroupRange(const NormParams &p, const Chunk &c, int L) {
+        const int first = min(c.v0 * L, p.C - 1), last = min((c.v0 + c.sv) * L, p.C) - 1;
+        g0 = first / p.cpg;
+        n = max(first, last) / p.cpg - g0 + 1;
     }
-    const float count = (float)p.HW * (float)p.cpg, mean = team_sum<TEAM>(s, scratch) / count;
-    s = 0.f;
-    for (int e = t; e < entries; e += TEAM) {
-        const int k = e / p.cpg, j = e - k * p.cpg;
-        const float2 v = __ldcg(part + (size_t)k * lanes + j);
-        const float d = v.x - mean;
-        s += v.y + d * d * (float)min(p.per, p.HW - k * p.per);
-    }
-    const float var = team_sum<TEAM>(s, scratch) / count;
-    if (t == 0) ((float2 *)p.stats)[id] = make_float2(mean, 1.f / sqrtf(var + p.eps));
-}
+};
 
-template <int KIND, int ACT>
-__global__ void __launch_bounds__(NORM_T) norm_apply_kernel(const __grid_constant__ NormParams p) {
+// Chunks of a channel that a thread of the second pass reads, all at once (a channel has up to 32 threads)
+constexpr int CHUNK_BATCH = 8;
+
+// Where a channel's constants lie: lane by lane, so that threads of neighbouring columns read neighbouring ones
+template <int L>
+__device__ __forceinline__ int slot(int q, int sv) { return q % L * sv + q / L; }
+
+template <int KIND, int ACT, bool RES>
+__global__ void __launch_bounds__(NORM_T, 3) norm_apply_kernel(const __grid_constant__ NormParams p, int lanes) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP, T = RES ? 2 : 1;
     using Raw = typename Lanes<KIND>::Raw;
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    const Chunk c(p);
+    const GroupRange range(p, c, L);
+    // backwards: what the first pass read last is still in the cache.  (x and the residual are not what the first pass writes.)
+    Stream<Raw, T, true> x(norm_smem, c, p.x, p.res);
+    x.begin();
+    float2 *image = (float2 *)(norm_smem + (size_t)ring_of(T) * T * NORM_T * sizeof(Raw)), *channel = image + p.range;
+    float4 *constants = (float4 *)(channel + p.room);
     pdl_wait();
     pdl_trigger();
-    const Chunk c(p);
-    if (c.cnt == 0) return;
-    Column<Lanes<KIND>::NP> k;
-    load_column<KIND>(p, k, blockIdx.z, (c.v0 + c.col) * Lanes<KIND>::L);
-    for (int i0 = 0; i0 < c.cnt; i0 += NORM_AHEAD) {
-        Raw raw[NORM_AHEAD], res[NORM_AHEAD];
+    // the chunks of every channel of the groups, all read at once
+    const float inv_hw = inverse(p.HW), inv_cpg = inverse(p.cpg);
+    {
+        const int n = range.n * p.cpg, log2 = sharers_log2(n), sub = 1 << log2, sl = threadIdx.x & (sub - 1);
+        const float2 *part = p.part + (size_t)blockIdx.z * p.chunks * lanes + range.g0 * p.cpg;
+        for (int q0 = 0; q0 < n; q0 += NORM_T >> log2) {
+            const int q = q0 + (threadIdx.x >> log2);
+            float2 w[CHUNK_BATCH];
+            float pixels[CHUNK_BATCH], s = 0.f, m2 = 0.f;
 #pragma unroll
-        for (int i = 0; i < NORM_AHEAD; ++i)
-            if (i0 + i < c.cnt) {
-                raw[i] = ((const Raw *)p.x)[c.base + (i0 + i) * c.step];
-                if (p.res) res[i] = ((const Raw *)p.res)[c.base + (i0 + i) * c.step];
+            for (int i = 0; i < CHUNK_BATCH; ++i) {
+                const int k = sl + (i << log2);
+                pixels[i] = q < n && k < p.chunks ? (float)min(p.per, p.HW - k * p.per) : 0.f;
+                w[i] = q < n && k < p.chunks ? __ldcg(part + (size_t)k * lanes + q) : make_float2(0.f, 0.f);
             }
 #pragma unroll
-        for (int i = 0; i < NORM_AHEAD; ++i)
-            if (i0 + i < c.cnt) apply_one<KIND, ACT>(p, k, raw[i], res[i], c.base + (i0 + i) * c.step);
+            for (int i = 0; i < CHUNK_BATCH; ++i) s += w[i].x * pixels[i];
+            const float mean = sum_sharers(s, log2) * inv_hw;
+#pragma unroll
+            for (int i = 0; i < CHUNK_BATCH; ++i) {
+                const float d = w[i].x - mean;
+                m2 += w[i].y + d * d * pixels[i];
+            }
+            m2 = sum_sharers(m2, log2);
+            if (q < n && sl == 0) channel[q] = make_float2(mean, m2);
+        }
     }
+    __syncthreads();
+    by_group(range.n, p.cpg, [&](int g, int i, int team, int log2) {
+        const float2 *w = channel + g * p.cpg;
+        float a = 0.f, b = 0.f;
+        if (g < range.n)
+            for (int j = i; j < p.cpg; j += team) a += w[j].x;
+        a = sum_sharers(a, log2) * inv_cpg;
+        if (g < range.n)
+            for (int j = i; j < p.cpg; j += team) {
+                const float d = w[j].x - a;
+                b += w[j].y + d * d * (float)p.HW;
+            }
+        b = sum_sharers(b, log2) * inv_hw * inv_cpg;
+        if (g < range.n && i == 0) {
+            const float2 result = make_float2(a, 1.f / sqrtf(b + p.eps));
+            image[g] = result;
+            if (blockIdx.x == 0) ((float2 *)p.stats)[(size_t)blockIdx.z * p.G + range.g0 + g] = result;       // (a group of two slices: the same twice)
+        }
+    });
+    __syncthreads();
+    for (int q = threadIdx.x; q < c.sv * L; q += NORM_T) {
+        const int ch = c.v0 * L + q;
+        float4 k = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (ch < p.C) {
+            const float2 w = image[ch / p.cpg - range.g0];
+            k = make_float4(-w.x, w.y * (p.gamma ? __ldg(p.gamma + ch) : 1.f), p.beta ? __ldg(p.beta + ch) : 0.f, 0.f);
+        }
+        constants[slot<L>(q, c.sv)] = k;
+    }
+    __syncthreads();
+    Column<NP> k;
+    fill_column<KIND>(k, [&](int l) {
+        const float4 w = constants[l * c.sv + c.col];
+        return make_float3(w.x, w.y, w.z);
+    });
+    x.run([&](int i, const Raw *at) { apply_one<KIND, ACT, RES>(p, k, at[0], at[RES ? NORM_T : 0], c.at(i)); });
 }
 
 // Sums of dz and dz (x - mean) of a thread
@@ -545,79 +630,59 @@ template <int NP> struct GradientSums {
     }
 };
 
+// Constants of the slice's channels from global memory: -mean, rstd gamma, beta, rstd
+template <int L>
+__device__ __forceinline__ void fetch_constants(const NormParams &p, const Chunk &c, float4 *constants) {
+    const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
+    for (int q = threadIdx.x; q < c.sv * L; q += NORM_T) {
+        const int ch = c.v0 * L + q;
+        float4 k = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (ch < p.C) {
+            const float2 w = __ldcg(stats + ch / p.cpg);
+            k = make_float4(-w.x, w.y * (p.gamma ? __ldg(p.gamma + ch) : 1.f), p.beta ? __ldg(p.beta + ch) : 0.f, w.y);
+        }
+        constants[slot<L>(q, c.sv)] = k;
+    }
+}
+
 // Sums of dz and dz xhat over a chunk of pixels, channel by channel
-template <int KIND, int ACT>
-__global__ void __launch_bounds__(NORM_T) norm_grad_partial_kernel(const __grid_constant__ NormParams p) {
-    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
+template <int KIND, int ACT, bool RES>
+__global__ void __launch_bounds__(NORM_T, 3) norm_grad_partial_kernel(const __grid_constant__ NormParams p) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP, T = RES ? 3 : 2;
     using Raw = typename Lanes<KIND>::Raw;
-    __shared__ float v[2 * L * NORM_PITCH];
-    pdl_wait();
-    pdl_trigger();
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    float *v = (float *)norm_smem;      // afterwards
+    float4 *constants = (float4 *)(norm_smem + p.ring_bytes);
     const Chunk c(p);
     const int c0 = (c.v0 + c.col) * L;
-    const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
+    pdl_wait();
+    pdl_trigger();
+    Stream<Raw, T, false> x(norm_smem, c, p.x, p.dy, p.res);
+    x.begin();
+    fetch_constants<L>(p, c, constants);
+    __syncthreads();
     GradientSums<NP> sums;
-    if (c.cnt > 0) {
-        Column<NP> k;
-        load_column<KIND>(p, k, blockIdx.z, c0);
-        for (int i0 = 0; i0 < c.cnt; i0 += 2) {
-            Raw x[2], dy[2], res[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (i0 + i < c.cnt) {
-                    const size_t at = c.base + (i0 + i) * c.step;
-                    x[i] = ((const Raw *)p.x)[at];
-                    dy[i] = ((const Raw *)p.dy)[at];
-                    if (p.res) res[i] = ((const Raw *)p.res)[at];
-                }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (i0 + i < c.cnt) {
-                    f2 d[NP], dz[NP];
-                    gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], (const Raw *)p.x + c.base + (i0 + i) * c.step, (const Raw *)p.res + c.base + (i0 + i) * c.step, d, dz);
-                    sums.add(d, dz);
-                }
-        }
-    }
+    Column<NP> k;
+    fill_column<KIND>(k, [&](int l) {
+        const float4 w = constants[l * c.sv + c.col];
+        return make_float3(w.x, w.y, w.z);
+    });
+    x.run([&](int, const Raw *at) {
+        f2 d[NP], dz[NP];
+        const Raw *res = at + (RES ? 2 * NORM_T : 0);
+        gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, c0, at[0], at[NORM_T], *res, at, res, d, dz);
+        sums.add(d, dz);
+    });
+    __syncthreads();
     if (c.r < c.rows) sums.template store<L>(v);
     __syncthreads();
     float2 *part = p.part + ((size_t)blockIdx.z * p.chunks + blockIdx.x) * p.pv * L + c.v0 * L;
-    sum_rows<L, 2>(v, c.sv, c.rows, [&](int q, const float *s) {
-        const int ch = c.v0 * L + q;
-        part[q] = make_float2(s[0], ch < p.C ? s[1] * __ldcg(stats + ch / p.cpg).y : 0.f);
-    });
-}
-
-template <int TEAM>
-__global__ void __launch_bounds__(NORM_T) norm_grad_combine_kernel(const __grid_constant__ NormParams p, int lanes) {
-    __shared__ float scratch[NORM_T / 32];
-    pdl_wait();
-    pdl_trigger();
-    const long long id = (long long)blockIdx.x * (NORM_T / TEAM) + threadIdx.x / TEAM;
-    if (id >= (long long)p.N * p.G) return;
-    const int n = (int)(id / p.G), g = (int)(id - (long long)n * p.G), t = threadIdx.x % TEAM;
-    const float2 *part = p.part + (size_t)n * p.chunks * lanes + (size_t)g * p.cpg;
-    const int entries = p.chunks * p.cpg;
-    float s1 = 0.f, s2 = 0.f;
-    for (int e = t; e < entries; e += TEAM) {
-        const int k = e / p.cpg, j = e - k * p.cpg;
-        const float2 v = __ldcg(part + (size_t)k * lanes + j);
-        const float gamma = p.gamma ? __ldg(p.gamma + g * p.cpg + j) : 1.f;
-        s1 += gamma * v.x;
-        s2 += gamma * v.y;
-    }
-    const float count = (float)p.HW * (float)p.cpg;
-    s1 = team_sum<TEAM>(s1, scratch);
-    s2 = team_sum<TEAM>(s2, scratch);
-    if (t == 0) p.means[id] = make_float2(s1 / count, s2 / count);
+    sum_rows<L, 2>(v, c.sv, c.rows, [&](int q, const float *s) { part[q] = make_float2(s[0], s[1] * constants[slot<L>(q, c.sv)].w); });
 }
 
 // dgamma and dbeta of 32 channels: the partial sums of all images and chunks, eight at a time, in a fixed order; their total in 64 bits
-__global__ void __launch_bounds__(NORM_T) norm_parameter_gradients_kernel(const __grid_constant__ NormParams p, int lanes) {
-    __shared__ double tot[2][8][33];
-    pdl_wait();
-    pdl_trigger();
-    const int cl = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + cl;
+__device__ __forceinline__ void parameter_gradients(const NormParams &p, int lanes, int block, double (*tot)[8][33]) {
+    const int cl = threadIdx.x & 31, k = threadIdx.x >> 5, c = block * 32 + cl;
     double a = 0.0, b = 0.0;
     const long long entries = (long long)p.N * p.chunks;
     if (c < p.C)
@@ -637,45 +702,94 @@ __global__ void __launch_bounds__(NORM_T) norm_parameter_gradients_kernel(const 
         float *to = k ? p.dgamma : p.dbeta;
         if (to) to[c] = (float)s;
     }
+    __syncthreads();
 }
-
-template <int KIND, int ACT>
-__global__ void __launch_bounds__(NORM_T) norm_grad_apply_kernel(const __grid_constant__ NormParams p, int lanes) {
-    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
-    using Raw = typename Lanes<KIND>::Raw;
+__global__ void __launch_bounds__(NORM_T) norm_parameter_gradients_kernel(const __grid_constant__ NormParams p, int lanes) {
+    __shared__ double tot[2][8][33];
     pdl_wait();
     pdl_trigger();
+    parameter_gradients(p, lanes, blockIdx.x, tot);
+}
+
+// The blocks of image N (grid z) take the parameters' gradients
+template <int KIND, int ACT, bool RES>
+__global__ void __launch_bounds__(NORM_T, 3) norm_grad_apply_kernel(const __grid_constant__ NormParams p, int lanes) {
+    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP, T = RES ? 3 : 2;
+    using Raw = typename Lanes<KIND>::Raw;
+    extern __shared__ __align__(16) unsigned char norm_smem[];
+    if (blockIdx.z == p.N) {
+        pdl_wait();
+        pdl_trigger();
+        for (int b = blockIdx.y * gridDim.x + blockIdx.x; b * 32 < p.C; b += gridDim.x * gridDim.y) parameter_gradients(p, lanes, b, (double (*)[8][33])norm_smem);
+        return;
+    }
     const Chunk c(p);
-    if (c.cnt == 0) return;
+    const GroupRange range(p, c, L);
     const int c0 = (c.v0 + c.col) * L;
-    const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G, *means = p.means + (size_t)blockIdx.z * p.G;
+    Stream<Raw, T, true> x(norm_smem, c, p.x, p.dy, p.res);
+    x.begin();
+    float2 *image = (float2 *)(norm_smem + p.ring_bytes), *channel = image + p.range;
+    float4 *constants = (float4 *)(channel + p.room);
+    fetch_constants<L>(p, c, constants);
+    pdl_wait();
+    pdl_trigger();
+    {
+        const int n = range.n * p.cpg, log2 = sharers_log2(n), sub = 1 << log2, sl = threadIdx.x & (sub - 1), first = range.g0 * p.cpg;
+        const float2 *part = p.part + (size_t)blockIdx.z * p.chunks * lanes + first;
+        for (int q0 = 0; q0 < n; q0 += NORM_T >> log2) {
+            const int q = q0 + (threadIdx.x >> log2);
+            const float gamma = p.gamma && q < n ? __ldg(p.gamma + first + q) : 1.f;
+            float2 w[CHUNK_BATCH];
+#pragma unroll
+            for (int i = 0; i < CHUNK_BATCH; ++i) {
+                const int k = sl + (i << log2);
+                w[i] = q < n && k < p.chunks ? __ldcg(part + (size_t)k * lanes + q) : make_float2(0.f, 0.f);
+            }
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < CHUNK_BATCH; ++i) { s1 += w[i].x; s2 += w[i].y; }
+            s1 = sum_sharers(s1, log2);
+            s2 = sum_sharers(s2, log2);
+            if (q < n && sl == 0) channel[q] = make_float2(gamma * s1, gamma * s2);
+        }
+    }
+    __syncthreads();
+    by_group(range.n, p.cpg, [&](int g, int i, int team, int log2) {
+        const float2 *w = channel + g * p.cpg;
+        float s1 = 0.f, s2 = 0.f;
+        if (g < range.n)
+            for (int j = i; j < p.cpg; j += team) { s1 += w[j].x; s2 += w[j].y; }
+        const float inv = 1.f / ((float)p.HW * (float)p.cpg);
+        s1 = sum_sharers(s1, log2) * inv;
+        s2 = sum_sharers(s2, log2) * inv;
+        if (g < range.n && i == 0) image[g] = make_float2(s1, s2);
+    });
+    __syncthreads();
+    float2 *means = channel;            // (their place: sv L of them at most, see the host)
+    for (int q = threadIdx.x; q < c.sv * L; q += NORM_T) {
+        const int ch = c.v0 * L + q;
+        float2 w = make_float2(0.f, 0.f);
+        if (ch < p.C) {
+            const float2 m = image[ch / p.cpg - range.g0];
+            const float rstd = constants[slot<L>(q, c.sv)].w;
+            w = make_float2(-rstd * m.x, -rstd * rstd * m.y);
+        }
+        means[slot<L>(q, c.sv)] = w;
+    }
+    __syncthreads();
     Column<NP> k;
     f2 k0[NP], k1[NP];
-    load_column<KIND>(p, k, blockIdx.z, c0);
-    fill_means<KIND>(k0, k1, [&](int l) {
-        if (c0 + l >= p.C) return make_float2(0.f, 0.f);
-        const float2 m = __ldcg(means + (c0 + l) / p.cpg);
-        const float rstd = __ldcg(stats + (c0 + l) / p.cpg).y;
-        return make_float2(-rstd * m.x, -rstd * rstd * m.y);
+    fill_column<KIND>(k, [&](int l) {
+        const float4 w = constants[l * c.sv + c.col];
+        return make_float3(w.x, w.y, w.z);
     });
-    for (int i0 = 0; i0 < c.cnt; i0 += 2) {
-        Raw x[2], dy[2], res[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i0 + i < c.cnt) {
-                const size_t at = c.base + (i0 + i) * c.step;
-                x[i] = ((const Raw *)p.x)[at];
-                dy[i] = ((const Raw *)p.dy)[at];
-                if (p.res) res[i] = ((const Raw *)p.res)[at];
-            }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (i0 + i < c.cnt) {
-                f2 d[NP], dz[NP];
-                gradient_one<KIND, ACT>(p, k, blockIdx.z, c0, x[i], dy[i], res[i], (const Raw *)p.x + c.base + (i0 + i) * c.step, (const Raw *)p.res + c.base + (i0 + i) * c.step, d, dz);
-                store_gradient<KIND>(p, k, k0, k1, d, dz, c.base + (i0 + i) * c.step);
-            }
-    }
+    fill_means<KIND>(k0, k1, [&](int l) { return means[l * c.sv + c.col]; });
+    x.run([&](int i, const Raw *at) {
+        f2 d[NP], dz[NP];
+        const Raw *res = at + (RES ? 2 * NORM_T : 0);
+        gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, c0, at[0], at[NORM_T], *res, at, res, d, dz);
+        store_gradient<KIND>(p, k, k0, k1, d, dz, c.at(i));
+    });
 }
 
 // ------------------------------------------------------------------------------------------------------- on chip
@@ -693,13 +807,6 @@ __device__ __forceinline__ void push_float2(const float2 *own, int rank, float2 
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(own)), "r"(rank));
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(a), "f"(v.x), "f"(v.y) : "memory");
 }
-template <typename Raw>
-__device__ __forceinline__ void copy_in(Raw *dst, const Raw *src) {
-    if constexpr (sizeof(Raw) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
 // What a block works on: pixels p0 .. p0 + n of an image, columns v0 .. v0 + sv, groups g0 .. g0 + sg
 struct Share {
     int v0, sv, g0, sg, p0, n, rows, r, col, few, cnt;
@@ -721,12 +828,6 @@ struct Share {
     }
 };
 
-// f(group, thread of its team, team, log2 of it) for the groups of the slice (and for numbers behind the last: whole warps go round)
-template <typename F>
-__device__ __forceinline__ void by_group(int sg, int cpg, F f) {
-    const int log2 = cpg <= 16 ? 4 : 5, team = 1 << log2;
-    for (int g0 = 0; g0 < sg; g0 += NORM_T >> log2) f(g0 + (int)(threadIdx.x >> log2), (int)(threadIdx.x & (team - 1)), team, log2);
-}
 // f(group, pair) for the groups of the slice: 16 threads a group, thread i with what rank i sent (zeros from `ranks` on)
 template <typename F>
 __device__ __forceinline__ void over_ranks(const float2 *inbox, int gs, int sg, int ranks, F f) {
@@ -735,11 +836,6 @@ __device__ __forceinline__ void over_ranks(const float2 *inbox, int gs, int sg, 
         const int g = g0 + threadIdx.x / 16;
         f(g, g < sg && q < ranks ? inbox[q * gs + g] : make_float2(0.f, 0.f));
     }
-}
-__device__ __forceinline__ float sum16(float s) {
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    return s;
 }
 
 // Dynamic shared memory: the data ([pixel of a thread][thread] per tensor), sums per thread (afterwards: what a column needs of its channels), what every
@@ -761,10 +857,6 @@ struct NormSmem {
     }
 };
 
-// Where a channel's constants lie: lane by lane, so that threads of neighbouring columns read neighbouring ones
-template <int L>
-__device__ __forceinline__ int slot(int q, int sv) { return q % L * sv + q / L; }
-
 // scale and shift of the slice's channels: read early, needed late
 template <int L>
 __device__ __forceinline__ void fetch_affine(const NormParams &p, const Share &s, float2 *to) {
@@ -775,7 +867,7 @@ __device__ __forceinline__ void fetch_affine(const NormParams &p, const Share &s
     }
 }
 
-template <int KIND, int ACT>
+template <int KIND, int ACT, bool RES>
 __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_constant__ NormParams p) {
     constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
     using Raw = typename Lanes<KIND>::Raw;
@@ -855,25 +947,25 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
             for (int i = 0; i < NORM_AHEAD; ++i)
                 if (i0 + i < s.cnt) {
                     raw[i] = data[(i0 + i) * NORM_T + t];
-                    if (p.res) res[i] = ((const Raw *)p.res)[s.base + (i0 + i) * s.step];
+                    if (RES) res[i] = ((const Raw *)p.res)[s.base + (i0 + i) * s.step];
                 }
 #pragma unroll
             for (int i = 0; i < NORM_AHEAD; ++i)
-                if (i0 + i < s.cnt) apply_one<KIND, ACT>(p, k, raw[i], res[i], s.base + (i0 + i) * s.step);
+                if (i0 + i < s.cnt) apply_one<KIND, ACT, RES>(p, k, raw[i], res[i], s.base + (i0 + i) * s.step);
         }
     }
 }
 
 // part: the sums of every rank's channels, [N][ranks][lanes], for the parameters' gradients
-template <int KIND, int ACT>
+template <int KIND, int ACT, bool RES>
 __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_constant__ NormParams p, int lanes) {
     constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
     using Raw = typename Lanes<KIND>::Raw;
     extern __shared__ __align__(16) unsigned char norm_smem[];
     const int ranks = gridDim.x, rank = (int)cluster_rank(), t = threadIdx.x;
     const Share s(p, L, rank);
-    const NormSmem m(norm_smem, p, p.res ? 3 : 2, std::integral_constant<int, L>());
-    Raw *x = (Raw *)m.data, *dy = (Raw *)(m.data + p.data_bytes), *res = p.res ? (Raw *)(m.data + 2 * (size_t)p.data_bytes) : x;
+    const NormSmem m(norm_smem, p, RES ? 3 : 2, std::integral_constant<int, L>());
+    Raw *x = (Raw *)m.data, *dy = (Raw *)(m.data + p.data_bytes), *res = RES ? (Raw *)(m.data + 2 * (size_t)p.data_bytes) : x;
     const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
     cluster_arrive();
     pdl_wait();
@@ -882,7 +974,7 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_
     for (int i = 0; i < s.cnt; ++i) {
         copy_in(x + i * NORM_T + t, (const Raw *)p.x + s.base + i * s.step);
         copy_in(dy + i * NORM_T + t, (const Raw *)p.dy + s.base + i * s.step);
-        if (p.res) copy_in(res + i * NORM_T + t, (const Raw *)p.res + s.base + i * s.step);
+        if (RES) copy_in(res + i * NORM_T + t, (const Raw *)p.res + s.base + i * s.step);
     }
     fetch_affine<L>(p, s, m.affine);
     for (int q = t; q < s.sv * L; q += NORM_T) {
@@ -901,7 +993,7 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_
 #pragma unroll 2
     for (int i = 0; i < s.cnt; ++i) {
         f2 d[NP], dz[NP];
-        gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
+        gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
         sums.add(d, dz);
     }
     __syncthreads();                                           // (the constants make room for the sums)
@@ -947,7 +1039,7 @@ __global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_
 #pragma unroll 2
         for (int i = 0; i < s.cnt; ++i) {
             f2 d[NP], dz[NP];
-            gradient_one<KIND, ACT>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
+            gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
             store_gradient<KIND>(p, k, k0, k1, d, dz, s.base + i * s.step);
         }
     }
@@ -1006,21 +1098,42 @@ static NormCluster norm_cluster(int kind, int N, int HW, int C, int G, int tenso
     return best;
 }
 
+// The limits of a kernel are attributes of a device
 template <typename K>
-static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaStream_t st, const NormParams &p, int lanes) {
+static cprune_status make_ready(K kernel, bool cluster) {
     int dev = 0;
     CPRUNE_CUDA_CHECK(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) return CPRUNE_ERR_UNSUPPORTED;
     static std::mutex mu;
-    static std::set<std::pair<int, const void *>> ready;        // the limits of a kernel are attributes of a device
-    {
-        std::lock_guard<std::mutex> lock(mu);
-        if (!ready.count({dev, (const void *)kernel})) {
-            CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_SMEM));
-            CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-            ready.insert({dev, (const void *)kernel});
-        }
-    }
+    static std::set<std::pair<int, const void *>> ready;
+    std::lock_guard<std::mutex> lock(mu);
+    if (ready.count({dev, (const void *)kernel})) return CPRUNE_OK;
+    CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_SMEM));
+    if (cluster) CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    ready.insert({dev, (const void *)kernel});
+    return CPRUNE_OK;
+}
+
+// The ring is also the place of the sums
+static int norm_ring_bytes(int kind, int tensors) {
+    const int ring = ring_of(tensors) * tensors * NORM_T * (kind == 2 ? 4 : 16), sums = 2 * L_of(kind) * NORM_PITCH * 4;
+    return ring > sums ? ring : sums;
+}
+// Behind it: results of the groups that a slice touches and of their channels (or, later, of its own), constants of its channels
+static size_t norm_pass_bytes(const NormParams &p, int L) { return (size_t)p.range * 8 + (size_t)p.room * 8 + (size_t)p.sv * L * 16; }
+
+template <typename K>
+static cprune_status launch_pass(K kernel, dim3 grid, size_t smem, cudaStream_t st, const NormParams &p, int lanes) {
+    const cprune_status s = make_ready(kernel, false);
+    if (s != CPRUNE_OK) return s;
+    if constexpr (std::is_invocable_v<K, NormParams, int>) CPRUNE_CUDA_CHECK(launch_chained(kernel, grid, dim3(NORM_T), smem, st, p, lanes));
+    else CPRUNE_CUDA_CHECK(launch_chained(kernel, grid, dim3(NORM_T), smem, st, p));
+    return CPRUNE_OK;
+}
+
+template <typename K>
+static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaStream_t st, const NormParams &p, int lanes) {
+    const cprune_status s = make_ready(kernel, true);
+    if (s != CPRUNE_OK) return s;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(c.ranks, c.slices, N);
     cfg.blockDim = dim3(NORM_T);
@@ -1052,8 +1165,11 @@ static int norm_kind(int type, int C, uintptr_t addresses) {
     return C % 4 == 0 && (addresses & 15) == 0 ? 1 : 2;
 }
 
-// Chunks of about `target` vectors, in whole rounds of the block's threads; never more of them than fit a grid's second dimension
-static NormTiling norm_tiling(int kind, int HW, int C) {
+// Chunks of pixels: as many blocks as are resident at a time (three to an SM), so that none waits for a second round, and at most as many
+// an image as the threads of a block of the second pass read at once
+constexpr int NORM_RESIDENT = 3 * 148;
+
+static NormTiling norm_tiling(int kind, int N, int HW, int C, int G) {
     NormTiling t;
     const int L = kind == 0 ? 8 : kind == 1 ? 4 : 1;
     t.lanes = kind == 0 ? cprune_padded_channels(C) : C;
@@ -1062,50 +1178,62 @@ static NormTiling norm_tiling(int kind, int HW, int C) {
     t.sv = (pv + t.slices - 1) / t.slices;
     t.slices = (pv + t.sv - 1) / t.sv;
     t.rows = NORM_T / t.sv;
-    const int rounds = 8;
-    t.per = t.rows * rounds;
+    long long chunks = NORM_RESIDENT / ((long long)N * t.slices);
+    const long long rounds = (HW + t.rows - 1) / t.rows, most = (rounds + 3) / 4;         // (four rounds of a block's threads at least)
+    if (chunks > most) chunks = most;
+    int readers = 1;                       // threads to a channel (of the groups that a slice touches)
+    const int touched = (t.sv * L + C / G - 1) / (C / G) + 1, channels = (touched < G ? touched : G) * (C / G);
+    while (readers < 32 && channels * readers * 2 <= NORM_T) readers *= 2;
+    if (chunks > CHUNK_BATCH * readers) chunks = CHUNK_BATCH * readers;
+    if (chunks < 1) chunks = 1;
+    t.per = (HW + (int)chunks - 1) / (int)chunks;
     t.chunks = (HW + t.per - 1) / t.per;
     return t;
 }
 
 // (the on-chip kernels have one chunk to a rank)
-static size_t norm_part_bytes(int N, int HW, int C, int kind) {
-    const NormTiling t = norm_tiling(kind, HW, C);
+static size_t norm_part_bytes(int N, int HW, int C, int G, int kind) {
+    const NormTiling t = norm_tiling(kind, N, HW, C, G);
     return ((size_t)N * (t.chunks > 16 ? t.chunks : 16) * t.lanes * sizeof(float2) + 255) / 256 * 256;
 }
+
+constexpr int NORM_GROUP = 8192;          // channels of a group: the second pass holds two groups' results in shared memory
 
 static cprune_status norm_check(int type, int N, int H, int W, int C, int groups, int act) {
     if ((type != CPRUNE_TYPE_BF16 && type != CPRUNE_TYPE_F32) || N <= 0 || H <= 0 || W <= 0 || C <= 0 || groups <= 0 || C % groups) return CPRUNE_ERR_INVALID_ARG;
     if (act < CPRUNE_ACT_NONE || act > CPRUNE_ACT_SILU) return CPRUNE_ERR_INVALID_ARG;
     const long long hw = (long long)H * W;
-    if (C > (1 << 20) || hw * (C + 16LL) > 0x7fffffffLL || N > 65535 || (long long)N * groups > 0x7fffffffLL) return CPRUNE_ERR_UNSUPPORTED;
+    if (C / groups > NORM_GROUP || hw * (C + 16LL) > 0x7fffffffLL || N > 65534 || (long long)N * groups > 0x7fffffffLL) return CPRUNE_ERR_UNSUPPORTED;
     return CPRUNE_OK;
 }
 
-// f(kind, activation) with both as constants
+// f(kind, activation, whether there is a residual), each as a constant
 template <typename F>
-static cprune_status by_kind(int kind, int act, F f) {
-    auto with = [&](auto k) -> cprune_status {
+static cprune_status by_kind(int kind, int act, bool residual, F f) {
+    auto third = [&](auto k, auto a) -> cprune_status { return residual ? f(k, a, std::true_type()) : f(k, a, std::false_type()); };
+    auto second = [&](auto k) -> cprune_status {
         switch (act) {
-            case CPRUNE_ACT_RELU: return f(k, std::integral_constant<int, CPRUNE_ACT_RELU>());
-            case CPRUNE_ACT_RELU6: return f(k, std::integral_constant<int, CPRUNE_ACT_RELU6>());
-            case CPRUNE_ACT_SILU: return f(k, std::integral_constant<int, CPRUNE_ACT_SILU>());
-            default: return f(k, std::integral_constant<int, CPRUNE_ACT_NONE>());
+            case CPRUNE_ACT_RELU: return third(k, std::integral_constant<int, CPRUNE_ACT_RELU>());
+            case CPRUNE_ACT_RELU6: return third(k, std::integral_constant<int, CPRUNE_ACT_RELU6>());
+            case CPRUNE_ACT_SILU: return third(k, std::integral_constant<int, CPRUNE_ACT_SILU>());
+            default: return third(k, std::integral_constant<int, CPRUNE_ACT_NONE>());
         }
     };
-    return kind == 0 ? with(std::integral_constant<int, 0>()) : kind == 1 ? with(std::integral_constant<int, 1>()) : with(std::integral_constant<int, 2>());
+    return kind == 0 ? second(std::integral_constant<int, 0>()) : kind == 1 ? second(std::integral_constant<int, 1>()) : second(std::integral_constant<int, 2>());
 }
 
 static NormParams norm_params(int kind, int N, int H, int W, int C, int groups, int act) {
     NormParams p = {};
     p.N = N; p.HW = H * W; p.C = C; p.G = groups; p.cpg = C / groups; p.act = act;
-    const NormTiling t = norm_tiling(kind, p.HW, C);
+    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
     p.pv = t.lanes / (kind == 0 ? 8 : kind == 1 ? 4 : 1);
     p.sv = t.sv; p.rows = t.rows; p.per = t.per; p.chunks = t.chunks;
+    const int touched = (t.sv * L_of(kind) + p.cpg - 1) / p.cpg + 1;
+    p.range = round_up(touched < groups ? touched : groups, 2);             // (what lies behind stays on 16 bytes)
+    const int channels = (touched < groups ? touched : groups) * p.cpg, own = t.sv * L_of(kind);
+    p.room = round_up(channels > own ? channels : own, 2);
     return p;
 }
-
-constexpr int NORM_TEAM_ENTRIES = 1024;      // a group of more chunk results than this is put together by a block, not by a warp
 
 }  // namespace cprune
 
@@ -1118,10 +1246,10 @@ size_t cprune_group_norm_workspace_bytes(int type, int N, int H, int W, int C, i
     size_t most = 0;
     for (int kind = type == CPRUNE_TYPE_BF16 ? 0 : 1; kind <= (type == CPRUNE_TYPE_BF16 ? 0 : 2); ++kind) {
         if (kind == 1 && C % 4) continue;
-        const size_t b = norm_part_bytes(N, H * W, C, kind);
+        const size_t b = norm_part_bytes(N, H * W, C, groups, kind);
         most = b > most ? b : most;
     }
-    return most + (backward ? ((size_t)N * groups * sizeof(float2) + 255) / 256 * 256 : 0);
+    return most;
 }
 
 cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, int C, int groups, const float *gamma, const float *beta, float eps, int act,
@@ -1132,28 +1260,27 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
     const uintptr_t tensors = (uintptr_t)x | (uintptr_t)y | (uintptr_t)residual;
     if (tensors & (type == CPRUNE_TYPE_BF16 ? 15 : 3) || ((uintptr_t)gamma | (uintptr_t)beta) & 3 || (uintptr_t)stats & 7 || (uintptr_t)workspace & 15) return CPRUNE_ERR_INVALID_ARG;
     const int kind = norm_kind(type, C, tensors);
-    if (workspace_bytes < norm_part_bytes(N, H * W, C, kind) || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < norm_part_bytes(N, H * W, C, groups, kind) || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
     NormParams p = norm_params(kind, N, H, W, C, groups, act);
     p.x = x; p.res = residual; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats; p.eps = eps;
     p.part = (float2 *)workspace;
-    const NormTiling t = norm_tiling(kind, p.HW, C);
+    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
     cudaStream_t st = (cudaStream_t)stream;
     const NormCluster c = norm_cluster(kind, N, p.HW, C, groups, 1);
-    return by_kind(kind, act, [&](auto k, auto a) -> cprune_status {
+    return by_kind(kind, act, residual != nullptr, [&](auto k, auto a, auto r) -> cprune_status {
         constexpr int K = decltype(k)::value, A = decltype(a)::value;
+        constexpr bool R = decltype(r)::value;
         if (c.ranks) {
             p.gs = c.gs; p.sv = c.widest; p.per = c.per; p.data_bytes = (int)c.data_bytes;
-            return launch_cluster(norm_cluster_kernel<K, A>, c, N, st, p, t.lanes);
+            return launch_cluster(norm_cluster_kernel<K, A, R>, c, N, st, p, t.lanes);
         }
         const dim3 grid(t.chunks, t.slices, N);
         ChainScope chain;
-        CPRUNE_CUDA_CHECK(launch_chained(norm_partial_kernel<K>, grid, dim3(NORM_T), 0, st, p));
+        const cprune_status e = launch_pass(norm_partial_kernel<K>, grid, norm_ring_bytes(K, 1), st, p, t.lanes);
+        if (e != CPRUNE_OK) return e;
         chain.follow();
-        const long long ids = (long long)N * groups;
-        if ((long long)t.chunks * p.cpg > NORM_TEAM_ENTRIES) CPRUNE_CUDA_CHECK(launch_chained(norm_combine_kernel<NORM_T>, dim3((unsigned)ids), dim3(NORM_T), 0, st, p, t.lanes));
-        else CPRUNE_CUDA_CHECK(launch_chained(norm_combine_kernel<32>, dim3((unsigned)ceil_div(ids, NORM_T / 32)), dim3(NORM_T), 0, st, p, t.lanes));
-        CPRUNE_CUDA_CHECK(launch_chained(norm_apply_kernel<K, A>, grid, dim3(NORM_T), 0, st, p));
-        return CPRUNE_OK;
+        p.ring_bytes = ring_of(R + 1) * (R + 1) * NORM_T * (K == 2 ? 4 : 16);
+        return launch_pass(norm_apply_kernel<K, A, R>, grid, p.ring_bytes + norm_pass_bytes(p, L_of(K)), st, p, t.lanes);
     });
 }
 
@@ -1167,37 +1294,33 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
     const uintptr_t floats = (uintptr_t)gamma | (uintptr_t)beta | (uintptr_t)dgamma | (uintptr_t)dbeta;
     if (tensors & (type == CPRUNE_TYPE_BF16 ? 15 : 3) || floats & 3 || (uintptr_t)stats & 7 || (uintptr_t)workspace & 15) return CPRUNE_ERR_INVALID_ARG;
     const int kind = norm_kind(type, C, tensors);
-    const size_t part_bytes = norm_part_bytes(N, H * W, C, kind);
-    if (workspace_bytes < part_bytes + (size_t)N * groups * sizeof(float2) || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    const size_t part_bytes = norm_part_bytes(N, H * W, C, groups, kind);
+    if (workspace_bytes < part_bytes || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
     NormParams p = norm_params(kind, N, H, W, C, groups, act);
     p.x = x; p.dy = dy; p.res = residual; p.out = dx; p.dres = dresidual; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float *>(stats);
     p.dgamma = dgamma; p.dbeta = dbeta;
     p.part = (float2 *)workspace;
-    p.means = (float2 *)((char *)workspace + part_bytes);
-    const NormTiling t = norm_tiling(kind, p.HW, C);
+    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
     cudaStream_t st = (cudaStream_t)stream;
     const NormCluster c = norm_cluster(kind, N, p.HW, C, groups, residual ? 3 : 2);
-    return by_kind(kind, act, [&](auto k, auto a) -> cprune_status {
+    return by_kind(kind, act, residual != nullptr, [&](auto k, auto a, auto r) -> cprune_status {
         constexpr int K = decltype(k)::value, A = decltype(a)::value;
+        constexpr bool R = decltype(r)::value;
         ChainScope chain;
         if (c.ranks) {
             p.gs = c.gs; p.sv = c.widest; p.per = c.per; p.data_bytes = (int)c.data_bytes; p.chunks = c.ranks;
-            const cprune_status e = launch_cluster(norm_grad_cluster_kernel<K, A>, c, N, st, p, t.lanes);
+            const cprune_status e = launch_cluster(norm_grad_cluster_kernel<K, A, R>, c, N, st, p, t.lanes);
             if (e != CPRUNE_OK || !(dgamma || dbeta)) return e;
             chain.follow();
             CPRUNE_CUDA_CHECK(launch_chained(norm_parameter_gradients_kernel, dim3((C + 31) / 32), dim3(NORM_T), 0, st, p, t.lanes));
             return CPRUNE_OK;
         }
         const dim3 grid(t.chunks, t.slices, N);
-        CPRUNE_CUDA_CHECK(launch_chained(norm_grad_partial_kernel<K, A>, grid, dim3(NORM_T), 0, st, p));
+        p.ring_bytes = norm_ring_bytes(K, R + 2);
+        const cprune_status e = launch_pass(norm_grad_partial_kernel<K, A, R>, grid, p.ring_bytes + (size_t)p.sv * L_of(K) * 16, st, p, t.lanes);
+        if (e != CPRUNE_OK) return e;
         chain.follow();
-        const long long ids = (long long)N * groups;
-        if ((long long)t.chunks * p.cpg > NORM_TEAM_ENTRIES)
-            CPRUNE_CUDA_CHECK(launch_chained(norm_grad_combine_kernel<NORM_T>, dim3((unsigned)ids), dim3(NORM_T), 0, st, p, t.lanes));
-        else CPRUNE_CUDA_CHECK(launch_chained(norm_grad_combine_kernel<32>, dim3((unsigned)ceil_div(ids, NORM_T / 32)), dim3(NORM_T), 0, st, p, t.lanes));
-        if (dgamma || dbeta) CPRUNE_CUDA_CHECK(launch_chained(norm_parameter_gradients_kernel, dim3((C + 31) / 32), dim3(NORM_T), 0, st, p, t.lanes));
-        CPRUNE_CUDA_CHECK(launch_chained(norm_grad_apply_kernel<K, A>, grid, dim3(NORM_T), 0, st, p, t.lanes));
-        return CPRUNE_OK;
+        return launch_pass(norm_grad_apply_kernel<K, A, R>, dim3(t.chunks, t.slices, N + (dgamma || dbeta ? 1 : 0)), p.ring_bytes + norm_pass_bytes(p, L_of(K)), st, p, t.lanes);
     });
 }
 

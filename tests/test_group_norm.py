@@ -272,7 +272,7 @@ def test_refusals(cp):
         assert call(x=0x1008) == 1 and call(res=0x1002) == 1 and call(stats=0x4004) == 1 and call(work=0x5004) == 1
         assert call(type=1, x=0x1002) == 1
         assert call(size=16) == 3 and call(work=None) == 3
-        assert call(N=70000) == 2
+        assert call(N=70000) == 2 and call(C=16400, G=2) == 2
     assert forward(y=None) == 1 and forward(eps=0.0) == 1 and forward(eps=-1.0) == 1 and forward(eps=float("nan")) == 1 and forward(eps=float("inf")) == 1
     assert forward(H=0) == 1 and forward(H=1 << 15, W=1 << 12) == 2
     assert backward(dy=None) == 1 and backward(dx=None) == 1 and backward(dres=0x6000) == 1

@@ -94,8 +94,8 @@ struct NormParams {
     int pv;                             // vectors per pixel
     int sv;                             // columns (vectors) of a block's slice; slices of the last range may reach beyond pv
     int rows;                           // R: pixels that the block's threads hold side by side
-    int per;                            // pixels of a block (on chip: of a rank; else: of a chunk)
-    int chunks;
+    int per;                            // on chip: pixels of a rank
+    int chunks;                         // two passes: blocks that share an image
     int gs, data_bytes;                 // on chip: groups of a slice, bytes of a tensor's share of a block
     int range, room, ring_bytes;        // two passes: groups that a slice touches at most, channels of these or of the slice (both even), bytes of the ring
     int act;
@@ -429,6 +429,20 @@ template <int N> __device__ __forceinline__ void copy_wait_but() { asm volatile(
 // pixels of a thread under way: 48 to 64 KB a block, three blocks to an SM
 __host__ __device__ constexpr int ring_of(int tensors) { return tensors == 1 ? 12 : tensors == 2 ? 8 : 5; }
 
+// Chunk k of an image: every chunks-th round of the block's rows, from the k-th on (blocks of an image read neighbouring rows at the same time).  The first
+// `last` chunks have a round more, chunk `last` the rows that fill none.
+struct Rounds {
+    int few, last, rest, rows;
+    __device__ __forceinline__ Rounds(const NormParams &p) : rows(p.rows) {
+        const int rounds = p.HW / p.rows;
+        few = rounds / p.chunks;
+        last = rounds - few * p.chunks;
+        rest = p.HW - rounds * p.rows;
+    }
+    __device__ __forceinline__ int full(int k) const { return few + (k < last); }
+    __device__ __forceinline__ int pixels(int k) const { return full(k) * rows + (k == last ? rest : 0); }
+};
+
 // The pixels and columns of a block
 struct Chunk {
     int v0, sv, rows, r, col, n, few, cnt;
@@ -436,15 +450,15 @@ struct Chunk {
     __device__ __forceinline__ Chunk(const NormParams &p) {
         v0 = blockIdx.y * p.sv;
         sv = min(p.sv, p.pv - v0);
-        rows = NORM_T / sv;
+        rows = p.rows;
         r = threadIdx.x / sv;
         col = threadIdx.x - r * sv;
-        const int p0 = blockIdx.x * p.per;
-        n = min(p.per, p.HW - p0);
-        few = n / rows;
+        const Rounds rounds(p);
+        few = rounds.full(blockIdx.x);
+        n = rounds.pixels(blockIdx.x);
         cnt = r < rows ? few + (r < n - few * rows) : 0;
-        base = ((size_t)blockIdx.z * p.HW + p0 + r) * p.pv + v0 + col;
-        step = (size_t)rows * p.pv;
+        base = ((size_t)blockIdx.z * p.HW + blockIdx.x * rows + r) * p.pv + v0 + col;
+        step = (size_t)p.chunks * rows * p.pv;
     }
     __device__ __forceinline__ size_t at(int i) const { return base + i * step; }
 };
@@ -540,11 +554,17 @@ __global__ void __launch_bounds__(NORM_T, 3) norm_apply_kernel(const __grid_cons
     x.begin();
     float2 *image = (float2 *)(norm_smem + (size_t)ring_of(T) * T * NORM_T * sizeof(Raw)), *channel = image + p.range;
     float4 *constants = (float4 *)(channel + p.room);
+    for (int q = threadIdx.x; q < c.sv * L; q += NORM_T) {
+        const int ch = c.v0 * L + q;
+        constants[slot<L>(q, c.sv)] = ch < p.C ? make_float4(0.f, p.gamma ? __ldg(p.gamma + ch) : 1.f, p.beta ? __ldg(p.beta + ch) : 0.f, __int_as_float(ch / p.cpg - range.g0))
+                                               : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
     pdl_wait();
     pdl_trigger();
     // the chunks of every channel of the groups, all read at once
     const float inv_hw = inverse(p.HW), inv_cpg = inverse(p.cpg);
     {
+        const Rounds rounds(p);
         const int n = range.n * p.cpg, log2 = sharers_log2(n), sub = 1 << log2, sl = threadIdx.x & (sub - 1);
         const float2 *part = p.part + (size_t)blockIdx.z * p.chunks * lanes + range.g0 * p.cpg;
         for (int q0 = 0; q0 < n; q0 += NORM_T >> log2) {
@@ -554,7 +574,7 @@ __global__ void __launch_bounds__(NORM_T, 3) norm_apply_kernel(const __grid_cons
 #pragma unroll
             for (int i = 0; i < CHUNK_BATCH; ++i) {
                 const int k = sl + (i << log2);
-                pixels[i] = q < n && k < p.chunks ? (float)min(p.per, p.HW - k * p.per) : 0.f;
+                pixels[i] = q < n && k < p.chunks ? (float)rounds.pixels(k) : 0.f;
                 w[i] = q < n && k < p.chunks ? __ldcg(part + (size_t)k * lanes + q) : make_float2(0.f, 0.f);
             }
 #pragma unroll
@@ -590,13 +610,12 @@ __global__ void __launch_bounds__(NORM_T, 3) norm_apply_kernel(const __grid_cons
     });
     __syncthreads();
     for (int q = threadIdx.x; q < c.sv * L; q += NORM_T) {
-        const int ch = c.v0 * L + q;
-        float4 k = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (ch < p.C) {
-            const float2 w = image[ch / p.cpg - range.g0];
-            k = make_float4(-w.x, w.y * (p.gamma ? __ldg(p.gamma + ch) : 1.f), p.beta ? __ldg(p.beta + ch) : 0.f, 0.f);
+        float4 &k = constants[slot<L>(q, c.sv)];               // (this thread's own)
+        if (c.v0 * L + q < p.C) {
+            const float2 w = image[__float_as_int(k.w)];
+            k.x = -w.x;
+            k.y *= w.y;
         }
-        constants[slot<L>(q, c.sv)] = k;
     }
     __syncthreads();
     Column<NP> k;
@@ -704,13 +723,6 @@ __device__ __forceinline__ void parameter_gradients(const NormParams &p, int lan
     }
     __syncthreads();
 }
-__global__ void __launch_bounds__(NORM_T) norm_parameter_gradients_kernel(const __grid_constant__ NormParams p, int lanes) {
-    __shared__ double tot[2][8][33];
-    pdl_wait();
-    pdl_trigger();
-    parameter_gradients(p, lanes, blockIdx.x, tot);
-}
-
 // The blocks of image N (grid z) take the parameters' gradients
 template <int KIND, int ACT, bool RES>
 __global__ void __launch_bounds__(NORM_T, 3) norm_grad_apply_kernel(const __grid_constant__ NormParams p, int lanes) {
@@ -956,145 +968,47 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
     }
 }
 
-// part: the sums of every rank's channels, [N][ranks][lanes], for the parameters' gradients
-template <int KIND, int ACT, bool RES>
-__global__ void __launch_bounds__(NORM_T) norm_grad_cluster_kernel(const __grid_constant__ NormParams p, int lanes) {
-    constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
-    using Raw = typename Lanes<KIND>::Raw;
-    extern __shared__ __align__(16) unsigned char norm_smem[];
-    const int ranks = gridDim.x, rank = (int)cluster_rank(), t = threadIdx.x;
-    const Share s(p, L, rank);
-    const NormSmem m(norm_smem, p, RES ? 3 : 2, std::integral_constant<int, L>());
-    Raw *x = (Raw *)m.data, *dy = (Raw *)(m.data + p.data_bytes), *res = RES ? (Raw *)(m.data + 2 * (size_t)p.data_bytes) : x;
-    const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
-    cluster_arrive();
-    pdl_wait();
-    pdl_trigger();
-#pragma unroll 4
-    for (int i = 0; i < s.cnt; ++i) {
-        copy_in(x + i * NORM_T + t, (const Raw *)p.x + s.base + i * s.step);
-        copy_in(dy + i * NORM_T + t, (const Raw *)p.dy + s.base + i * s.step);
-        if (RES) copy_in(res + i * NORM_T + t, (const Raw *)p.res + s.base + i * s.step);
-    }
-    fetch_affine<L>(p, s, m.affine);
-    for (int q = t; q < s.sv * L; q += NORM_T) {
-        const float2 w = s.v0 * L + q < p.C ? __ldcg(stats + (s.v0 * L + q) / p.cpg) : make_float2(0.f, 0.f), k = m.affine[q];
-        m.constants[slot<L>(q, s.sv)] = make_float4(-w.x, w.y * k.x, k.y, 0.f);
-        m.channel[q].x = w.y;
-    }
-    __syncthreads();
-    Column<NP> k;
-    fill_column<KIND>(k, [&](int l) {
-        const float4 c = m.constants[l * s.sv + s.col];
-        return make_float3(c.x, c.y, c.z);
-    });
-    copy_wait();
-    GradientSums<NP> sums;
-#pragma unroll 2
-    for (int i = 0; i < s.cnt; ++i) {
-        f2 d[NP], dz[NP];
-        gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
-        sums.add(d, dz);
-    }
-    __syncthreads();                                           // (the constants make room for the sums)
-    if (s.r < s.rows) sums.template store<L>(m.v);
-    __syncthreads();
-    sum_rows<L, 2>(m.v, s.sv, s.rows, [&](int q, const float *w) {
-        const float2 c = make_float2(w[0], w[1] * m.channel[q].x);
-        p.part[((size_t)blockIdx.z * ranks + rank) * lanes + s.v0 * L + q] = c;
-        // rstd stays where it is; the sums, weighted, take the shift's and the scale's place
-        m.affine[q] = make_float2(m.affine[q].x * c.x, m.affine[q].x * c.y);
-    });
-    __syncthreads();
-    cluster_wait();
-    by_group(s.sg, p.cpg, [&](int g, int i, int team, int log2) {
-        const float2 *c = m.affine + (s.g0 + g) * p.cpg - s.v0 * L;
-        float s1 = 0.f, s2 = 0.f;
-        if (g < s.sg)
-            for (int j = i; j < p.cpg; j += team) {
-                s1 += c[j].x;
-                s2 += c[j].y;
-            }
-        s1 = sum_sharers(s1, log2);
-        s2 = sum_sharers(s2, log2);
-        if (g < s.sg && i < ranks) push_float2(m.inbox + rank * p.gs + g, i, make_float2(s1, s2));
-    });
-    cluster_arrive();
-    cluster_wait();
-    const float inv = 1.f / ((float)p.HW * (float)p.cpg);
-    over_ranks(m.inbox, p.gs, s.sg, ranks, [&](int g, float2 w) {
-        const float m1 = sum16(w.x) * inv, m2 = sum16(w.y) * inv;
-        if (g < s.sg && (t & 15) == 0) m.image[g] = make_float2(m1, m2);
-    });
-    __syncthreads();
-    for (int q = t; q < s.sv * L; q += NORM_T) {
-        const float2 w = s.v0 * L + q < p.C ? m.image[(s.v0 * L + q) / p.cpg - s.g0] : make_float2(0.f, 0.f);
-        const float rstd = m.channel[q].x;
-        ((float2 *)m.v)[slot<L>(q, s.sv)] = make_float2(-rstd * w.x, -rstd * rstd * w.y);
-    }
-    __syncthreads();
-    if (s.cnt > 0) {
-        f2 k0[NP], k1[NP];
-        fill_means<KIND>(k0, k1, [&](int l) { return ((const float2 *)m.v)[l * s.sv + s.col]; });
-#pragma unroll 2
-        for (int i = 0; i < s.cnt; ++i) {
-            f2 d[NP], dz[NP];
-            gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, (s.v0 + s.col) * L, x[i * NORM_T + t], dy[i * NORM_T + t], res[i * NORM_T + t], x + i * NORM_T + t, res + i * NORM_T + t, d, dz);
-            store_gradient<KIND>(p, k, k0, k1, d, dz, s.base + i * s.step);
-        }
-    }
-}
-
 // ------------------------------------------------------------------------------------------------------------- host
 
-// How the on-chip kernels share out an image; ranks == 0: they do not take it
+// How the on-chip kernel shares out an image; ranks == 0: it does not take it.
 struct NormCluster {
     int ranks = 0, gs = 0, slices = 0, per = 0, widest = 0;
     size_t data_bytes = 0, smem = 0;
 };
 
 constexpr size_t NORM_SMEM = 227 * 1024;
+constexpr int NORM_ON_CHIP = 12;          // pixels of a thread
 
-static NormCluster norm_cluster(int kind, int N, int HW, int C, int G, int tensors) {
+static NormCluster norm_cluster(int kind, int N, int HW, int C, int G) {
     NormCluster best;
-    const int L = kind == 0 ? 8 : kind == 1 ? 4 : 1, lanes = kind == 0 ? cprune_padded_channels(C) : C, pv = lanes / L, cpg = C / G;
+    const int L = L_of(kind), pv = (kind == 0 ? cprune_padded_channels(C) : C) / L, cpg = C / G;
     int granule = 1;                       // groups that begin at a vector's boundary
     while ((long long)granule * cpg % L) ++granule;
-    auto plan = [&](int gs, int ranks) {
+    double least = 1e30;
+    const int most = (G + granule - 1) / granule;
+    for (int part = 1; part <= 16 && (part == 1 || part / 2 < most); part *= 2) {
         NormCluster c;
-        int widest = 0;
-        for (int g0 = 0; g0 < G; g0 += gs) {
-            const int v1 = g0 + gs >= G ? pv : (g0 + gs) * cpg / L, sv = v1 - g0 * cpg / L;
-            widest = sv > widest ? sv : widest;
+        c.gs = (most + part - 1) / part * granule;
+        c.slices = (G + c.gs - 1) / c.gs;
+        const int last = pv - (int)((long long)(c.slices - 1) * c.gs * cpg / L), first = c.slices > 1 ? (int)((long long)c.gs * cpg / L) : last;
+        c.widest = first > last ? first : last;
+        if (c.widest > NORM_T) continue;
+        const int rows = NORM_T / c.widest;
+        for (c.ranks = 1; c.ranks <= 16; c.ranks *= 2) {
+            c.per = (HW + c.ranks - 1) / c.ranks;
+            const int pixels = (c.per + rows - 1) / rows;
+            const long long blocks = (long long)N * c.slices * c.ranks;
+            if (blocks > 2 * 148 && pixels <= NORM_ON_CHIP) break;
+            if (pixels > NORM_ON_CHIP || blocks > 2 * 148) continue;
+            c.data_bytes = (size_t)pixels * NORM_T * (kind == 2 ? 4 : 16);
+            c.smem = c.data_bytes + norm_sums_bytes(L, c.widest) + (size_t)c.gs * 8 * (c.ranks + 1) + (size_t)c.widest * L * 16;
+            const double cost = pixels * (1.0 + blocks / 592.0) + 0.05 * c.ranks;
+            if (c.smem <= NORM_SMEM / 2 - 1024 && cost < least) {
+                least = cost;
+                best = c;
+            }
         }
-        if (widest > NORM_T) return c;
-        c.widest = widest;
-        c.gs = gs;
-        c.slices = (G + gs - 1) / gs;
-        c.per = (HW + ranks - 1) / ranks;
-        const int rows = NORM_T / widest;
-        c.data_bytes = (size_t)((c.per + rows - 1) / rows) * NORM_T * (kind == 2 ? 4 : 16);
-        c.smem = c.data_bytes * tensors + norm_sums_bytes(L, widest) + (size_t)gs * 8 * (ranks + 1) + (size_t)widest * L * 16;
-        c.ranks = c.smem <= NORM_SMEM ? ranks : 0;
-        return c;
-    };
-    // the widest slices of whole granules that a block's threads span
-    int gs = (G + granule - 1) / granule * granule;
-    while (gs > granule && !plan(gs, 16).ranks) gs = (gs / granule + 1) / 2 * granule;
-    const size_t caps[3] = {72 * 1024, 110 * 1024, NORM_SMEM};
-    for (int k = 0; k < 3 && !best.ranks; ++k)
-        for (int ranks = 1; ranks <= 16; ranks *= 2) {
-            const NormCluster c = plan(gs, ranks);
-            if (c.ranks && c.smem <= caps[k]) { best = c; break; }
-        }
-    if (!best.ranks) return best;
-    // few images: more blocks, as long as each keeps two pixels a thread
-    while ((long long)N * best.slices * best.ranks < 148 && best.ranks < 16 && best.data_bytes > 2u * NORM_T * (kind == 2 ? 4 : 16)) {
-        const NormCluster c = plan(best.gs, best.ranks * 2);
-        if (!c.ranks) break;
-        best = c;
     }
-    if (best.slices > 65535) best.ranks = 0;
     return best;
 }
 
@@ -1131,7 +1045,7 @@ static cprune_status launch_pass(K kernel, dim3 grid, size_t smem, cudaStream_t 
 }
 
 template <typename K>
-static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaStream_t st, const NormParams &p, int lanes) {
+static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaStream_t st, const NormParams &p) {
     const cprune_status s = make_ready(kernel, true);
     if (s != CPRUNE_OK) return s;
     cudaLaunchConfig_t cfg = {};
@@ -1150,14 +1064,13 @@ static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaS
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.numAttrs = 2;
     }
-    if constexpr (std::is_invocable_v<K, NormParams, int>) CPRUNE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, p, lanes));
-    else CPRUNE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, p));
+    CPRUNE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, p));
     return CPRUNE_OK;
 }
 
 struct NormTiling {
     int lanes;          // per pixel
-    int sv, slices, rows, per, chunks;
+    int sv, slices, rows, chunks;
 };
 
 static int norm_kind(int type, int C, uintptr_t addresses) {
@@ -1186,15 +1099,13 @@ static NormTiling norm_tiling(int kind, int N, int HW, int C, int G) {
     while (readers < 32 && channels * readers * 2 <= NORM_T) readers *= 2;
     if (chunks > CHUNK_BATCH * readers) chunks = CHUNK_BATCH * readers;
     if (chunks < 1) chunks = 1;
-    t.per = (HW + (int)chunks - 1) / (int)chunks;
-    t.chunks = (HW + t.per - 1) / t.per;
+    t.chunks = (int)chunks;
     return t;
 }
 
-// (the on-chip kernels have one chunk to a rank)
 static size_t norm_part_bytes(int N, int HW, int C, int G, int kind) {
     const NormTiling t = norm_tiling(kind, N, HW, C, G);
-    return ((size_t)N * (t.chunks > 16 ? t.chunks : 16) * t.lanes * sizeof(float2) + 255) / 256 * 256;
+    return ((size_t)N * t.chunks * t.lanes * sizeof(float2) + 255) / 256 * 256;
 }
 
 constexpr int NORM_GROUP = 8192;          // channels of a group: the second pass holds two groups' results in shared memory
@@ -1227,7 +1138,7 @@ static NormParams norm_params(int kind, int N, int H, int W, int C, int groups, 
     p.N = N; p.HW = H * W; p.C = C; p.G = groups; p.cpg = C / groups; p.act = act;
     const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
     p.pv = t.lanes / (kind == 0 ? 8 : kind == 1 ? 4 : 1);
-    p.sv = t.sv; p.rows = t.rows; p.per = t.per; p.chunks = t.chunks;
+    p.sv = t.sv; p.rows = t.rows; p.chunks = t.chunks;
     const int touched = (t.sv * L_of(kind) + p.cpg - 1) / p.cpg + 1;
     p.range = round_up(touched < groups ? touched : groups, 2);             // (what lies behind stays on 16 bytes)
     const int channels = (touched < groups ? touched : groups) * p.cpg, own = t.sv * L_of(kind);
@@ -1266,13 +1177,13 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
     p.part = (float2 *)workspace;
     const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
     cudaStream_t st = (cudaStream_t)stream;
-    const NormCluster c = norm_cluster(kind, N, p.HW, C, groups, 1);
+    const NormCluster c = norm_cluster(kind, N, p.HW, C, groups);
     return by_kind(kind, act, residual != nullptr, [&](auto k, auto a, auto r) -> cprune_status {
         constexpr int K = decltype(k)::value, A = decltype(a)::value;
         constexpr bool R = decltype(r)::value;
         if (c.ranks) {
             p.gs = c.gs; p.sv = c.widest; p.per = c.per; p.data_bytes = (int)c.data_bytes;
-            return launch_cluster(norm_cluster_kernel<K, A, R>, c, N, st, p, t.lanes);
+            return launch_cluster(norm_cluster_kernel<K, A, R>, c, N, st, p);
         }
         const dim3 grid(t.chunks, t.slices, N);
         ChainScope chain;
@@ -1302,19 +1213,10 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
     p.part = (float2 *)workspace;
     const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
     cudaStream_t st = (cudaStream_t)stream;
-    const NormCluster c = norm_cluster(kind, N, p.HW, C, groups, residual ? 3 : 2);
     return by_kind(kind, act, residual != nullptr, [&](auto k, auto a, auto r) -> cprune_status {
         constexpr int K = decltype(k)::value, A = decltype(a)::value;
         constexpr bool R = decltype(r)::value;
         ChainScope chain;
-        if (c.ranks) {
-            p.gs = c.gs; p.sv = c.widest; p.per = c.per; p.data_bytes = (int)c.data_bytes; p.chunks = c.ranks;
-            const cprune_status e = launch_cluster(norm_grad_cluster_kernel<K, A, R>, c, N, st, p, t.lanes);
-            if (e != CPRUNE_OK || !(dgamma || dbeta)) return e;
-            chain.follow();
-            CPRUNE_CUDA_CHECK(launch_chained(norm_parameter_gradients_kernel, dim3((C + 31) / 32), dim3(NORM_T), 0, st, p, t.lanes));
-            return CPRUNE_OK;
-        }
         const dim3 grid(t.chunks, t.slices, N);
         p.ring_bytes = norm_ring_bytes(K, R + 2);
         const cprune_status e = launch_pass(norm_grad_partial_kernel<K, A, R>, grid, p.ring_bytes + (size_t)p.sv * L_of(K) * 16, st, p, t.lanes);

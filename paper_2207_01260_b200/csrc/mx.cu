@@ -141,30 +141,13 @@ __global__ void mx_pad_bias_kernel(const float *__restrict__ b, int n, int n_pad
 // takes the same 32 channels of its two rows: eight MMA steps, in an order of the channels that both sides share.
 // The tensor core truncates where it adds to an accumulator; four steps start from zero and are added to the running sum by a rounded
 // addition, and the warps' sums meet in float64.
-constexpr int MXF_WARPS = 8, MXF_NT = 2, MXF_AHEAD = 2;
-
-struct MxProduct {
-    const uint4 *codes;                    // weights [out][blocks] of 16 bytes
-    const uint8_t *scales;
-    const float *bias;
-    const __nv_bfloat16 *res;
-    void *y;
-    unsigned long long rows;
-    int blocks, tiles4, out, out_pad, act, out_is_f32;
-};
+constexpr int MXF_WARPS = 8, MXF_NT = 2, MXF_AHEAD = 2, MXF_ROWS = 32;
 
 // (one float32 of y, in its form)
 __device__ __forceinline__ void mx_store(const MxProduct &p, unsigned long long n, int o, float v) {
     if (p.out_is_f32) {
         if (o < p.out) ((float *)p.y)[n * p.out + o] = v;
     } else ((__nv_bfloat16 *)p.y)[n * p.out_pad + o] = __float2bfloat16_rn(o < p.out ? v : 0.f);
-}
-
-// relu and relu6 that keep a NaN
-__device__ __forceinline__ float mx_act(float v, int act) {
-    if (act == CPRUNE_ACT_NONE) return v;
-    v = v < 0.f ? 0.f : v;
-    return act == CPRUNE_ACT_RELU6 && v > 6.f ? 6.f : v;
 }
 
 __global__ void __launch_bounds__(MXF_WARPS * 32) mx_few_rows_kernel(const bf16x8 *__restrict__ x, const MxProduct p) {
@@ -326,9 +309,18 @@ cprune_status cprune_mx_pack(const float *w, const float *b, int out, int in, vo
     return CPRUNE_OK;
 }
 
+// Up to this many rows the weights are read by the kernel for few rows
+static MxTiling mx_product_tiling(size_t rows, int in, int out) {
+    MxTiling t = {};
+    return rows <= MXF_ROWS ? t : mx_tiling(rows, in, out);
+}
+static size_t mx_codes_bytes(size_t rows, int in) { return (rows * (size_t)mx_blocks(in) * 16 + 255) / 256 * 256; }
+
 size_t cprune_mx_fc_workspace_bytes(size_t rows, int in, int out) {
     if (rows == 0 || in <= 0 || out <= 0) return 0;
-    return rows * (size_t)mx_blocks(in) * MX_BLOCK * 2;
+    const MxTiling t = mx_product_tiling(rows, in, out);
+    if (!t.tensor) return rows * (size_t)mx_blocks(in) * MX_BLOCK * 2;
+    return t.round ? 16 : mx_codes_bytes(rows, in) + cprune_mx_scale_bytes(rows, in);
 }
 
 cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes, const void *scales, const float *b_packed, int out, int act, const void *residual,
@@ -336,13 +328,22 @@ cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes
     if (!x || !codes || !scales || !b_packed || !y || rows == 0 || in <= 0 || out <= 0 || act < CPRUNE_ACT_NONE || act > CPRUNE_ACT_RELU6) return CPRUNE_ERR_INVALID_ARG;
     if (((uintptr_t)x | (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)residual | (uintptr_t)workspace) & 15 || (uintptr_t)b_packed & 3) return CPRUNE_ERR_INVALID_ARG;
     if ((uintptr_t)y & (out_is_f32 ? 3 : 15)) return CPRUNE_ERR_INVALID_ARG;
-    if (rows > 16ull * 65535 || in > (1 << 24) || out > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
+    if (rows >> 31 || in > (1 << 24) || out > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < cprune_mx_fc_workspace_bytes(rows, in, out)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t st = (cudaStream_t)stream;
     MxProduct p = {};
     p.codes = (const uint4 *)codes; p.scales = (const uint8_t *)scales; p.bias = b_packed; p.res = (const __nv_bfloat16 *)residual; p.y = y; p.rows = rows;
     p.blocks = mx_blocks(in); p.tiles4 = (p.blocks + 3) / 4; p.out = out; p.out_pad = cprune_padded_channels(out); p.act = act; p.out_is_f32 = out_is_f32;
     ChainScope chain;
+    const MxTiling t = mx_product_tiling(rows, in, out);
+    if (t.tensor && t.round) return launch_mx_product(p, t, x, nullptr, in, st);
+    if (t.tensor) {
+        uint8_t *xscales = (uint8_t *)workspace + mx_codes_bytes(rows, in);
+        CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 0>, dim3(mx_grid(rows * p.tiles4, MX_T / 16)), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
+                                         cprune_padded_channels(in), p.tiles4, (uint32_t *)workspace, xscales, (void *)nullptr));
+        chain.follow();
+        return launch_mx_product(p, t, workspace, xscales, in, st);
+    }
     CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 1>, dim3(mx_grid(rows * p.tiles4, MX_T / 16)), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
                                      cprune_padded_channels(in), p.tiles4, (uint32_t *)nullptr, (uint8_t *)nullptr, workspace));
     chain.follow();

@@ -62,4 +62,30 @@ __device__ __forceinline__ void mx_values(uint32_t w, float scale, float *f) {
     }
 }
 
+struct MxProduct {
+    const uint4 *codes;                    // weights [out][blocks] of 16 bytes
+    const uint8_t *scales;
+    const float *bias;
+    const __nv_bfloat16 *res;
+    void *y;
+    unsigned long long rows;
+    int blocks, tiles4, out, out_pad, act, out_is_f32;
+};
+
+// relu and relu6 that keep a NaN
+__device__ __forceinline__ float mx_act(float v, int act) {
+    if (act == CPRUNE_ACT_NONE) return v;
+    v = v < 0.f ? 0.f : v;
+    return act == CPRUNE_ACT_RELU6 && v > 6.f ? 6.f : v;
+}
+
+// How a product is shared out (mx_product.cu); tensor == 0: the kernel for few rows takes it
+struct MxTiling {
+    int tensor;
+    int nt, subs, tiles_n;                 // features of a block, in parts of 128; blocks along the features
+    int round;                             // the rows are rounded by the product itself
+};
+MxTiling mx_tiling(unsigned long long rows, int in, int out);
+cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const void *x, const uint8_t *xscales, int in, cudaStream_t st);
+
 }  // namespace cprune

@@ -237,7 +237,7 @@ def test_refusals(cp):
     assert fc(x=0x1008) == 1 and fc(codes=0x2008) == 1 and fc(scales=0x3008) == 1 and fc(res=0x7008) == 1 and fc(y=0x5008) == 1 and fc(f32=1, y=0x5002) == 1
     assert fc(b=0x4002) == 1 and fc(work=0x6008) == 1
     assert fc(work=None) == 3 and fc(size=8) == 3
-    assert fc(rows=1 << 20) == 2 and fc(inn=(1 << 24) + 1) == 2 and fc(out=(1 << 24) + 1) == 2
+    assert fc(rows=1 << 31) == 2 and fc(inn=(1 << 24) + 1) == 2 and fc(out=(1 << 24) + 1) == 2
 
 
 def test_python_refusals(cp):

@@ -259,7 +259,7 @@ cprune_status cprune_fc(const void *x, int N, int in, const void *w_packed, cons
  *   groups    divides C; C / groups may be any number (a pruned layer's channels need not fill vectors)
  *   gamma, beta  float32 [C] or NULL (ones, zeros);   residual  as x, or NULL;   eps > 0
  *   y         may be x or residual;   stats  float32 [N][groups][2], written: mean and rstd, which the gradients need
- *   workspace cprune_group_norm_workspace_bytes (never 0 for arguments that are in order), 16-byte aligned
+ *   workspace cprune_group_norm_workspace_bytes, 16-byte aligned (0: none is needed, or the arguments are not in order)
  * A NaN in a group, or an infinity, makes its outputs NaN; the activations hand a NaN on.  Other groups keep their values.
  *
  * Gradients, given dy = dL/dy and the stats of the forward pass: dx, dgamma [C], dbeta [C] (either may be NULL) and

@@ -3,6 +3,9 @@ buffers (``data_ptr``) and for their stream handles.  No arithmetic happens in t
 from __future__ import annotations
 
 import ctypes
+import functools
+import math
+import operator
 import os
 from array import array
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, c_void_p
@@ -478,49 +481,70 @@ def cprune_fc(x, in_features, w_packed, b_packed, out_features, activation="none
 
 # The operators below check what they are given before they hand addresses on: a tensor of another type, shape or device would be read out of
 # bounds.  What they allocate belongs to the stream that they run on, so that a workspace is not handed out again while it is in use there.
+# The checks are most of what a small call costs on the host, and are written for that: a tensor that is in order passes one expression,
+# what depends on sizes alone is remembered by sizes.
 TYPE = {torch.bfloat16: 0, torch.float32: 1}
+_BF16, _F32, _U8 = torch.bfloat16, torch.float32, torch.uint8
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_SIZES = 4096                              # sizes remembered
 
 
 def _refuse(where, why):
     raise CpruneError(1, where, why)
 
 
-def _checked(where, name, t, shape, dtype, device=None):
+def _current_device():
+    return _device() if torch.cuda.is_initialized() else -2        # (no tensor is on it)
+
+
+def _checked(where, name, t, shape, dtype, device):
     """`t`'s address; refuses anything but a contiguous tensor of this shape and type on the current device."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        _refuse(where, "%s has to be a contiguous %s tensor of shape %s" % (name, dtype, tuple(shape)))
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device:
+        return t.data_ptr()
+    if t.get_device() != device:
         _refuse(where, "%s is not on the current device" % name)
-    return t.data_ptr()
+    _refuse(where, "%s has to be a contiguous %s tensor of shape %s" % (name, dtype, tuple(shape)))
 
 
-def _empty(stream, shape, dtype, device):
+def _empty(stream, shape, dtype, like):
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _norm_input(where, x, C, groups, activation):
-    """(type, N, H, W, lanes) of an activation [N, H, W, lanes]."""
-    if x.dtype not in TYPE or x.dim() != 4 or C < 1:
+def _empty_like(stream, t):
+    if stream is None:
+        return torch.empty_like(t)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t)
+
+
+def _workspace(where, workspace, need, stream, device, like):
+    """(address, bytes) of a workspace, and the tensor that keeps it."""
+    if workspace is None:
+        if not need:
+            return None, 0, None
+        workspace = _empty(stream, need, _U8, like)
+    else:
+        _checked(where, "workspace", workspace, (workspace.numel(),), _U8, device)
+    return workspace.data_ptr(), workspace.numel(), workspace
+
+
+@functools.lru_cache(_SIZES)
+def _norm_geometry(where, dtype, shape, C, groups, activation, backward):
+    """((type, N, H, W), activation's number, bytes of workspace) for an activation [N, H, W, lanes]."""
+    if dtype not in TYPE or len(shape) != 4 or C < 1:
         _refuse(where, "x has to be a bf16 or float32 tensor [N, H, W, channels in memory]")
-    lanes = cprune_padded_channels(C) if x.dtype == torch.bfloat16 else C
-    if x.shape[3] != lanes:
-        _refuse(where, "x has %d channels in memory; %d channels take %d" % (x.shape[3], C, lanes))
+    lanes = cprune_padded_channels(C) if dtype == _BF16 else C
+    if shape[3] != lanes:
+        _refuse(where, "x has %d channels in memory; %d channels take %d" % (shape[3], C, lanes))
     if activation not in NORM_ACT:
         _refuse(where, "unknown activation %r" % (activation,))
-    return (TYPE[x.dtype],) + tuple(x.shape[:3])
-
-
-def _norm_workspace(where, geometry, C, groups, backward, workspace, stream, device):
-    need = lib().cprune_group_norm_workspace_bytes(*geometry, C, groups, backward)
-    if workspace is None:
-        return _empty(stream, (need,), torch.uint8, device)
-    _checked(where, "workspace", workspace, (workspace.numel(),), torch.uint8)
-    return workspace
+    geometry = (TYPE[dtype],) + tuple(shape[:3])
+    return geometry, NORM_ACT[activation], lib().cprune_group_norm_workspace_bytes(*geometry, C, groups, backward)
 
 
 def cprune_group_norm(x, C, groups, gamma=None, beta=None, eps=1e-5, activation="none", residual=None, y=None, stats=None, workspace=None, stream=None):
@@ -528,17 +552,20 @@ def cprune_group_norm(x, C, groups, gamma=None, beta=None, eps=1e-5, activation=
     and shift (float32 [C]), a tensor added to it and an activation (none, relu, relu6, silu).  Returns (y, stats); stats, float32
     [N, groups, 2], holds mean and 1 / sqrt(variance + eps) for cprune_group_norm_backward.  y may be x."""
     where = "cprune_group_norm"
-    geometry = _norm_input(where, x, C, groups, activation)
-    px, pr = _checked(where, "x", x, x.shape, x.dtype), _checked(where, "residual", residual, x.shape, x.dtype)
-    pg, pb = _checked(where, "gamma", gamma, (C,), torch.float32), _checked(where, "beta", beta, (C,), torch.float32)
+    dtype, shape, dev = x.dtype, x.shape, _current_device()
+    geometry, act, need = _norm_geometry(where, dtype, shape, C, groups, activation, 0)
+    px, pr = _checked(where, "x", x, shape, dtype, dev), _checked(where, "residual", residual, shape, dtype, dev)
+    pg, pb = _checked(where, "gamma", gamma, (C,), _F32, dev), _checked(where, "beta", beta, (C,), _F32, dev)
     if y is None:
-        y = _empty(stream, x.shape, x.dtype, x.device)
+        y = _empty_like(stream, x)
+    elif y is not x:
+        _checked(where, "y", y, shape, dtype, dev)
     if stats is None:
-        stats = _empty(stream, (x.shape[0], max(groups, 0), 2), torch.float32, x.device)
-    workspace = _norm_workspace(where, geometry, C, groups, 0, workspace, stream, x.device)
-    _check(lib().cprune_group_norm(px, *geometry, C, groups, pg, pb, eps, NORM_ACT[activation], pr, _checked(where, "y", y, x.shape, x.dtype),
-                                   _checked(where, "stats", stats, (x.shape[0], groups, 2), torch.float32), workspace.data_ptr(), workspace.numel(),
-                                   _stream(stream)), where)
+        stats = _empty(stream, (shape[0], max(groups, 0), 2), _F32, x)
+    else:
+        _checked(where, "stats", stats, (shape[0], groups, 2), _F32, dev)
+    pw, size, workspace = _workspace(where, workspace, need, stream, dev, x)
+    _check(_lib.cprune_group_norm(px, *geometry, C, groups, pg, pb, eps, act, pr, y.data_ptr(), stats.data_ptr(), pw, size, _stream(stream)), where)
     return y, stats
 
 
@@ -547,90 +574,104 @@ def cprune_group_norm_backward(dy, x, C, groups, stats, gamma=None, beta=None, a
     """Gradients of cprune_group_norm's y, given dy and the stats of the forward pass.  Returns (dx, dgamma, dbeta, dresidual); dresidual is None
     where there is no residual."""
     where = "cprune_group_norm_backward"
-    geometry = _norm_input(where, x, C, groups, activation)
-    px, pr, pdy = (_checked(where, n, t, x.shape, x.dtype) for n, t in (("x", x), ("residual", residual), ("dy", dy)))
-    pg, pb = _checked(where, "gamma", gamma, (C,), torch.float32), _checked(where, "beta", beta, (C,), torch.float32)
-    ps = _checked(where, "stats", stats, (x.shape[0], groups, 2), torch.float32)
+    dtype, shape, dev = x.dtype, x.shape, _current_device()
+    geometry, act, need = _norm_geometry(where, dtype, shape, C, groups, activation, 1)
+    px, pr, pdy = _checked(where, "x", x, shape, dtype, dev), _checked(where, "residual", residual, shape, dtype, dev), _checked(where, "dy", dy, shape, dtype, dev)
+    pg, pb = _checked(where, "gamma", gamma, (C,), _F32, dev), _checked(where, "beta", beta, (C,), _F32, dev)
+    ps = _checked(where, "stats", stats, (shape[0], groups, 2), _F32, dev)
     if dx is None:
-        dx = _empty(stream, x.shape, x.dtype, x.device)
+        dx = _empty_like(stream, x)
+    else:
+        _checked(where, "dx", dx, shape, dtype, dev)
     if dgamma is None:
-        dgamma = _empty(stream, (C,), torch.float32, x.device)
+        dgamma = _empty(stream, C, _F32, x)
+    else:
+        _checked(where, "dgamma", dgamma, (C,), _F32, dev)
     if dbeta is None:
-        dbeta = _empty(stream, (C,), torch.float32, x.device)
-    if dresidual is None and residual is not None:
-        dresidual = _empty(stream, x.shape, x.dtype, x.device)
-    workspace = _norm_workspace(where, geometry, C, groups, 1, workspace, stream, x.device)
-    _check(lib().cprune_group_norm_backward(pdy, px, *geometry, C, groups, ps, pg, pb, NORM_ACT[activation], pr, _checked(where, "dx", dx, x.shape, x.dtype),
-                                            _checked(where, "dgamma", dgamma, (C,), torch.float32), _checked(where, "dbeta", dbeta, (C,), torch.float32),
-                                            _checked(where, "dresidual", dresidual, x.shape, x.dtype), workspace.data_ptr(), workspace.numel(),
-                                            _stream(stream)), where)
+        dbeta = _empty(stream, C, _F32, x)
+    else:
+        _checked(where, "dbeta", dbeta, (C,), _F32, dev)
+    if dresidual is not None:
+        _checked(where, "dresidual", dresidual, shape, dtype, dev)
+    elif residual is not None:
+        dresidual = _empty_like(stream, x)
+    pw, size, workspace = _workspace(where, workspace, need, stream, dev, x)
+    _check(_lib.cprune_group_norm_backward(pdy, px, *geometry, C, groups, ps, pg, pb, act, pr, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _ptr(dresidual),
+                                           pw, size, _stream(stream)), where)
     return dx, dgamma, dbeta, dresidual
 
 
-def _gradient_list(where, tensors):
+_dtype_of = operator.attrgetter("dtype")
+
+
+def _gradient_list(where, tensors, device):
     """(addresses, counts, types) of a list of tensors, as arrays that the library reads."""
-    device = torch.cuda.current_device() if tensors else None
-    addresses, counts, types = array("Q"), array("Q"), array("i")
-    for t in tensors:
-        if t.dtype not in TYPE or not t.is_contiguous():
-            _refuse(where, "gradients have to be contiguous bf16 or float32 tensors")
-        if t.get_device() != device:
-            _refuse(where, "a gradient is not on the current device")
-        addresses.append(t.data_ptr())
-        counts.append(t.numel())
-        types.append(TYPE[t.dtype])
-    there = [a for a, n in zip(addresses, counts) if n]
-    if len(set(there)) != len(there):
-        _refuse(where, "a tensor is in the list twice")
-    return addresses, counts, types
+    dtypes = set(map(_dtype_of, tensors))
+    if not dtypes <= TYPE.keys() or not all(map(torch.Tensor.is_contiguous, tensors)):
+        _refuse(where, "gradients have to be contiguous bf16 or float32 tensors")
+    if not set(map(torch.Tensor.get_device, tensors)) <= {device}:
+        _refuse(where, "a gradient is not on the current device")
+    addresses, counts = list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors))
+    if len(set(addresses)) != len(addresses):
+        there = [a for a, n in zip(addresses, counts) if n]
+        if len(set(there)) != len(there):
+            _refuse(where, "a tensor is in the list twice")
+    types = array("i", [TYPE[next(iter(dtypes))]]) * len(counts) if len(dtypes) == 1 else array("i", [TYPE[t.dtype] for t in tensors])
+    return array("Q", addresses), array("Q", counts), types
 
 
-def _gradient_buffers(n, norm, workspace, where, stream):
-    if norm is None:
-        norm = _empty(stream, (1,), torch.float32, torch.device("cuda", torch.cuda.current_device()))
-    else:
-        _checked(where, "norm", norm, (1,), torch.float32)
-    if workspace is None:
-        workspace = _empty(stream, (lib().cprune_gradient_workspace_bytes(n),), torch.uint8, norm.device)
-    else:
-        _checked(where, "workspace", workspace, (workspace.numel(),), torch.uint8)
-    return norm, workspace
+def _norm_buffer(where, norm, stream, device):
+    if norm is not None:
+        _checked(where, "norm", norm, (1,), _F32, device)
+        return norm
+    with torch.cuda.stream(stream):            # (None: no other than the current one)
+        return torch.empty(1, dtype=_F32, device=device)
+
+
+@functools.lru_cache(_SIZES)
+def _gradient_bytes(n):
+    return lib().cprune_gradient_workspace_bytes(n)
 
 
 def cprune_gradient_norm(grads, norm=None, workspace=None, stream=None):
     """The global 2-norm of a list of contiguous bf16 or float32 tensors, as a float32 tensor [1]."""
     where = "cprune_gradient_norm"
-    a, c, t = _gradient_list(where, grads)
-    norm, workspace = _gradient_buffers(len(a), norm, workspace, where, stream)
-    _check(lib().cprune_gradient_norm(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                      _stream(stream)), where)
+    dev = torch.cuda.current_device()
+    a, c, t = _gradient_list(where, grads, dev)
+    norm = _norm_buffer(where, norm, stream, dev)
+    pw, size, workspace = _workspace(where, workspace, _gradient_bytes(len(a)), stream, dev, norm)
+    _check(_lib.cprune_gradient_norm(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), norm.data_ptr(), pw, size, _stream(stream)), where)
     return norm
 
 
 def cprune_clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """Scales the gradients, a list of contiguous bf16 or float32 tensors, by min(1, max_norm / (norm + 1e-6)) with their global 2-norm: in place, or
-    into the tensors of `out` (same shapes and types).  Returns the norm before, a float32 tensor [1]."""
+    into the tensors of `out` (same sizes and types).  Returns the norm before, a float32 tensor [1]."""
     where = "cprune_clip_gradients"
-    a, c, t = _gradient_list(where, grads)
+    dev = torch.cuda.current_device()
+    a, c, t = _gradient_list(where, grads, dev)
     o = None
     if out is not None:
-        o, oc, ot = _gradient_list(where, out)
+        o, oc, ot = _gradient_list(where, out, dev)
         if oc != c or ot != t:
             _refuse(where, "out has to have the gradients' sizes and types")
-    norm, workspace = _gradient_buffers(len(a), norm, workspace, where, stream)
-    _check(lib().cprune_clip_gradients(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), max_norm, None if o is None else o.buffer_info()[0],
-                                       norm.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(stream)), where)
+    norm = _norm_buffer(where, norm, stream, dev)
+    pw, size, workspace = _workspace(where, workspace, _gradient_bytes(len(a)), stream, dev, norm)
+    _check(_lib.cprune_clip_gradients(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), max_norm, None if o is None else o.buffer_info()[0],
+                                      norm.data_ptr(), pw, size, _stream(stream)), where)
     return norm
 
 
-def _mx_rows(where, x, C):
-    """(rows, type) of x, a tensor [..., channels in memory]."""
-    if x.dtype not in TYPE or x.dim() < 1 or C < 1:
+@functools.lru_cache(_SIZES)
+def _mx_geometry(where, dtype, shape, C):
+    """(rows, type, shape of the codes, of the scales) of a tensor [..., channels in memory]."""
+    if dtype not in TYPE or len(shape) < 1 or C < 1:
         _refuse(where, "x has to be a bf16 or float32 tensor [..., channels in memory]")
-    lanes = cprune_padded_channels(C) if x.dtype == torch.bfloat16 else C
-    if x.shape[-1] != lanes:
-        _refuse(where, "x has %d channels in memory; %d channels take %d" % (x.shape[-1], C, lanes))
-    return x.numel() // lanes, TYPE[x.dtype]
+    lanes = cprune_padded_channels(C) if dtype == _BF16 else C
+    if shape[-1] != lanes:
+        _refuse(where, "x has %d channels in memory; %d channels take %d" % (shape[-1], C, lanes))
+    rows = math.prod(shape[:-1])
+    return (rows, TYPE[dtype]) + _mx_shapes(rows, C)
 
 
 def _mx_shapes(rows, C):
@@ -644,16 +685,24 @@ def cprune_mx_quantize(x, C, codes=None, scales=None, values=False, stream=None)
     [rows / 128, blocks / 4, 32, 4, 4], values): values is None, or with values=True (or a tensor like x, which may be x) what the codes
     stand for, in the form of x."""
     where = "cprune_mx_quantize"
-    rows, typ = _mx_rows(where, x, C)
-    shape_c, shape_s = _mx_shapes(rows, C)
-    px = _checked(where, "x", x, x.shape, x.dtype)
+    dtype, shape, dev = x.dtype, x.shape, _current_device()
+    rows, typ, shape_c, shape_s = _mx_geometry(where, dtype, shape, C)
+    px = _checked(where, "x", x, shape, dtype, dev)
     if codes is None:
-        codes = _empty(stream, shape_c, torch.uint8, x.device)
+        codes = _empty(stream, shape_c, _U8, x)
+    else:
+        _checked(where, "codes", codes, shape_c, _U8, dev)
     if scales is None:
-        scales = _empty(stream, shape_s, torch.uint8, x.device)
-    values = None if values is False else _empty(stream, x.shape, x.dtype, x.device) if values is True else values
-    _check(lib().cprune_mx_quantize(px, typ, rows, C, _checked(where, "codes", codes, shape_c, torch.uint8), _checked(where, "scales", scales, shape_s, torch.uint8),
-                                    _checked(where, "values", values, x.shape, x.dtype), _stream(stream)), where)
+        scales = _empty(stream, shape_s, _U8, x)
+    else:
+        _checked(where, "scales", scales, shape_s, _U8, dev)
+    if values is True:
+        values = _empty_like(stream, x)
+    elif values is False:
+        values = None
+    else:
+        _checked(where, "values", values, shape, dtype, dev)
+    _check(lib().cprune_mx_quantize(px, typ, rows, C, codes.data_ptr(), scales.data_ptr(), _ptr(values), _stream(stream)), where)
     return codes, scales, values
 
 
@@ -662,10 +711,10 @@ def cprune_mx_dequantize(codes, scales, C, dtype=torch.float32, stream=None):
     where = "cprune_mx_dequantize"
     if dtype not in TYPE or codes.dim() != 2 or C < 1:
         _refuse(where, "codes have to be a tensor [rows, blocks * 16], dtype bf16 or float32")
-    rows = codes.shape[0]
+    rows, dev = codes.shape[0], _current_device()
     shape_c, shape_s = _mx_shapes(rows, C)
-    pc, ps = _checked(where, "codes", codes, shape_c, torch.uint8), _checked(where, "scales", scales, shape_s, torch.uint8)
-    values = _empty(stream, (rows, cprune_padded_channels(C) if dtype == torch.bfloat16 else C), dtype, codes.device)
+    pc, ps = _checked(where, "codes", codes, shape_c, _U8, dev), _checked(where, "scales", scales, shape_s, _U8, dev)
+    values = _empty(stream, (rows, cprune_padded_channels(C) if dtype == _BF16 else C), dtype, codes)
     _check(lib().cprune_mx_dequantize(pc, ps, rows, C, TYPE[dtype], values.data_ptr(), _stream(stream)), where)
     return values
 
@@ -674,40 +723,49 @@ def cprune_mx_pack(w, b=None, stream=None):
     """Weights float32 [out, in] (or the filters [out, in, 1, 1] of a 1x1 layer) and biases -> (codes, scales, bias padded to the channels in memory)
     for cprune_mx_fc."""
     where = "cprune_mx_pack"
-    if w.dim() not in (2, 4) or w[0].numel() != w.shape[1]:
+    if w.dim() not in (2, 4) or w.numel() != w.shape[0] * w.shape[1]:
         _refuse(where, "w has to be [out, in] or [out, in, 1, 1]")
-    out, inn = w.shape[:2]
-    pw, pb = _checked(where, "w", w, w.shape, torch.float32), _checked(where, "b", b, (out,), torch.float32)
+    (out, inn), dev = w.shape[:2], _current_device()
+    pw, pb = _checked(where, "w", w, w.shape, _F32, dev), _checked(where, "b", b, (out,), _F32, dev)
     shape_c, shape_s = _mx_shapes(out, inn)
-    codes, scales = _empty(stream, shape_c, torch.uint8, w.device), _empty(stream, shape_s, torch.uint8, w.device)
-    bp = _empty(stream, (cprune_padded_channels(out),), torch.float32, w.device)
+    codes, scales = _empty(stream, shape_c, _U8, w), _empty(stream, shape_s, _U8, w)
+    bp = _empty(stream, cprune_padded_channels(out), _F32, w)
     _check(lib().cprune_mx_pack(pw, pb, out, inn, codes.data_ptr(), scales.data_ptr(), bp.data_ptr(), _stream(stream)), where)
     return codes, scales, bp
+
+
+@functools.lru_cache(_SIZES)
+def _mx_fc_geometry(where, dtype, shape, in_features, out_features, activation, out_f32):
+    """(rows, shapes of codes, scales, bias and residual, of y, its type, activation's number, bytes of workspace)"""
+    if dtype != _BF16:
+        _refuse(where, "x has to be bf16")
+    if activation not in ACT:
+        _refuse(where, "unknown activation %r" % (activation,))
+    if out_features < 1:
+        _refuse(where, "no output features")
+    rows = _mx_geometry(where, dtype, shape, in_features)[0]
+    out_pad = cprune_padded_channels(out_features)
+    shape_c, shape_s = _mx_shapes(out_features, in_features)
+    lead = tuple(shape[:-1])
+    return (rows, shape_c, shape_s, (out_pad,), lead + (out_pad,), lead + (out_features if out_f32 else out_pad,), _F32 if out_f32 else _BF16, ACT[activation],
+            lib().cprune_mx_fc_workspace_bytes(rows, in_features, out_features))
 
 
 def cprune_mx_fc(x, in_features, codes, scales, b_packed, out_features, activation="none", residual=None, out_f32=False, y=None, workspace=None, stream=None):
     """act(q(x) W^T + b + residual): x bf16 [..., in_pad], a row per image or pixel, rounded to MXFP4 on the way in; W and b from cprune_mx_pack;
     residual bf16 [..., out_pad].  Returns y, bf16 [..., out_pad] or float32 [..., out_features]; y may be residual."""
     where = "cprune_mx_fc"
-    if x.dtype != torch.bfloat16:
-        _refuse(where, "x has to be bf16")
-    if activation not in ACT:
-        _refuse(where, "unknown activation %r" % (activation,))
-    if out_features < 1:
-        _refuse(where, "no output features")
-    rows, _ = _mx_rows(where, x, in_features)
-    out_pad = cprune_padded_channels(out_features)
-    shape_c, shape_s = _mx_shapes(out_features, in_features)
-    px = _checked(where, "x", x, x.shape, torch.bfloat16)
-    pc, ps = _checked(where, "codes", codes, shape_c, torch.uint8), _checked(where, "scales", scales, shape_s, torch.uint8)
-    pb, pr = _checked(where, "b_packed", b_packed, (out_pad,), torch.float32), _checked(where, "residual", residual, x.shape[:-1] + (out_pad,), torch.bfloat16)
-    shape, dtype = (x.shape[:-1] + (out_features,), torch.float32) if out_f32 else (x.shape[:-1] + (out_pad,), torch.bfloat16)
+    shape, dev = x.shape, _current_device()
+    rows, shape_c, shape_s, shape_b, shape_r, shape_y, dtype, act, need = _mx_fc_geometry(where, x.dtype, shape, in_features, out_features, activation, bool(out_f32))
+    px = _checked(where, "x", x, shape, _BF16, dev)
+    pc, ps = _checked(where, "codes", codes, shape_c, _U8, dev), _checked(where, "scales", scales, shape_s, _U8, dev)
+    pb, pr = _checked(where, "b_packed", b_packed, shape_b, _F32, dev), _checked(where, "residual", residual, shape_r, _BF16, dev)
     if y is None:
-        y = _empty(stream, shape, dtype, x.device)
-    if workspace is None:
-        workspace = _empty(stream, (lib().cprune_mx_fc_workspace_bytes(rows, in_features, out_features),), torch.uint8, x.device)
-    _check(lib().cprune_mx_fc(px, rows, in_features, pc, ps, pb, out_features, ACT[activation], pr, 1 if out_f32 else 0, _checked(where, "y", y, shape, dtype),
-                              _checked(where, "workspace", workspace, (workspace.numel(),), torch.uint8), workspace.numel(), _stream(stream)), where)
+        y = _empty(stream, shape_y, dtype, x)
+    else:
+        _checked(where, "y", y, shape_y, dtype, dev)
+    pw, size, workspace = _workspace(where, workspace, need, stream, dev, x)
+    _check(_lib.cprune_mx_fc(px, rows, in_features, pc, ps, pb, out_features, act, pr, 1 if out_f32 else 0, y.data_ptr(), pw, size, _stream(stream)), where)
     return y
 
 

@@ -649,13 +649,14 @@ template <int NP> struct GradientSums {
     }
 };
 
-// Constants of the slice's channels from global memory: -mean, rstd gamma, beta, rstd
+// Constants of the slice's channels from global memory: -mean, rstd gamma, beta, rstd.  Lanes behind the last channel get z = 1, far from the borders of
+// relu and relu6; everything else about them is 0.
 template <int L>
 __device__ __forceinline__ void fetch_constants(const NormParams &p, const Chunk &c, float4 *constants) {
     const float2 *stats = (const float2 *)p.stats + (size_t)blockIdx.z * p.G;
     for (int q = threadIdx.x; q < c.sv * L; q += NORM_T) {
         const int ch = c.v0 * L + q;
-        float4 k = make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 k = make_float4(0.f, 0.f, 1.f, 0.f);
         if (ch < p.C) {
             const float2 w = __ldcg(stats + ch / p.cpg);
             k = make_float4(-w.x, w.y * (p.gamma ? __ldg(p.gamma + ch) : 1.f), p.beta ? __ldg(p.beta + ch) : 0.f, w.y);
@@ -1157,6 +1158,7 @@ size_t cprune_group_norm_workspace_bytes(int type, int N, int H, int W, int C, i
     size_t most = 0;
     for (int kind = type == CPRUNE_TYPE_BF16 ? 0 : 1; kind <= (type == CPRUNE_TYPE_BF16 ? 0 : 2); ++kind) {
         if (kind == 1 && C % 4) continue;
+        if (!backward && norm_cluster(kind, N, H * W, C, groups).ranks) continue;
         const size_t b = norm_part_bytes(N, H * W, C, groups, kind);
         most = b > most ? b : most;
     }
@@ -1171,13 +1173,13 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
     const uintptr_t tensors = (uintptr_t)x | (uintptr_t)y | (uintptr_t)residual;
     if (tensors & (type == CPRUNE_TYPE_BF16 ? 15 : 3) || ((uintptr_t)gamma | (uintptr_t)beta) & 3 || (uintptr_t)stats & 7 || (uintptr_t)workspace & 15) return CPRUNE_ERR_INVALID_ARG;
     const int kind = norm_kind(type, C, tensors);
-    if (workspace_bytes < norm_part_bytes(N, H * W, C, groups, kind) || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    const NormCluster c = norm_cluster(kind, N, H * W, C, groups);
+    if (!c.ranks && (workspace_bytes < norm_part_bytes(N, H * W, C, groups, kind) || !workspace)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
     NormParams p = norm_params(kind, N, H, W, C, groups, act);
     p.x = x; p.res = residual; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats; p.eps = eps;
     p.part = (float2 *)workspace;
     const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
     cudaStream_t st = (cudaStream_t)stream;
-    const NormCluster c = norm_cluster(kind, N, p.HW, C, groups);
     return by_kind(kind, act, residual != nullptr, [&](auto k, auto a, auto r) -> cprune_status {
         constexpr int K = decltype(k)::value, A = decltype(a)::value;
         constexpr bool R = decltype(r)::value;

@@ -320,7 +320,7 @@ size_t cprune_mx_fc_workspace_bytes(size_t rows, int in, int out) {
     if (rows == 0 || in <= 0 || out <= 0) return 0;
     const MxTiling t = mx_product_tiling(rows, in, out);
     if (!t.tensor) return rows * (size_t)mx_blocks(in) * MX_BLOCK * 2;
-    return t.round ? 16 : mx_codes_bytes(rows, in) + cprune_mx_scale_bytes(rows, in);
+    return t.round ? 0 : mx_codes_bytes(rows, in) + cprune_mx_scale_bytes(rows, in);
 }
 
 cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes, const void *scales, const float *b_packed, int out, int act, const void *residual,
@@ -329,7 +329,8 @@ cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes
     if (((uintptr_t)x | (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)residual | (uintptr_t)workspace) & 15 || (uintptr_t)b_packed & 3) return CPRUNE_ERR_INVALID_ARG;
     if ((uintptr_t)y & (out_is_f32 ? 3 : 15)) return CPRUNE_ERR_INVALID_ARG;
     if (rows >> 31 || in > (1 << 24) || out > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
-    if (!workspace || workspace_bytes < cprune_mx_fc_workspace_bytes(rows, in, out)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = cprune_mx_fc_workspace_bytes(rows, in, out);
+    if (need && (!workspace || workspace_bytes < need)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t st = (cudaStream_t)stream;
     MxProduct p = {};
     p.codes = (const uint4 *)codes; p.scales = (const uint8_t *)scales; p.bias = b_packed; p.res = (const __nv_bfloat16 *)residual; p.y = y; p.rows = rows;

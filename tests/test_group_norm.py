@@ -256,10 +256,10 @@ def test_more_than_32_bits_of_bytes(cp):
 def test_refusals(cp):
     L, vp = cp.lib(), ctypes.c_void_p
     ws = cp.lib().cprune_group_norm_workspace_bytes
-    assert ws(0, 2, 7, 7, 24, 3, 0) > 0 and ws(0, 2, 7, 7, 24, 3, 1) > ws(0, 2, 7, 7, 24, 3, 0)
+    assert ws(0, 2, 7, 7, 24, 3, 1) > 0 and ws(0, 64, 112, 112, 24, 3, 0) > 0 and ws(0, 2, 7, 7, 24, 3, 0) == 0      # (a small forward pass stays on chip)
     assert ws(0, 2, 7, 7, 24, 5, 0) == 0 and ws(2, 2, 7, 7, 24, 3, 0) == 0 and ws(0, 0, 7, 7, 24, 3, 0) == 0
 
-    def forward(x=0x1000, type=0, N=2, H=7, W=7, C=24, G=3, gamma=0x2000, beta=0x2000, eps=1e-5, act=1, res=None, y=0x3000, stats=0x4000, work=0x5000, size=1 << 20):
+    def forward(x=0x1000, type=0, N=64, H=112, W=112, C=24, G=3, gamma=0x2000, beta=0x2000, eps=1e-5, act=1, res=None, y=0x3000, stats=0x4000, work=0x5000, size=1 << 20):
         return L.cprune_group_norm(vp(x), type, N, H, W, C, G, vp(gamma), vp(beta), eps, act, vp(res), vp(y), vp(stats), vp(work), size, vp(0))
 
     def backward(dy=0x1000, x=0x1000, type=0, N=2, C=24, G=3, stats=0x4000, act=1, res=None, dx=0x3000, dres=None, work=0x5000, size=1 << 20):
@@ -303,5 +303,5 @@ def test_python_refusals_on_the_device(cp):
         cp.cprune_group_norm(x, 16, 3)
     assert e.value.status == 1
     with pytest.raises(cp.CpruneError) as e:
-        cp.cprune_group_norm(x, 16, 2, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda")[:16])
+        cp.cprune_group_norm_backward(x, x, 16, 2, torch.zeros((1, 2, 2), device="cuda"), workspace=torch.zeros(64, dtype=torch.uint8, device="cuda")[:16])
     assert e.value.status == 3

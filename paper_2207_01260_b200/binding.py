@@ -624,7 +624,9 @@ def _norm_buffer(where, norm, stream, device):
     if norm is not None:
         _checked(where, "norm", norm, (1,), _F32, device)
         return norm
-    with torch.cuda.stream(stream):            # (None: no other than the current one)
+    if stream is None:
+        return torch.empty(1, dtype=_F32, device=device)
+    with torch.cuda.stream(stream):
         return torch.empty(1, dtype=_F32, device=device)
 
 

@@ -142,6 +142,7 @@ __global__ void mx_pad_bias_kernel(const float *__restrict__ b, int n, int n_pad
 // The tensor core truncates where it adds to an accumulator; four steps start from zero and are added to the running sum by a rounded
 // addition, and the warps' sums meet in float64.
 constexpr int MXF_WARPS = 8, MXF_NT = 2, MXF_AHEAD = 2, MXF_ROWS = 32;
+constexpr long long MXF_WEIGHTS = 4 << 20;
 
 // (one float32 of y, in its form)
 __device__ __forceinline__ void mx_store(const MxProduct &p, unsigned long long n, int o, float v) {
@@ -309,10 +310,10 @@ cprune_status cprune_mx_pack(const float *w, const float *b, int out, int in, vo
     return CPRUNE_OK;
 }
 
-// Up to this many rows the weights are read by the kernel for few rows
+// Few rows and weights that are read in no time: one kernel behind the rounding, not two
 static MxTiling mx_product_tiling(size_t rows, int in, int out) {
     MxTiling t = {};
-    return rows <= MXF_ROWS ? t : mx_tiling(rows, in, out);
+    return rows <= MXF_ROWS && (long long)in * out <= MXF_WEIGHTS ? t : mx_tiling(rows, in, out);
 }
 static size_t mx_codes_bytes(size_t rows, int in) { return (rows * (size_t)mx_blocks(in) * 16 + 255) / 256 * 256; }
 
@@ -320,7 +321,7 @@ size_t cprune_mx_fc_workspace_bytes(size_t rows, int in, int out) {
     if (rows == 0 || in <= 0 || out <= 0) return 0;
     const MxTiling t = mx_product_tiling(rows, in, out);
     if (!t.tensor) return rows * (size_t)mx_blocks(in) * MX_BLOCK * 2;
-    return t.round ? 0 : mx_codes_bytes(rows, in) + cprune_mx_scale_bytes(rows, in);
+    return t.round ? 0 : mx_codes_bytes(rows, in) + cprune_mx_scale_bytes(rows, in) + mx_partial_bytes(t, rows, out);
 }
 
 cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes, const void *scales, const float *b_packed, int out, int act, const void *residual,
@@ -337,13 +338,13 @@ cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes
     p.blocks = mx_blocks(in); p.tiles4 = (p.blocks + 3) / 4; p.out = out; p.out_pad = cprune_padded_channels(out); p.act = act; p.out_is_f32 = out_is_f32;
     ChainScope chain;
     const MxTiling t = mx_product_tiling(rows, in, out);
-    if (t.tensor && t.round) return launch_mx_product(p, t, x, nullptr, in, st);
+    if (t.tensor && t.round) return launch_mx_product(p, t, x, nullptr, in, nullptr, chain, st);
     if (t.tensor) {
         uint8_t *xscales = (uint8_t *)workspace + mx_codes_bytes(rows, in);
         CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 0>, dim3(mx_grid(rows * p.tiles4, MX_T / 16)), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
                                          cprune_padded_channels(in), p.tiles4, (uint32_t *)workspace, xscales, (void *)nullptr));
         chain.follow();
-        return launch_mx_product(p, t, workspace, xscales, in, st);
+        return launch_mx_product(p, t, workspace, xscales, in, (float *)(xscales + cprune_mx_scale_bytes(rows, in)), chain, st);
     }
     CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 1>, dim3(mx_grid(rows * p.tiles4, MX_T / 16)), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
                                      cprune_padded_channels(in), p.tiles4, (uint32_t *)nullptr, (uint8_t *)nullptr, workspace));

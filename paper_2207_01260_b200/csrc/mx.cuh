@@ -84,8 +84,10 @@ struct MxTiling {
     int tensor;
     int nt, subs, tiles_n;                 // features of a block, in parts of 128; blocks along the features
     int round;                             // the rows are rounded by the product itself
+    int features, splits, per;             // features first: shares of the channels, chunks of a share
 };
 MxTiling mx_tiling(unsigned long long rows, int in, int out);
-cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const void *x, const uint8_t *xscales, int in, cudaStream_t st);
+size_t mx_partial_bytes(const MxTiling &t, unsigned long long rows, int out);
+cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const void *x, const uint8_t *xscales, int in, float *partial, ChainScope &chain, cudaStream_t st);
 
 }  // namespace cprune

@@ -7,6 +7,8 @@
 //     of 32 channels never leaves a thread) and write codes and scales where the tensor core reads them.  x is read once and nothing else
 //     is written: taken where one block covers all features.
 //   - already rounded (by mx_quantize_kernel) where several blocks share the rows: codes by TMA, scales by bulk copies.
+// Up to 128 rows change places with the features: a block takes 128 features and all rows, and a share of the channels (so that enough blocks read the
+// weights, which is what such a product consists of); the shares' sums meet in a second kernel, in a fixed order.
 // Scales lie in shared memory in pieces of 512 bytes (128 rows by 4 blocks); tcgen05.cp brings a piece into four columns of tensor memory.
 // The accumulator leaves through registers: bias, shortcut and activation on the way.
 #include <mutex>
@@ -23,7 +25,7 @@ constexpr int MXP_WARPS = 8;                          // round and store; two mo
 constexpr int MXP_THREADS = (MXP_WARPS + 2) * 32;
 constexpr int MXP_XBYTES = MXP_ROWS * 128 * 2;        // 128 channels of bf16 rows
 constexpr int MXP_MOST = 384;                         // features of a block
-constexpr int MXP_CTRL = 256;
+constexpr int MXP_CTRL = 512;
 
 struct MxpParams {
     MxProduct q;
@@ -33,7 +35,9 @@ struct MxpParams {
     int stages, xstages;
     int b_bytes, tmem_cols, sf_col;  // bytes of a chunk of weights, columns of tensor memory, where its scales begin
     const uint8_t *xscales;          // of rows that are already rounded
-    int tiles_n;
+    float *partial;                  // features first: sums of the shares [splits][rows][out_pad]
+    int tiles_n;                     // blocks along the features; features first: shares of the channels
+    int per;                         // chunks of a share
     int *status;
 };
 
@@ -77,29 +81,33 @@ __device__ __forceinline__ uint4 mx_round_block(const bf16x8 *v, uint32_t &scale
     return r;
 }
 
-template <bool ROUND>
+enum { MXP_ROUND = 0, MXP_CODES = 1, MXP_FEATURES = 2 };        // rows rounded here; rows already rounded; features first
+
+template <int FORM>
 __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ MxpParams p) {
+    constexpr bool ROUND = FORM == MXP_ROUND, FEATURES = FORM == MXP_FEATURES;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (base - raw);
-    // shared memory: codes of the rows, codes of the features, bf16 rows, scales of rows and of features, barriers, bias
+    // shared memory: codes of the rows (features first: of the features), codes of the features (of the rows), bf16 rows, scales of rows and of features, barriers, bias
     const uint32_t a0 = base, b0 = a0 + p.stages * 16384u, x0 = b0 + (uint32_t)(p.stages * p.b_bytes), sa0 = x0 + (uint32_t)(p.xstages * MXP_XBYTES);
     const uint32_t sb0 = sa0 + p.stages * 1024u, ctrl0 = sb0 + (uint32_t)(p.stages * p.subs) * 1024u;
     uint8_t *ctrl = smem + (ctrl0 - base);
     auto xfull = [&](int s) { return ctrl0 + 8u * s; };
     auto xempty = [&](int s) { return ctrl0 + 32u + 8u * s; };
     auto afull = [&](int s) { return ctrl0 + 64u + 8u * s; };          // rows rounded
-    auto bfull = [&](int s) { return ctrl0 + 96u + 8u * s; };          // weights (and rounded rows) here
-    auto empty = [&](int s) { return ctrl0 + 128u + 8u * s; };         // the MMAs have read a stage
-    const uint32_t done = ctrl0 + 160u;
-    uint32_t *tmem_slot = (uint32_t *)(ctrl + 168);
-    volatile int *abort_flag = (volatile int *)(ctrl + 172);
+    auto bfull = [&](int s) { return ctrl0 + 128u + 8u * s; };         // weights (and rounded rows) here
+    auto empty = [&](int s) { return ctrl0 + 192u + 8u * s; };         // the MMAs have read a stage
+    const uint32_t done = ctrl0 + 256u;
+    uint32_t *tmem_slot = (uint32_t *)(ctrl + 264);
+    volatile int *abort_flag = (volatile int *)(ctrl + 268);
     float *bias_s = (float *)(ctrl + MXP_CTRL);
 
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int tile_n = blockIdx.x % p.tiles_n;
-    const long long row0 = (long long)(blockIdx.x / p.tiles_n) * MXP_ROWS;
-    const int o0 = tile_n * p.nt;
+    const long long row0 = (long long)(blockIdx.x / p.tiles_n) * MXP_ROWS;       // (features first: the first feature)
+    const int o0 = FEATURES ? 0 : tile_n * p.nt;                                 // (... the first row)
+    const int c_begin = FEATURES ? tile_n * p.per : 0, c_end = FEATURES ? min(p.chunks, c_begin + p.per) : p.chunks;
     if (warp == MXP_WARPS) {
         tmem_alloc(smem_u32(tmem_slot), (uint32_t)p.tmem_cols);
         tmem_relinquish();
@@ -112,7 +120,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
-    } else if (warp < MXP_WARPS) {
+    } else if (warp < MXP_WARPS && !FEATURES) {
         for (int e = threadIdx.x; e < p.nt; e += MXP_WARPS * 32) bias_s[e] = o0 + e < p.q.out ? __ldg(p.q.bias + o0 + e) : 0.f;
     }
     tc_fence_before();
@@ -120,11 +128,29 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     bool ok = true;
-    pdl_wait();
 
     if (warp == MXP_WARPS) {
         // -------------------------------------------------------------------------------------------- loads
+        // The weights are nobody's result: those of the first chunks are asked for before the preceding kernel has finished.
+        const uint32_t w0 = FEATURES ? a0 : b0, w_step = FEATURES ? 16384u : (uint32_t)p.b_bytes, ws0 = FEATURES ? sa0 : sb0;
+        const int w_first = FEATURES ? (int)row0 : o0, w_parts = FEATURES ? 1 : p.subs, w_box = FEATURES ? MXP_ROWS : p.box;
+        const int w_tiles = min(w_parts, (p.q.out + 127) / 128 - w_first / 128);         // tiles of scales that there are
         int half = 0;
+        auto scale_tiles = [&](int c) { return min(2, p.q.tiles4 - 2 * c); };
+        auto load_w = [&](int c, int s) {
+            const int tiles = scale_tiles(c);
+            const uint32_t rows = ROUND ? 0u : (uint32_t)((FEATURES ? p.box * 128 : 16384) + tiles * 512);
+            mbar_expect_tx(bfull(s), (uint32_t)(w_parts * w_box * 128 + w_tiles * tiles * 512) + rows);
+            for (int n = 0; n < w_parts; ++n) tma_load_2d(w0 + (uint32_t)s * w_step + (uint32_t)n * 16384u, &tm_w, bfull(s), c * 64, w_first + n * 128);
+            for (int n = 0; n < w_tiles; ++n)
+                bulk_load(ws0 + (uint32_t)((s * w_parts + n) * 1024), p.q.scales + ((size_t)(w_first / 128 + n) * p.q.tiles4 + 2 * c) * 512, (uint32_t)tiles * 512u, bfull(s));
+        };
+        auto load_rows = [&](int c, int s) {
+            if (ROUND) return;
+            const int first = FEATURES ? 0 : (int)row0;
+            tma_load_2d(FEATURES ? b0 + (uint32_t)(s * p.b_bytes) : a0 + (uint32_t)s * 16384u, &tm_x, bfull(s), c * 64, first);
+            bulk_load((FEATURES ? sb0 : sa0) + (uint32_t)s * 1024u, p.xscales + ((size_t)(first / 128) * p.q.tiles4 + 2 * c) * 512, (uint32_t)scale_tiles(c) * 512u, bfull(s));
+        };
         auto load_x = [&](int h) {
             const int s = h % p.xstages;
             if (h >= p.xstages) ok = __all_sync(0xffffffffu, mbar_wait(xempty(s), (uint32_t)(h / p.xstages - 1) & 1u, abort_flag, p.status));
@@ -135,19 +161,17 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             }
             __syncwarp();
         };
-        for (int c = 0; c < p.chunks && ok; ++c) {
-            const int s = c % p.stages, tiles = min(2, p.q.tiles4 - 2 * c);
-            if (c >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (uint32_t)(c / p.stages - 1) & 1u, abort_flag, p.status));
+        const int ahead = min(p.stages, c_end - c_begin);
+        if (elect_one())
+            for (int i = 0; i < ahead; ++i) load_w(c_begin + i, i);
+        __syncwarp();
+        pdl_wait();
+        for (int i = 0; c_begin + i < c_end && ok; ++i) {
+            const int c = c_begin + i, s = i % p.stages;
+            if (i >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (uint32_t)(i / p.stages - 1) & 1u, abort_flag, p.status));
             if (ok && elect_one()) {
-                const int row_tiles = min(p.subs, (p.q.out + 127) / 128 - o0 / 128);       // tiles of scales that there are
-                mbar_expect_tx(bfull(s), (uint32_t)(p.subs * p.box * 128 + row_tiles * tiles * 512 + (ROUND ? 0 : 16384 + tiles * 512)));
-                for (int n = 0; n < p.subs; ++n) tma_load_2d(b0 + (uint32_t)(s * p.b_bytes + n * 16384), &tm_w, bfull(s), c * 64, o0 + n * 128);
-                for (int n = 0; n < row_tiles; ++n)
-                    bulk_load(sb0 + (uint32_t)((s * p.subs + n) * 1024), p.q.scales + ((size_t)(o0 / 128 + n) * p.q.tiles4 + 2 * c) * 512, (uint32_t)tiles * 512u, bfull(s));
-                if (!ROUND) {
-                    tma_load_2d(a0 + (uint32_t)s * 16384u, &tm_x, bfull(s), c * 64, (int)row0);
-                    bulk_load(sa0 + (uint32_t)s * 1024u, p.xscales + ((size_t)(row0 / 128) * p.q.tiles4 + 2 * c) * 512, (uint32_t)tiles * 512u, bfull(s));
-                }
+                if (i >= ahead) load_w(c, s);
+                load_rows(c, s);
             }
             __syncwarp();
             if (ROUND)
@@ -157,9 +181,9 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
         // --------------------------------------------------------------------------------------------- MMAs
         // E2M1 operands, scales that are powers of two; 64 channels of every 128 under scales 0 or 2 of a column
         const uint32_t idesc = (1u << 7) | (1u << 10) | (1u << 23) | (1u << 27);
-        for (int c = 0; c < p.chunks && ok; ++c) {
-            const int s = c % p.stages;
-            const uint32_t parity = (uint32_t)(c / p.stages) & 1u;
+        for (int i = 0; c_begin + i < c_end && ok; ++i) {
+            const int c = c_begin + i, s = i % p.stages;
+            const uint32_t parity = (uint32_t)(i / p.stages) & 1u;
             ok = __all_sync(0xffffffffu, mbar_wait(bfull(s), parity, abort_flag, p.status));
             if (ROUND) ok = ok && __all_sync(0xffffffffu, mbar_wait(afull(s), parity, abort_flag, p.status));
             if (!ok) break;
@@ -178,11 +202,11 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                         const uint32_t b = desc_lo(b0 + (uint32_t)(s * p.b_bytes + n * 16384)) + 2u * k;
                         const int width = min(128, p.nt - n * 128);
                         umma_mxf4(tmem_base + (uint32_t)(n * 128), a, b, idesc | (uint32_t)(width >> 3) << 17 | id << 29 | id << 4, sfa + 4u * (k >> 1),
-                                  sfb + (uint32_t)((k >> 1) * p.subs + n) * 4u + first, (c | k) ? 1u : 0u);
+                                  sfb + (uint32_t)((k >> 1) * p.subs + n) * 4u + first, (i | k) ? 1u : 0u);
                     }
                 }
                 umma_commit(empty(s));
-                if (c + 1 == p.chunks) umma_commit(done);
+                if (c + 1 == c_end) umma_commit(done);
             }
             __syncwarp();
         }
@@ -221,30 +245,117 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                 }
             }
         // ------------------------------------------------------------------------------------------ epilogue
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag, p.status));
-        if (ok) {
-            tc_fence_after();
-            const int quarter = warp & 3;
-            const long long row = row0 + quarter * 32 + lane;
-            const bool in = row < (long long)p.q.rows;
-            for (int u = warp >> 2; u * 16 < p.nt; u += 2) {
-                const int o = o0 + u * 16;
-                if (o >= p.q.out_pad) break;
-                bf16x8 rv[2] = {};
-                if (p.q.res && in) {
-                    rv[0] = *reinterpret_cast<const bf16x8 *>(p.q.res + (size_t)row * p.q.out_pad + o);
-                    if (o + 8 < p.q.out_pad) rv[1] = *reinterpret_cast<const bf16x8 *>(p.q.res + (size_t)row * p.q.out_pad + o + 8);
-                }
-                uint32_t v[16];
-                tmem_ld16(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(u * 16), v);
-                tmem_ld_wait();
-                float f[16], g[16];
-                unpack8(rv[0], g);
-                unpack8(rv[1], g + 8);
+        pdl_wait();
+        const int quarter = warp & 3;
+        const uint32_t t_lane = tmem_base + ((uint32_t)(quarter * 32) << 16);
+        if (FEATURES) {
+            // a lane has a feature, a column is a row
+            ok = __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag, p.status));
+            if (ok) {
+                tc_fence_after();
+                const int o = (int)row0 + quarter * 32 + lane;
+                for (int u = warp >> 2; u * 16 < p.nt; u += 2) {
+                    uint32_t v[16];
+                    tmem_ld16(t_lane + (uint32_t)(u * 16), v);
+                    tmem_ld_wait();
+                    float *to = p.partial + ((size_t)tile_n * p.q.rows + u * 16) * p.q.out_pad + o;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) f[j] = o + j < p.q.out ? mx_act(__uint_as_float(v[j]) + bias_s[u * 16 + j] + g[j], p.q.act) : 0.f;
-                if (!in) continue;
-                if (p.q.out_is_f32) {
+                    for (int j = 0; j < 16; ++j)
+                        if (u * 16 + j < (int)p.q.rows && o < p.q.out) to[(size_t)j * p.q.out_pad] = __uint_as_float(v[j]);
+                }
+            }
+        } else if (!p.q.out_is_f32) {
+            // A warp takes 32 rows of 64 features at a time; in its 4 KB of shared memory the rows of tensor memory become whole lines.  The shortcut's lines
+            // are asked for before the sums are there.
+            uint8_t *stage = smem + warp * 4096;           // (codes that the MMAs have read)
+            const int piece = lane & 7, line = lane >> 3;
+            const long long r0 = row0 + quarter * 32;
+            const __nv_bfloat16 *res = p.q.res;
+            __nv_bfloat16 *y = (__nv_bfloat16 *)p.q.y;
+            const int panels = (min(p.nt, p.q.out_pad - o0) + 63) / 64;
+            bf16x8 rv[8];
+            auto fetch = [&](int panel) {
+                const int o = o0 + panel * 64 + piece * 8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const long long r = r0 + i * 4 + line;
+                    if (panel < panels && o < p.q.out_pad && r < (long long)p.q.rows) rv[i] = *reinterpret_cast<const bf16x8 *>(res + (size_t)r * p.q.out_pad + o);
+                    else rv[i] = bf16x8{{0u, 0u, 0u, 0u}};
+                }
+            };
+            int panel = warp >> 2;
+            if (res) fetch(panel);
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag, p.status));
+            if (ok) {
+                tc_fence_after();
+                for (; panel < panels; panel += 2) {
+                    if (res) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) *reinterpret_cast<bf16x8 *>(stage + sub_off(i * 4 + line, piece)) = rv[i];
+                        __syncwarp();
+                        fetch(panel + 2);
+                    }
+                    const int left = min(64, p.nt - panel * 64);               // (whole sixteens)
+#pragma unroll 1
+                    for (int u = 0; u * 16 < left; ++u) {
+                        uint32_t v[16];
+                        tmem_ld16(t_lane + (uint32_t)(panel * 64 + u * 16), v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            bf16x8 *at = reinterpret_cast<bf16x8 *>(stage + sub_off(lane, u * 2 + h));
+                            const int e = panel * 64 + u * 16 + h * 8;
+                            float f[8], g[8];
+                            if (res) unpack8(*at, g);
+                            const float4 b0v = *reinterpret_cast<const float4 *>(bias_s + e), b1v = *reinterpret_cast<const float4 *>(bias_s + e + 4);
+                            const float bias[8] = {b0v.x, b0v.y, b0v.z, b0v.w, b1v.x, b1v.y, b1v.z, b1v.w};
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                float z = __uint_as_float(v[8 * h + j]) + bias[j];
+                                if (res) z += g[j];
+                                f[j] = o0 + e + j < p.q.out ? mx_act(z, p.q.act) : 0.f;
+                            }
+                            *at = pack8(f);
+                        }
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const long long r = r0 + i * 4 + line;
+                        const int o = o0 + panel * 64 + piece * 8;
+                        if (piece * 8 < left && o < p.q.out_pad && r < (long long)p.q.rows)
+                            *reinterpret_cast<bf16x8 *>(y + (size_t)r * p.q.out_pad + o) = *reinterpret_cast<const bf16x8 *>(stage + sub_off(i * 4 + line, piece));
+                    }
+                    __syncwarp();
+                }
+            }
+        } else {
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag, p.status));
+            if (ok) {
+                tc_fence_after();
+                const long long row = row0 + quarter * 32 + lane;
+                const bool in = row < (long long)p.q.rows;
+                for (int u = warp >> 2; u * 16 < p.nt; u += 2) {
+                    const int o = o0 + u * 16;
+                    if (o >= p.q.out) break;
+                    bf16x8 rv[2] = {};
+                    if (p.q.res && in) {
+                        rv[0] = *reinterpret_cast<const bf16x8 *>(p.q.res + (size_t)row * p.q.out_pad + o);
+                        if (o + 8 < p.q.out_pad) rv[1] = *reinterpret_cast<const bf16x8 *>(p.q.res + (size_t)row * p.q.out_pad + o + 8);
+                    }
+                    uint32_t v[16];
+                    tmem_ld16(t_lane + (uint32_t)(u * 16), v);
+                    tmem_ld_wait();
+                    float f[16], g[16];
+                    unpack8(rv[0], g);
+                    unpack8(rv[1], g + 8);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float z = __uint_as_float(v[j]) + bias_s[u * 16 + j];
+                        if (p.q.res) z += g[j];
+                        f[j] = mx_act(z, p.q.act);
+                    }
+                    if (!in) continue;
                     float *y = (float *)p.q.y + (size_t)row * p.q.out + o;
                     if (((uintptr_t)y & 15) == 0 && o + 16 <= p.q.out) {
 #pragma unroll
@@ -254,10 +365,6 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                         for (int j = 0; j < 16; ++j)
                             if (o + j < p.q.out) y[j] = f[j];
                     }
-                } else {
-                    __nv_bfloat16 *y = (__nv_bfloat16 *)p.q.y + (size_t)row * p.q.out_pad + o;
-                    *reinterpret_cast<bf16x8 *>(y) = pack8(f);
-                    if (o + 8 < p.q.out_pad) *reinterpret_cast<bf16x8 *>(y + 8) = pack8(f + 8);
                 }
             }
         }
@@ -275,9 +382,57 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
     }
 }
 
+// The shares' sums of a product whose features come first, then bias, shortcut and activation: a thread has four features of a row
+constexpr int MXP_FINISH = 128;
+__global__ void __launch_bounds__(MXP_FINISH) mx_finish_kernel(const float *__restrict__ partial, int splits, const MxProduct q) {
+    pdl_wait();
+    pdl_trigger();
+    const int o = (blockIdx.x * MXP_FINISH + threadIdx.x) * 4;
+    const size_t n = blockIdx.y;
+    if (o >= q.out_pad) return;
+    const size_t step = (size_t)q.rows * q.out_pad;
+    const float *from = partial + n * q.out_pad + o;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < splits; k0 += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = k0 + k < splits ? __ldcg(reinterpret_cast<const float4 *>(from + (k0 + k) * step)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { s[0] += v[k].x; s[1] += v[k].y; s[2] += v[k].z; s[3] += v[k].w; }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (o + j < q.out) {
+            s[j] += __ldg(q.bias + o + j);
+            if (q.res) s[j] += __bfloat162float(q.res[n * q.out_pad + o + j]);
+            s[j] = mx_act(s[j], q.act);
+        } else s[j] = 0.f;
+    }
+    if (q.out_is_f32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (o + j < q.out) ((float *)q.y)[n * q.out + o + j] = s[j];
+    } else {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(s[0], s[1]), hi = __floats2bfloat162_rn(s[2], s[3]);
+        *reinterpret_cast<uint2 *>((__nv_bfloat16 *)q.y + n * q.out_pad + o) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+    }
+}
+
 // How a product is shared out
 MxTiling mx_tiling(unsigned long long rows, int in, int out) {
     MxTiling t = {};
+    t.tensor = 1;
+    if (rows <= MXP_ROWS) {
+        t.features = 1;
+        t.nt = round_up((int)rows, 16);
+        t.subs = 1;
+        const int tiles = (out + MXP_ROWS - 1) / MXP_ROWS, chunks = (in + MXP_CHUNK - 1) / MXP_CHUNK;
+        t.splits = (148 + tiles - 1) / tiles;              // a block to an SM
+        if (t.splits > chunks) t.splits = chunks;
+        t.per = (chunks + t.splits - 1) / t.splits;
+        t.splits = (chunks + t.per - 1) / t.per;
+        return t;
+    }
     const long long tiles_m = (long long)((rows + MXP_ROWS - 1) / MXP_ROWS);
     const int all = round_up(out, 16);
     t.nt = all <= MXP_MOST ? all : 256;
@@ -286,11 +441,13 @@ MxTiling mx_tiling(unsigned long long rows, int in, int out) {
     t.tiles_n = (all + t.nt - 1) / t.nt;
     t.subs = (t.nt + 127) / 128;
     t.round = t.tiles_n == 1;
-    t.tensor = 1;
     return t;
 }
+size_t mx_partial_bytes(const MxTiling &t, unsigned long long rows, int out) {
+    return t.features ? (size_t)t.splits * rows * cprune_padded_channels(out) * sizeof(float) : 0;
+}
 
-template <bool ROUND>
+template <int FORM>
 static cprune_status launch_product(const CUtensorMap *tm, const MxpParams &p, long long blocks, size_t smem, cudaStream_t st) {
     static std::mutex attr_mu;
     static bool attr_set[64] = {false};    // the shared-memory limit of a kernel is a per-device attribute
@@ -300,60 +457,73 @@ static cprune_status launch_product(const CUtensorMap *tm, const MxpParams &p, l
         if (dev < 0 || dev >= 64) return CPRUNE_ERR_UNSUPPORTED;
         std::lock_guard<std::mutex> lock(attr_mu);
         if (!attr_set[dev]) {
-            CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(mx_product_kernel<ROUND>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+            CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(mx_product_kernel<FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
             attr_set[dev] = true;
         }
     }
-    CPRUNE_CUDA_CHECK(launch_chained(mx_product_kernel<ROUND>, dim3((unsigned)blocks), dim3(MXP_THREADS), smem, st, tm[0], tm[1], p));
+    CPRUNE_CUDA_CHECK(launch_chained(mx_product_kernel<FORM>, dim3((unsigned)blocks), dim3(MXP_THREADS), smem, st, tm[0], tm[1], p));
     return CPRUNE_OK;
 }
 
-// x: bf16 rows (t.round), else their codes, with their scales behind them
-cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const void *x, const uint8_t *xscales, int in, cudaStream_t st) {
+static cprune_status encode_codes(CUtensorMap *map, const void *codes, int blocks, unsigned long long rows, int box_rows) {
+    const unsigned long long dims[2] = {(unsigned long long)blocks * 8, rows};           // (in units of two bytes)
+    const unsigned long long strides[1] = {(unsigned long long)blocks * 16};
+    const unsigned box[2] = {64, (unsigned)box_rows};
+    return encode_tiled_bf16_swz(map, codes, 2, dims, strides, box, 128, true);
+}
+
+// x: bf16 rows (t.round), else their codes, with their scales
+cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const void *x, const uint8_t *xscales, int in, float *partial, ChainScope &chain, cudaStream_t st) {
     MxpParams p = {};
     p.q = q;
-    p.nt = t.nt; p.subs = t.subs; p.tiles_n = t.tiles_n;
+    p.nt = t.nt; p.subs = t.subs; p.tiles_n = t.features ? t.splits : t.tiles_n; p.per = t.per;
     p.box = t.nt < 128 ? t.nt : 128;
     p.chunks = (in + MXP_CHUNK - 1) / MXP_CHUNK;
     p.halves = (in + 127) / 128;
     p.steps_last = (in - (p.chunks - 1) * MXP_CHUNK + 63) / 64;
-    p.b_bytes = t.subs * 16384;
+    p.b_bytes = t.features ? round_up(p.box * 128, 1024) : t.subs * 16384;
     p.xscales = xscales;
+    p.partial = partial;
     p.status = device_status_word();
     if (!p.status) return cuda_fail(cudaGetLastError(), "status word");
     p.sf_col = t.nt;
+    const int chunks = t.features ? t.per : p.chunks;
     auto bytes = [&](int stages, int xstages) {
-        return 1024 + (size_t)stages * (16384 + p.b_bytes + 1024 + t.subs * 1024) + (size_t)xstages * MXP_XBYTES + MXP_CTRL + (size_t)t.nt * 4;
+        const size_t s = (size_t)stages * (16384 + p.b_bytes + 1024 + t.subs * 1024) + (size_t)xstages * MXP_XBYTES + MXP_CTRL + (size_t)t.nt * 4;
+        return 1024 + (s > 32768 ? s : 32768);              // (the epilogue needs 32 KB at the front)
     };
-    p.stages = p.chunks < 4 ? p.chunks : 4;
+    // four stages of weights (eight where they are all there is to read) and of rows, as far as two blocks fit an SM
+    const int most = t.features ? 8 : 4;
+    p.stages = chunks < most ? chunks : most;
     p.xstages = t.round ? (p.halves < 4 ? p.halves : 4) : 0;
-    while (bytes(p.stages, p.xstages) > 113 * 1024 && (p.stages > 2 || p.xstages > 2)) {
+    while (!t.features && bytes(p.stages, p.xstages) > 113 * 1024 && (p.stages > 2 || p.xstages > 2)) {
         if (p.xstages > 2) --p.xstages;
         else --p.stages;
     }
-    while (p.stages > 1 && p.sf_col + p.stages * 8 * (t.subs + 1) > 512) --p.stages;
+    while (p.stages > 1 && (p.sf_col + p.stages * 8 * (t.subs + 1) > 512 || bytes(p.stages, p.xstages) > 226 * 1024)) --p.stages;
     const int cols = p.sf_col + p.stages * 8 * (t.subs + 1);
     for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
     CUtensorMap tm[2];
-    const unsigned long long kb = q.blocks;
-    {
-        const unsigned long long dims[2] = {t.round ? (unsigned long long)in : kb * 8, q.rows};
-        const unsigned long long strides[1] = {t.round ? (unsigned long long)cprune_padded_channels(in) * 2 : kb * 16};
+    cprune_status s;
+    if (t.round) {
+        const unsigned long long dims[2] = {(unsigned long long)in, q.rows};
+        const unsigned long long strides[1] = {(unsigned long long)cprune_padded_channels(in) * 2};
         const unsigned box[2] = {64, MXP_ROWS};
-        cprune_status s = encode_tiled_bf16_swz(&tm[0], x, 2, dims, strides, box, 128, true);
-        if (s != CPRUNE_OK) return s;
-    }
-    {
-        const unsigned long long dims[2] = {kb * 8, (unsigned long long)q.out};
-        const unsigned long long strides[1] = {kb * 16};
-        const unsigned box[2] = {64, (unsigned)p.box};
-        cprune_status s = encode_tiled_bf16_swz(&tm[1], q.codes, 2, dims, strides, box, 128, true);
-        if (s != CPRUNE_OK) return s;
-    }
-    const long long blocks = (long long)((q.rows + MXP_ROWS - 1) / MXP_ROWS) * t.tiles_n;
+        s = encode_tiled_bf16_swz(&tm[0], x, 2, dims, strides, box, 128, true);
+    } else s = encode_codes(&tm[0], x, q.blocks, q.rows, t.features ? p.box : MXP_ROWS);
+    if (s == CPRUNE_OK) s = encode_codes(&tm[1], q.codes, q.blocks, q.out, t.features ? MXP_ROWS : p.box);
+    if (s != CPRUNE_OK) return s;
+    const long long blocks = t.features ? (long long)((q.out + MXP_ROWS - 1) / MXP_ROWS) * t.splits : (long long)((q.rows + MXP_ROWS - 1) / MXP_ROWS) * t.tiles_n;
     if (blocks > 0x7fffffffLL) return CPRUNE_ERR_UNSUPPORTED;
     const size_t smem = bytes(p.stages, p.xstages);
-    return t.round ? launch_product<true>(tm, p, blocks, smem, st) : launch_product<false>(tm, p, blocks, smem, st);
+    if (t.round) return launch_product<MXP_ROUND>(tm, p, blocks, smem, st);
+    if (!t.features) return launch_product<MXP_CODES>(tm, p, blocks, smem, st);
+    s = launch_product<MXP_FEATURES>(tm, p, blocks, smem, st);
+    if (s != CPRUNE_OK) return s;
+    chain.follow();
+    CPRUNE_CUDA_CHECK(launch_chained(mx_finish_kernel, dim3((q.out_pad / 4 + MXP_FINISH - 1) / MXP_FINISH, (unsigned)q.rows), dim3(MXP_FINISH), 0, st, (const float *)partial,
+                                     t.splits, q));
+    return CPRUNE_OK;
 }
 
 }  // namespace cprune

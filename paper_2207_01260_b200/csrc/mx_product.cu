@@ -26,6 +26,7 @@ constexpr int MXP_THREADS = (MXP_WARPS + 2) * 32;
 constexpr int MXP_XBYTES = MXP_ROWS * 128 * 2;        // 128 channels of bf16 rows
 constexpr int MXP_MOST = 384;                         // features of a block
 constexpr int MXP_CTRL = 512;
+constexpr int MXP_SF_COLS = 8 + 2 * 12;               // columns of a stage's scales
 
 struct MxpParams {
     MxProduct q;
@@ -53,8 +54,9 @@ __device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint32_t a_lo, uint32
         : "memory");
 }
 // 32 rows of 16 bytes (8-row groups 128 bytes apart) into four columns, the same for every quarter of the lanes
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint32_t smem) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(smem_desc_interleaved(smem, 128)) : "memory");
+constexpr uint32_t DESC_HI_SCALES = (128u >> 4) | (1u << 14);
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint32_t desc_lo) {
+    asm volatile("{\n\t.reg .b64 d;\n\tmov.b64 d, {%1, %2};\n\ttcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}" ::"r"(taddr), "r"(desc_lo), "r"(DESC_HI_SCALES) : "memory");
 }
 
 // 32 bf16 values to codes (16 bytes) and a scale
@@ -180,7 +182,11 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
     } else if (warp == MXP_WARPS + 1) {
         // --------------------------------------------------------------------------------------------- MMAs
         // E2M1 operands, scales that are powers of two; 64 channels of every 128 under scales 0 or 2 of a column
-        const uint32_t idesc = (1u << 7) | (1u << 10) | (1u << 23) | (1u << 27);
+        const uint32_t idesc = (1u << 7) | (1u << 10) | (1u << 23) | (1u << 27), idesc_128 = idesc | 16u << 17;
+        const uint32_t idesc_last = idesc | (uint32_t)((p.nt - (p.subs - 1) * 128) >> 3) << 17;
+        const uint32_t a_lo = desc_lo(a0), b_lo = desc_lo(b0), b_step = (uint32_t)p.b_bytes >> 4, sa_lo = desc_lo(sa0), sb_lo = desc_lo(sb0), cb_step = (uint32_t)p.subs * 64u;
+        // a stage's scales: 8 columns of the rows', 2 x 12 of the features' (those that begin in the middle of a piece: a column has those of 32)
+        const uint32_t sf_base = tmem_base + (uint32_t)p.sf_col, sf_step = MXP_SF_COLS, first = (uint32_t)(o0 % 128) / 32u;
         for (int i = 0; c_begin + i < c_end && ok; ++i) {
             const int c = c_begin + i, s = i % p.stages;
             const uint32_t parity = (uint32_t)(i / p.stages) & 1u;
@@ -189,21 +195,27 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-                // (features that begin in the middle of a piece of scales: a column has those of 32)
-                const uint32_t sfa = tmem_base + (uint32_t)(p.sf_col + s * 8 * (p.subs + 1)), sfb = sfa + 8u, first = (uint32_t)(o0 % 128) / 32u;
+                // (One thread issues all of it, so that every instruction of address arithmetic counts: written out, with additions only.)
                 const int steps = c + 1 == p.chunks ? p.steps_last : 4;
-                for (int h = 0; 2 * h < steps; ++h) {
-                    tmem_copy_scales(sfa + 4u * h, sa0 + (uint32_t)(s * 1024 + h * 512));
-                    for (int n = 0; n < p.subs; ++n) tmem_copy_scales(sfb + (uint32_t)(h * p.subs + n) * 4u, sb0 + (uint32_t)((s * p.subs + n) * 1024 + h * 512));
+                const uint32_t sfa = sf_base + (uint32_t)s * sf_step, a = a_lo + (uint32_t)s * 1024u, b = b_lo + (uint32_t)s * b_step;
+                const uint32_t ca = sa_lo + (uint32_t)s * 64u, cb = sb_lo + (uint32_t)s * cb_step;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (2 * h >= steps) break;
+                    tmem_copy_scales(sfa + 4u * h, ca + 32u * h);
+#pragma unroll
+                    for (int n = 0; n < MXP_MOST / 128; ++n)
+                        if (n < p.subs) tmem_copy_scales(sfa + 8u + 12u * h + 4u * n, cb + 64u * n + 32u * h);
                 }
-                for (int k = 0; k < steps; ++k) {
-                    const uint32_t a = desc_lo(a0 + (uint32_t)s * 16384u) + 2u * k, id = (uint32_t)(k & 1) * 2u;
-                    for (int n = 0; n < p.subs; ++n) {
-                        const uint32_t b = desc_lo(b0 + (uint32_t)(s * p.b_bytes + n * 16384)) + 2u * k;
-                        const int width = min(128, p.nt - n * 128);
-                        umma_mxf4(tmem_base + (uint32_t)(n * 128), a, b, idesc | (uint32_t)(width >> 3) << 17 | id << 29 | id << 4, sfa + 4u * (k >> 1),
-                                  sfb + (uint32_t)((k >> 1) * p.subs + n) * 4u + first, (i | k) ? 1u : 0u);
-                    }
+                const uint32_t sfb = sfa + 8u + first;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k >= steps) break;
+#pragma unroll
+                    for (int n = 0; n < MXP_MOST / 128; ++n)
+                        if (n < p.subs)
+                            umma_mxf4(tmem_base + 128u * n, a + 2u * k, b + 1024u * n + 2u * k, (n + 1 < p.subs ? idesc_128 : idesc_last) + (k & 1) * ((2u << 29) | (2u << 4)),
+                                      sfa + 4u * (k >> 1), sfb + 12u * (k >> 1) + 4u * n, (i | k) ? 1u : 0u);
                 }
                 umma_commit(empty(s));
                 if (c + 1 == c_end) umma_commit(done);
@@ -500,8 +512,8 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
         if (p.xstages > 2) --p.xstages;
         else --p.stages;
     }
-    while (p.stages > 1 && (p.sf_col + p.stages * 8 * (t.subs + 1) > 512 || bytes(p.stages, p.xstages) > 226 * 1024)) --p.stages;
-    const int cols = p.sf_col + p.stages * 8 * (t.subs + 1);
+    while (p.stages > 1 && (p.sf_col + p.stages * MXP_SF_COLS > 512 || bytes(p.stages, p.xstages) > 226 * 1024)) --p.stages;
+    const int cols = p.sf_col + p.stages * MXP_SF_COLS;
     for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
     CUtensorMap tm[2];
     cprune_status s;

@@ -3,8 +3,8 @@
 //
 // A block takes 128 rows and up to 384 features (each 128 of them one MMA), and goes through the channels 256 at a time: a row of codes of such a
 // chunk is 128 bytes.  The rows come in one of two ways:
-//   - rounded here: the bf16 rows arrive by TMA, 128 channels at a time; eight warps round them (a thread 64 channels of a row, so that a block
-//     of 32 channels never leaves a thread) and write codes and scales where the tensor core reads them.  x is read once and nothing else
+//   - rounded here: the bf16 rows arrive by TMA, 64 channels at a time; eight warps round them (a thread a block of 32 channels of a row)
+//     and write codes and scales where the tensor core reads them.  x is read once and nothing else
 //     is written: taken where one block covers all features.
 //   - already rounded (by mx_quantize_kernel) where several blocks share the rows: codes by TMA, scales by bulk copies.
 // Up to 128 rows change places with the features: a block takes 128 features and all rows, and a share of the channels (so that enough blocks read the
@@ -23,15 +23,15 @@ namespace cprune {
 constexpr int MXP_ROWS = 128, MXP_CHUNK = 256;        // rows of a block; channels of a chunk (128 bytes of codes)
 constexpr int MXP_WARPS = 8;                          // round and store; two more load and multiply
 constexpr int MXP_THREADS = (MXP_WARPS + 2) * 32;
-constexpr int MXP_XBYTES = MXP_ROWS * 128 * 2;        // 128 channels of bf16 rows
+constexpr int MXP_XBYTES = MXP_ROWS * 64 * 2;         // 64 channels of bf16 rows
 constexpr int MXP_MOST = 384;                         // features of a block
 constexpr int MXP_CTRL = 512;
 constexpr int MXP_SF_COLS = 8 + 2 * 12;               // columns of a stage's scales
 
 struct MxpParams {
     MxProduct q;
-    int nt, subs, box;               // features of a block, in parts of 128; feature rows of a TMA box
-    int chunks, halves;              // of 256 and of 128 channels
+    int nt, subs, box;               // features of a block, in parts of 128; rows of a TMA box of them
+    int chunks, boxes;               // of 256 and of 64 channels
     int steps_last;                  // MMA steps (64 channels) of the last chunk
     int stages, xstages;
     int b_bytes, tmem_cols, sf_col;  // bytes of a chunk of weights, columns of tensor memory, where its scales begin
@@ -83,6 +83,19 @@ __device__ __forceinline__ uint4 mx_round_block(const bf16x8 *v, uint32_t &scale
     return r;
 }
 
+// relu and relu6 of bf16 values, which keep a NaN; 0 and 6 are bf16 values, so that the clamp may follow the rounding
+__device__ __forceinline__ bf16x8 mx_clamp8(bf16x8 v, int act) {
+    if (act != CPRUNE_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(v.w[i]) : "r"(0u));
+        if (act == CPRUNE_ACT_RELU6) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm("min.NaN.bf16x2 %0, %0, %1;" : "+r"(v.w[i]) : "r"(0x40C040C0u));
+        }
+    }
+    return v;
+}
+
 enum { MXP_ROUND = 0, MXP_CODES = 1, MXP_FEATURES = 2 };        // rows rounded here; rows already rounded; features first
 
 template <int FORM>
@@ -96,13 +109,13 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
     const uint32_t sb0 = sa0 + p.stages * 1024u, ctrl0 = sb0 + (uint32_t)(p.stages * p.subs) * 1024u;
     uint8_t *ctrl = smem + (ctrl0 - base);
     auto xfull = [&](int s) { return ctrl0 + 8u * s; };
-    auto xempty = [&](int s) { return ctrl0 + 32u + 8u * s; };
-    auto afull = [&](int s) { return ctrl0 + 64u + 8u * s; };          // rows rounded
-    auto bfull = [&](int s) { return ctrl0 + 128u + 8u * s; };         // weights (and rounded rows) here
-    auto empty = [&](int s) { return ctrl0 + 192u + 8u * s; };         // the MMAs have read a stage
-    const uint32_t done = ctrl0 + 256u;
-    uint32_t *tmem_slot = (uint32_t *)(ctrl + 264);
-    volatile int *abort_flag = (volatile int *)(ctrl + 268);
+    auto xempty = [&](int s) { return ctrl0 + 64u + 8u * s; };
+    auto afull = [&](int s) { return ctrl0 + 128u + 8u * s; };         // rows rounded
+    auto bfull = [&](int s) { return ctrl0 + 192u + 8u * s; };         // weights (and rounded rows) here
+    auto empty = [&](int s) { return ctrl0 + 256u + 8u * s; };         // the MMAs have read a stage
+    const uint32_t done = ctrl0 + 320u;
+    uint32_t *tmem_slot = (uint32_t *)(ctrl + 328);
+    volatile int *abort_flag = (volatile int *)(ctrl + 332);
     float *bias_s = (float *)(ctrl + MXP_CTRL);
 
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -116,7 +129,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
         pdl_trigger();
         if (lane == 0) {
             for (int s = 0; s < p.xstages; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), MXP_WARPS); }
-            for (int s = 0; s < p.stages; ++s) { mbar_init(afull(s), 2 * MXP_WARPS); mbar_init(bfull(s), 1); mbar_init(empty(s), 1); }
+            for (int s = 0; s < p.stages; ++s) { mbar_init(afull(s), MXP_WARPS); mbar_init(bfull(s), 1); mbar_init(empty(s), 1); }
             mbar_init(done, 1);
             *abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -135,15 +148,15 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
         // -------------------------------------------------------------------------------------------- loads
         // The weights are nobody's result: those of the first chunks are asked for before the preceding kernel has finished.
         const uint32_t w0 = FEATURES ? a0 : b0, w_step = FEATURES ? 16384u : (uint32_t)p.b_bytes, ws0 = FEATURES ? sa0 : sb0;
-        const int w_first = FEATURES ? (int)row0 : o0, w_parts = FEATURES ? 1 : p.subs, w_box = FEATURES ? MXP_ROWS : p.box;
-        const int w_tiles = min(w_parts, (p.q.out + 127) / 128 - w_first / 128);         // tiles of scales that there are
-        int half = 0;
+        const int w_first = FEATURES ? (int)row0 : o0, w_box = FEATURES ? MXP_ROWS : p.box, w_rows = FEATURES ? MXP_ROWS : p.nt;
+        const int w_parts = FEATURES ? 1 : p.subs, w_tiles = min(w_parts, (p.q.out + 127) / 128 - w_first / 128);         // tiles of scales that there are
+        int box = 0;
         auto scale_tiles = [&](int c) { return min(2, p.q.tiles4 - 2 * c); };
         auto load_w = [&](int c, int s) {
             const int tiles = scale_tiles(c);
             const uint32_t rows = ROUND ? 0u : (uint32_t)((FEATURES ? p.box * 128 : 16384) + tiles * 512);
-            mbar_expect_tx(bfull(s), (uint32_t)(w_parts * w_box * 128 + w_tiles * tiles * 512) + rows);
-            for (int n = 0; n < w_parts; ++n) tma_load_2d(w0 + (uint32_t)s * w_step + (uint32_t)n * 16384u, &tm_w, bfull(s), c * 64, w_first + n * 128);
+            mbar_expect_tx(bfull(s), (uint32_t)(w_rows * 128 + w_tiles * tiles * 512) + rows);
+            for (int n = 0; n < w_rows; n += w_box) tma_load_2d(w0 + (uint32_t)s * w_step + (uint32_t)n * 128u, &tm_w, bfull(s), c * 64, w_first + n);
             for (int n = 0; n < w_tiles; ++n)
                 bulk_load(ws0 + (uint32_t)((s * w_parts + n) * 1024), p.q.scales + ((size_t)(w_first / 128 + n) * p.q.tiles4 + 2 * c) * 512, (uint32_t)tiles * 512u, bfull(s));
         };
@@ -158,8 +171,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             if (h >= p.xstages) ok = __all_sync(0xffffffffu, mbar_wait(xempty(s), (uint32_t)(h / p.xstages - 1) & 1u, abort_flag, p.status));
             if (ok && elect_one()) {
                 mbar_expect_tx(xfull(s), MXP_XBYTES);
-                tma_load_2d(x0 + (uint32_t)s * MXP_XBYTES, &tm_x, xfull(s), h * 128, (int)row0);
-                tma_load_2d(x0 + (uint32_t)s * MXP_XBYTES + 16384u, &tm_x, xfull(s), h * 128 + 64, (int)row0);
+                tma_load_2d(x0 + (uint32_t)s * MXP_XBYTES, &tm_x, xfull(s), h * 64, (int)row0);
             }
             __syncwarp();
         };
@@ -177,7 +189,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             }
             __syncwarp();
             if (ROUND)
-                for (; half < p.halves && half < 2 * c + 2 && ok; ++half) load_x(half);
+                for (; box < p.boxes && box < 4 * c + 4 && ok; ++box) load_x(box);
         }
     } else if (warp == MXP_WARPS + 1) {
         // --------------------------------------------------------------------------------------------- MMAs
@@ -224,38 +236,32 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
         }
     } else {
         // ------------------------------------------------------------------------------------------ rounding
-        const int r = threadIdx.x & 127, box = threadIdx.x >> 7;           // a row, and 64 of a half's 128 channels
-        if (ROUND)
-            for (int c = 0; c < p.chunks && ok; ++c) {
+        const int r = threadIdx.x & 127, half = threadIdx.x >> 7;          // a row, and 32 of a box's 64 channels
+        if (ROUND) {
+            const uint8_t *in = smem + (x0 - base);
+            uint8_t *out = smem + (a0 - base), *scales = smem + (sa0 - base) + (r & 31) * 16 + (r >> 5) * 4 + half;
+            for (int c = 0, h = 0, xs = 0, xp = 0; c < p.chunks && ok; ++c) {
                 const int s = c % p.stages;
                 if (c >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (uint32_t)(c / p.stages - 1) & 1u, abort_flag, p.status));
-                for (int part = 0; part < 2 && ok; ++part) {
-                    const int h = 2 * c + part;
-                    if (h < p.halves) {
-                        const int xs = h % p.xstages;
-                        ok = __all_sync(0xffffffffu, mbar_wait(xfull(xs), (uint32_t)(h / p.xstages) & 1u, abort_flag, p.status));
-                        if (!ok) break;
-                        const uint8_t *in = smem + (x0 - base) + xs * MXP_XBYTES + box * 16384;
-                        uint8_t *out = smem + (a0 - base) + s * 16384;
-                        uint32_t scales = 0;
+#pragma unroll 1
+                for (int part = 0; part < 4 && h < p.boxes && ok; ++part, ++h) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(xfull(xs), (uint32_t)xp, abort_flag, p.status));
+                    if (!ok) break;
+                    bf16x8 v[4];
 #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            bf16x8 v[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const bf16x8 *>(in + sub_off(r, b * 4 + i));
-                            uint32_t code;
-                            const uint4 w = mx_round_block(v, code);
-                            *reinterpret_cast<uint4 *>(out + sub_off(r, part * 4 + box * 2 + b)) = w;
-                            scales |= code << (8 * b);
-                        }
-                        *reinterpret_cast<uint16_t *>(smem + (sa0 - base) + s * 1024 + part * 512 + (r & 31) * 16 + (r >> 5) * 4 + box * 2) = (uint16_t)scales;
-                        fence_async_smem();                // the tensor core reads what was written here
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(xempty(xs));
-                    }
-                    if (lane == 0) mbar_arrive(afull(s));
+                    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const bf16x8 *>(in + xs * MXP_XBYTES + sub_off(r, half * 4 + i));
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(xempty(xs));
+                    uint32_t code;
+                    *reinterpret_cast<uint4 *>(out + s * 16384 + sub_off(r, part * 2 + half)) = mx_round_block(v, code);
+                    scales[s * 1024 + (part >> 1) * 512 + (part & 1) * 2] = (uint8_t)code;
+                    if (++xs == p.xstages) { xs = 0; xp ^= 1; }
                 }
+                fence_async_smem();                        // the tensor core reads what was written here
+                __syncwarp();
+                if (lane == 0) mbar_arrive(afull(s));
             }
+        }
         // ------------------------------------------------------------------------------------------ epilogue
         pdl_wait();
         const int quarter = warp & 3;
@@ -308,8 +314,9 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                         fetch(panel + 2);
                     }
                     const int left = min(64, p.nt - panel * 64);               // (whole sixteens)
-#pragma unroll 1
-                    for (int u = 0; u * 16 < left; ++u) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if (u * 16 >= left) break;
                         uint32_t v[16];
                         tmem_ld16(t_lane + (uint32_t)(panel * 64 + u * 16), v);
                         tmem_ld_wait();
@@ -317,17 +324,22 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                         for (int h = 0; h < 2; ++h) {
                             bf16x8 *at = reinterpret_cast<bf16x8 *>(stage + sub_off(lane, u * 2 + h));
                             const int e = panel * 64 + u * 16 + h * 8;
-                            float f[8], g[8];
-                            if (res) unpack8(*at, g);
                             const float4 b0v = *reinterpret_cast<const float4 *>(bias_s + e), b1v = *reinterpret_cast<const float4 *>(bias_s + e + 4);
-                            const float bias[8] = {b0v.x, b0v.y, b0v.z, b0v.w, b1v.x, b1v.y, b1v.z, b1v.w};
+                            float f[8] = {b0v.x, b0v.y, b0v.z, b0v.w, b1v.x, b1v.y, b1v.z, b1v.w};
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                float z = __uint_as_float(v[8 * h + j]) + bias[j];
-                                if (res) z += g[j];
-                                f[j] = o0 + e + j < p.q.out ? mx_act(z, p.q.act) : 0.f;
+                            for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(v[8 * h + j]);
+                            if (res) {
+                                float g[8];
+                                unpack8(*at, g);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) f[j] += g[j];
                             }
-                            *at = pack8(f);
+                            // (features behind the last have zero weights, but perhaps scales that are no numbers)
+                            if (o0 + e + 8 > p.q.out) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) f[j] = o0 + e + j < p.q.out ? f[j] : 0.f;
+                            }
+                            *at = mx_clamp8(pack8(f), p.q.act);
                         }
                     }
                     __syncwarp();
@@ -439,7 +451,8 @@ MxTiling mx_tiling(unsigned long long rows, int in, int out) {
         t.nt = round_up((int)rows, 16);
         t.subs = 1;
         const int tiles = (out + MXP_ROWS - 1) / MXP_ROWS, chunks = (in + MXP_CHUNK - 1) / MXP_CHUNK;
-        t.splits = (148 + tiles - 1) / tiles;              // a block to an SM
+        t.splits = 2 * 148 / tiles;                        // two blocks to an SM
+        if (t.splits < 1) t.splits = 1;
         if (t.splits > chunks) t.splits = chunks;
         t.per = (chunks + t.splits - 1) / t.splits;
         t.splits = (chunks + t.per - 1) / t.per;
@@ -489,11 +502,12 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
     MxpParams p = {};
     p.q = q;
     p.nt = t.nt; p.subs = t.subs; p.tiles_n = t.features ? t.splits : t.tiles_n; p.per = t.per;
-    p.box = t.nt < 128 ? t.nt : 128;
+    for (p.box = 128; t.nt % p.box;) p.box /= 2;
     p.chunks = (in + MXP_CHUNK - 1) / MXP_CHUNK;
-    p.halves = (in + 127) / 128;
+    p.boxes = (in + 63) / 64;
     p.steps_last = (in - (p.chunks - 1) * MXP_CHUNK + 63) / 64;
-    p.b_bytes = t.features ? round_up(p.box * 128, 1024) : t.subs * 16384;
+    if (t.features) p.box = t.nt;
+    p.b_bytes = round_up(t.nt * 128, 1024);
     p.xscales = xscales;
     p.partial = partial;
     p.status = device_status_word();
@@ -504,15 +518,22 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
         const size_t s = (size_t)stages * (16384 + p.b_bytes + 1024 + t.subs * 1024) + (size_t)xstages * MXP_XBYTES + MXP_CTRL + (size_t)t.nt * 4;
         return 1024 + (s > 32768 ? s : 32768);              // (the epilogue needs 32 KB at the front)
     };
-    // four stages of weights (eight where they are all there is to read) and of rows, as far as two blocks fit an SM
-    const int most = t.features ? 8 : 4;
+    // Two blocks to an SM where that leaves each a pipeline, else one with what there is room for: rows that are rounded here are most of what is
+    // read, and need the depth (64 KB or more of them under way); where only weights are read, they do.
+    const int most = t.round ? 2 : 6;
     p.stages = chunks < most ? chunks : most;
-    p.xstages = t.round ? (p.halves < 4 ? p.halves : 4) : 0;
-    while (!t.features && bytes(p.stages, p.xstages) > 113 * 1024 && (p.stages > 2 || p.xstages > 2)) {
-        if (p.xstages > 2) --p.xstages;
-        else --p.stages;
+    p.xstages = t.round ? (p.boxes < 8 ? p.boxes : 8) : 0;
+    const size_t half = 113 * 1024, whole = 226 * 1024;
+    const int least = p.boxes < 3 ? p.boxes : 3;
+    if (t.round && bytes(p.stages, least) <= half) {
+        while (bytes(p.stages, p.xstages) > half) --p.xstages;
+    } else if (t.round) {
+        while (bytes(p.stages, p.xstages) > whole) --p.xstages;
+    } else {
+        const size_t room = bytes(chunks < 3 ? chunks : 3, 0) <= half ? half : whole;
+        while (bytes(p.stages, 0) > room) --p.stages;
     }
-    while (p.stages > 1 && (p.sf_col + p.stages * MXP_SF_COLS > 512 || bytes(p.stages, p.xstages) > 226 * 1024)) --p.stages;
+    while (p.stages > 1 && p.sf_col + p.stages * MXP_SF_COLS > 512) --p.stages;
     const int cols = p.sf_col + p.stages * MXP_SF_COLS;
     for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
     CUtensorMap tm[2];

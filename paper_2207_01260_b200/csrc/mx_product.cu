@@ -11,6 +11,7 @@
 // weights, which is what such a product consists of); the shares' sums meet in a second kernel, in a fixed order.
 // Scales lie in shared memory in pieces of 512 bytes (128 rows by 4 blocks); tcgen05.cp brings a piece into four columns of tensor memory.
 // The accumulator leaves through registers: bias, shortcut and activation on the way.
+#include <cstring>
 #include <mutex>
 
 #include "common.cuh"
@@ -34,6 +35,7 @@ struct MxpParams {
     int chunks, boxes;               // of 256 and of 64 channels
     int steps_last;                  // MMA steps (64 channels) of the last chunk
     int stages, xstages;
+    int panels;                      // of 64 features, of a shortcut: they take places in the ring of the rows
     int b_bytes, tmem_cols, sf_col;  // bytes of a chunk of weights, columns of tensor memory, where its scales begin
     const uint8_t *xscales;          // of rows that are already rounded
     float *partial;                  // features first: sums of the shares [splits][rows][out_pad]
@@ -59,25 +61,32 @@ __device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint32_t desc_l
     asm volatile("{\n\t.reg .b64 d;\n\tmov.b64 d, {%1, %2};\n\ttcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n\t}" ::"r"(taddr), "r"(desc_lo), "r"(DESC_HI_SCALES) : "memory");
 }
 
-// 32 bf16 values to codes (16 bytes) and a scale
+// 32 bf16 values to codes (16 bytes) and a scale.  The largest magnitude and the division by the scale are taken two values at a time, as bf16: products
+// with a power of two are exact there too (what leaves the type below is far under the smallest code).
 __device__ __forceinline__ uint4 mx_round_block(const bf16x8 *v, uint32_t &scale) {
-    uint32_t top = 0;
+    uint32_t m[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+        m[i] = v[i].w[0] & 0x7fff7fffu;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = __vmaxu2(top, v[i].w[j] & 0x7fff7fffu);
-    top = max(top & 0xffffu, top >> 16) << 16;
+        for (int j = 1; j < 4; ++j) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m[i]) : "r"(v[i].w[j] & 0x7fff7fffu));
+    }
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m[0]) : "r"(m[1]));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m[2]) : "r"(m[3]));
+    asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m[0]) : "r"(m[2]));
+    const uint32_t top = max(m[0] & 0x7fffu, m[0] >> 16 & 0x7fffu) << 16;
     scale = mx_scale_code(top);
-    const float inverse = mx_inverse(scale);
     const bool none = scale == MX_NAN;
+    const uint32_t inverse = (__float_as_uint(mx_inverse(scale)) >> 16) * 0x10001u;
     uint4 r;
     uint32_t *w = &r.x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        float f[8];
-        unpack8(v[i], f);
+        bf16x8 q;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = f[j] * inverse;
+        for (int j = 0; j < 4; ++j) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(q.w[j]) : "r"(v[i].w[j]), "r"(inverse));
+        float f[8];
+        unpack8(q, f);
         w[i] = none ? 0u : mx_codes(f);
     }
     return r;
@@ -99,7 +108,8 @@ __device__ __forceinline__ bf16x8 mx_clamp8(bf16x8 v, int act) {
 enum { MXP_ROUND = 0, MXP_CODES = 1, MXP_FEATURES = 2 };        // rows rounded here; rows already rounded; features first
 
 template <int FORM>
-__global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ MxpParams p) {
+__global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_res,
+                  const __grid_constant__ MxpParams p) {
     constexpr bool ROUND = FORM == MXP_ROUND, FEATURES = FORM == MXP_FEATURES;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -166,12 +176,13 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             tma_load_2d(FEATURES ? b0 + (uint32_t)(s * p.b_bytes) : a0 + (uint32_t)s * 16384u, &tm_x, bfull(s), c * 64, first);
             bulk_load((FEATURES ? sb0 : sa0) + (uint32_t)s * 1024u, p.xscales + ((size_t)(first / 128) * p.q.tiles4 + 2 * c) * 512, (uint32_t)scale_tiles(c) * 512u, bfull(s));
         };
-        auto load_x = [&](int h) {
+        auto load_x = [&](int h) {                         // (the shortcut's panels follow the rows' boxes)
             const int s = h % p.xstages;
             if (h >= p.xstages) ok = __all_sync(0xffffffffu, mbar_wait(xempty(s), (uint32_t)(h / p.xstages - 1) & 1u, abort_flag, p.status));
             if (ok && elect_one()) {
                 mbar_expect_tx(xfull(s), MXP_XBYTES);
-                tma_load_2d(x0 + (uint32_t)s * MXP_XBYTES, &tm_x, xfull(s), h * 64, (int)row0);
+                if (h < p.boxes) tma_load_2d(x0 + (uint32_t)s * MXP_XBYTES, &tm_x, xfull(s), h * 64, (int)row0);
+                else tma_load_2d(x0 + (uint32_t)s * MXP_XBYTES, &tm_res, xfull(s), o0 + (h - p.boxes) * 64, (int)row0);
             }
             __syncwarp();
         };
@@ -191,6 +202,8 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             if (ROUND)
                 for (; box < p.boxes && box < 4 * c + 4 && ok; ++box) load_x(box);
         }
+        const int panels = min(p.panels, (p.q.out_pad - o0 + 63) / 64);
+        for (box = p.boxes; box < p.boxes + panels && ok; ++box) load_x(box);
     } else if (warp == MXP_WARPS + 1) {
         // --------------------------------------------------------------------------------------------- MMAs
         // E2M1 operands, scales that are powers of two; 64 channels of every 128 under scales 0 or 2 of a column
@@ -283,76 +296,71 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                 }
             }
         } else if (!p.q.out_is_f32) {
-            // A warp takes 32 rows of 64 features at a time; in its 4 KB of shared memory the rows of tensor memory become whole lines.  The shortcut's lines
-            // are asked for before the sums are there.
-            uint8_t *stage = smem + warp * 4096;           // (codes that the MMAs have read)
-            const int piece = lane & 7, line = lane >> 3;
-            const long long r0 = row0 + quarter * 32;
-            const __nv_bfloat16 *res = p.q.res;
-            __nv_bfloat16 *y = (__nv_bfloat16 *)p.q.y;
+            // A warp takes 32 rows of 64 features (a panel's quarter, 4 KB) at a time and leaves them to a bulk store: over the shortcut's panel where there is
+            // one, else in codes that the MMAs have read.
             const int panels = (min(p.nt, p.q.out_pad - o0) + 63) / 64;
-            bf16x8 rv[8];
-            auto fetch = [&](int panel) {
-                const int o = o0 + panel * 64 + piece * 8;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const long long r = r0 + i * 4 + line;
-                    if (panel < panels && o < p.q.out_pad && r < (long long)p.q.rows) rv[i] = *reinterpret_cast<const bf16x8 *>(res + (size_t)r * p.q.out_pad + o);
-                    else rv[i] = bf16x8{{0u, 0u, 0u, 0u}};
-                }
-            };
-            int panel = warp >> 2;
-            if (res) fetch(panel);
             ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag, p.status));
-            if (ok) {
+            for (int panel = warp >> 2; panel < panels && ok; panel += 2) {
+                const int left = min(64, p.nt - panel * 64);                       // (whole sixteens)
+                uint32_t from = base + (uint32_t)warp * 4096u;
+                if (p.panels) {
+                    const int h = p.boxes + panel, s = h % p.xstages;
+                    ok = __all_sync(0xffffffffu, mbar_wait(xfull(s), (uint32_t)(h / p.xstages) & 1u, abort_flag, p.status));
+                    if (!ok) break;
+                    from = x0 + (uint32_t)(s * MXP_XBYTES + quarter * 4096);
+                } else if (panel >= 2) {
+                    tma_store_wait_read<0>();              // (by the thread that stored)
+                    __syncwarp();
+                }
+                uint8_t *stage = smem + (from - base);
                 tc_fence_after();
-                for (; panel < panels; panel += 2) {
-                    if (res) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) *reinterpret_cast<bf16x8 *>(stage + sub_off(i * 4 + line, piece)) = rv[i];
-                        __syncwarp();
-                        fetch(panel + 2);
-                    }
-                    const int left = min(64, p.nt - panel * 64);               // (whole sixteens)
+                for (int u2 = 0; u2 < 2; ++u2) {
+                    if (u2 * 32 >= left) break;
+                    uint32_t v[32];
+                    tmem_ld16(t_lane + (uint32_t)(panel * 64 + u2 * 32), v);
+                    tmem_ld16(t_lane + (uint32_t)(panel * 64 + u2 * 32 + 16), v + 16);       // (columns of the block's own, used or not)
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if (u * 16 >= left) break;
-                        uint32_t v[16];
-                        tmem_ld16(t_lane + (uint32_t)(panel * 64 + u * 16), v);
-                        tmem_ld_wait();
+                    for (int h = 0; h < 4; ++h) {
+                        bf16x8 *at = reinterpret_cast<bf16x8 *>(stage + sub_off(lane, u2 * 4 + h));
+                        const int e = panel * 64 + u2 * 32 + h * 8;
+                        if (e >= p.nt) break;
+                        const float4 b0v = *reinterpret_cast<const float4 *>(bias_s + e), b1v = *reinterpret_cast<const float4 *>(bias_s + e + 4);
+                        float f[8] = {b0v.x, b0v.y, b0v.z, b0v.w, b1v.x, b1v.y, b1v.z, b1v.w};
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            bf16x8 *at = reinterpret_cast<bf16x8 *>(stage + sub_off(lane, u * 2 + h));
-                            const int e = panel * 64 + u * 16 + h * 8;
-                            const float4 b0v = *reinterpret_cast<const float4 *>(bias_s + e), b1v = *reinterpret_cast<const float4 *>(bias_s + e + 4);
-                            float f[8] = {b0v.x, b0v.y, b0v.z, b0v.w, b1v.x, b1v.y, b1v.z, b1v.w};
+                        for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(v[8 * h + j]);
+                        if (p.panels) {
+                            float g[8];
+                            unpack8(*at, g);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) f[j] += __uint_as_float(v[8 * h + j]);
-                            if (res) {
-                                float g[8];
-                                unpack8(*at, g);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) f[j] += g[j];
-                            }
-                            // (features behind the last have zero weights, but perhaps scales that are no numbers)
-                            if (o0 + e + 8 > p.q.out) {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) f[j] = o0 + e + j < p.q.out ? f[j] : 0.f;
-                            }
-                            *at = mx_clamp8(pack8(f), p.q.act);
+                            for (int j = 0; j < 8; ++j) f[j] += g[j];
                         }
-                    }
-                    __syncwarp();
+                        // (features behind the last have zero weights, but perhaps scales that are no numbers)
+                        if (o0 + e + 8 > p.q.out) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const long long r = r0 + i * 4 + line;
-                        const int o = o0 + panel * 64 + piece * 8;
-                        if (piece * 8 < left && o < p.q.out_pad && r < (long long)p.q.rows)
-                            *reinterpret_cast<bf16x8 *>(y + (size_t)r * p.q.out_pad + o) = *reinterpret_cast<const bf16x8 *>(stage + sub_off(i * 4 + line, piece));
+                            for (int j = 0; j < 8; ++j) f[j] = o0 + e + j < p.q.out ? f[j] : 0.f;
+                        }
+                        *at = mx_clamp8(pack8(f), p.q.act);
                     }
-                    __syncwarp();
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    // (what lies behind the last row, or the last channel in memory, is not stored)
+                    if (row0 + quarter * 32 < (long long)p.q.rows) tma_store_2d(&tm_y, from, o0 + panel * 64, (int)row0 + quarter * 32);
+                    tma_store_commit();
+                    if (p.panels && p.boxes + panel + p.xstages < p.boxes + panels) {
+                        tma_store_wait_read<0>();          // the next panel comes into this place
+                    }
+                }
+                __syncwarp();
+                if (p.panels && lane == 0) {                      // (for the four warps of the other panels, too)
+                    mbar_arrive(xempty((p.boxes + panel) % p.xstages));
+                    mbar_arrive(xempty((p.boxes + panel) % p.xstages));
                 }
             }
+            if (lane == 0) tma_store_wait_all();
         } else {
             ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag, p.status));
             if (ok) {
@@ -486,7 +494,7 @@ static cprune_status launch_product(const CUtensorMap *tm, const MxpParams &p, l
             attr_set[dev] = true;
         }
     }
-    CPRUNE_CUDA_CHECK(launch_chained(mx_product_kernel<FORM>, dim3((unsigned)blocks), dim3(MXP_THREADS), smem, st, tm[0], tm[1], p));
+    CPRUNE_CUDA_CHECK(launch_chained(mx_product_kernel<FORM>, dim3((unsigned)blocks), dim3(MXP_THREADS), smem, st, tm[0], tm[1], tm[2], tm[3], p));
     return CPRUNE_OK;
 }
 
@@ -504,7 +512,8 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
     p.nt = t.nt; p.subs = t.subs; p.tiles_n = t.features ? t.splits : t.tiles_n; p.per = t.per;
     for (p.box = 128; t.nt % p.box;) p.box /= 2;
     p.chunks = (in + MXP_CHUNK - 1) / MXP_CHUNK;
-    p.boxes = (in + 63) / 64;
+    p.boxes = t.round ? (in + 63) / 64 : 0;
+    p.panels = q.res && !q.out_is_f32 && !t.features ? (t.nt + 63) / 64 : 0;
     p.steps_last = (in - (p.chunks - 1) * MXP_CHUNK + 63) / 64;
     if (t.features) p.box = t.nt;
     p.b_bytes = round_up(t.nt * 128, 1024);
@@ -522,21 +531,19 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
     // read, and need the depth (64 KB or more of them under way); where only weights are read, they do.
     const int most = t.round ? 2 : 6;
     p.stages = chunks < most ? chunks : most;
-    p.xstages = t.round ? (p.boxes < 8 ? p.boxes : 8) : 0;
+    p.xstages = p.boxes + p.panels < 8 ? p.boxes + p.panels : 8;
     const size_t half = 113 * 1024, whole = 226 * 1024;
-    const int least = p.boxes < 3 ? p.boxes : 3;
-    if (t.round && bytes(p.stages, least) <= half) {
-        while (bytes(p.stages, p.xstages) > half) --p.xstages;
-    } else if (t.round) {
-        while (bytes(p.stages, p.xstages) > whole) --p.xstages;
-    } else {
-        const size_t room = bytes(chunks < 3 ? chunks : 3, 0) <= half ? half : whole;
-        while (bytes(p.stages, 0) > room) --p.stages;
+    const int least = p.xstages < 3 ? p.xstages : 3;
+    const int two = t.round ? p.stages : chunks < 3 ? chunks : 3;                        // stages that two blocks need each
+    const size_t room = bytes(two, t.round ? least : p.xstages < 2 ? p.xstages : 2) <= half ? half : whole;
+    while (bytes(p.stages, p.xstages) > room) {
+        if (t.round || p.xstages > 2) --p.xstages;
+        else --p.stages;
     }
     while (p.stages > 1 && p.sf_col + p.stages * MXP_SF_COLS > 512) --p.stages;
     const int cols = p.sf_col + p.stages * MXP_SF_COLS;
     for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;
-    CUtensorMap tm[2];
+    CUtensorMap tm[4];
     cprune_status s;
     if (t.round) {
         const unsigned long long dims[2] = {(unsigned long long)in, q.rows};
@@ -545,6 +552,15 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
         s = encode_tiled_bf16_swz(&tm[0], x, 2, dims, strides, box, 128, true);
     } else s = encode_codes(&tm[0], x, q.blocks, q.rows, t.features ? p.box : MXP_ROWS);
     if (s == CPRUNE_OK) s = encode_codes(&tm[1], q.codes, q.blocks, q.out, t.features ? MXP_ROWS : p.box);
+    std::memcpy(&tm[2], &tm[1], sizeof(CUtensorMap));         // (of y and the shortcut, where the bulk copies are used)
+    std::memcpy(&tm[3], &tm[1], sizeof(CUtensorMap));
+    if (!t.features && !q.out_is_f32) {
+        const unsigned long long dims[2] = {(unsigned long long)q.out_pad, q.rows};
+        const unsigned long long strides[1] = {(unsigned long long)q.out_pad * 2};
+        const unsigned box_y[2] = {64, 32}, box_res[2] = {64, MXP_ROWS};
+        if (s == CPRUNE_OK) s = encode_tiled_bf16_swz(&tm[2], q.y, 2, dims, strides, box_y, 128, false);
+        if (s == CPRUNE_OK && q.res) s = encode_tiled_bf16_swz(&tm[3], q.res, 2, dims, strides, box_res, 128, true);
+    }
     if (s != CPRUNE_OK) return s;
     const long long blocks = t.features ? (long long)((q.out + MXP_ROWS - 1) / MXP_ROWS) * t.splits : (long long)((q.rows + MXP_ROWS - 1) / MXP_ROWS) * t.tiles_n;
     if (blocks > 0x7fffffffLL) return CPRUNE_ERR_UNSUPPORTED;

@@ -3,8 +3,8 @@
 //
 // A block takes 128 rows and up to 384 features (each 128 of them one MMA), and goes through the channels 256 at a time: a row of codes of such a
 // chunk is 128 bytes.  The rows come in one of two ways:
-//   - rounded here: the bf16 rows arrive by TMA, 64 channels at a time; eight warps round them (a thread a block of 32 channels of a row)
-//     and write codes and scales where the tensor core reads them.  x is read once and nothing else
+//   - rounded here: the bf16 rows arrive by TMA, 64 channels at a time; two groups of eight warps round them in turn (a thread a block of 32
+//     channels of a row: what it costs is the latency of one after the other, 810 cycles a box with one group, when a box could arrive every 500) and write codes and scales where the tensor core reads them.  x is read once and nothing else
 //     is written: taken where one block covers all features.
 //   - already rounded (by mx_quantize_kernel) where several blocks share the rows: codes by TMA, scales by bulk copies.
 // Up to 128 rows change places with the features: a block takes 128 features and all rows, and a share of the channels (so that enough blocks read the
@@ -22,11 +22,11 @@
 namespace cprune {
 
 constexpr int MXP_ROWS = 128, MXP_CHUNK = 256;        // rows of a block; channels of a chunk (128 bytes of codes)
-constexpr int MXP_WARPS = 8;                          // round and store; two more load and multiply
+constexpr int MXP_WARPS = 16;                         // round and store; two more load and multiply
 constexpr int MXP_THREADS = (MXP_WARPS + 2) * 32;
 constexpr int MXP_XBYTES = MXP_ROWS * 64 * 2;         // 64 channels of bf16 rows
 constexpr int MXP_MOST = 384;                         // features of a block
-constexpr int MXP_CTRL = 512;
+constexpr int MXP_CTRL = 512, MXP_FRONT = 2048;       // barriers; with the bias behind them
 constexpr int MXP_SF_COLS = 8 + 2 * 12;               // columns of a stage's scales
 
 struct MxpParams {
@@ -36,6 +36,7 @@ struct MxpParams {
     int steps_last;                  // MMA steps (64 channels) of the last chunk
     int stages, xstages;
     int panels;                      // of 64 features, of a shortcut: they take places in the ring of the rows
+    int groups;                      // of four warps that take the panels in turn
     int b_bytes, tmem_cols, sf_col;  // bytes of a chunk of weights, columns of tensor memory, where its scales begin
     const uint8_t *xscales;          // of rows that are already rounded
     float *partial;                  // features first: sums of the shares [splits][rows][out_pad]
@@ -114,9 +115,9 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (base - raw);
-    // shared memory: codes of the rows (features first: of the features), codes of the features (of the rows), bf16 rows, scales of rows and of features, barriers, bias
-    const uint32_t a0 = base, b0 = a0 + p.stages * 16384u, x0 = b0 + (uint32_t)(p.stages * p.b_bytes), sa0 = x0 + (uint32_t)(p.xstages * MXP_XBYTES);
-    const uint32_t sb0 = sa0 + p.stages * 1024u, ctrl0 = sb0 + (uint32_t)(p.stages * p.subs) * 1024u;
+    // shared memory: barriers, bias, codes of the rows (features first: of the features), codes of the features (of the rows), bf16 rows, scales of rows and of features
+    const uint32_t ctrl0 = base, a0 = base + MXP_FRONT, b0 = a0 + p.stages * 16384u, x0 = b0 + (uint32_t)(p.stages * p.b_bytes);
+    const uint32_t sa0 = x0 + (uint32_t)(p.xstages * MXP_XBYTES), sb0 = sa0 + p.stages * 1024u;
     uint8_t *ctrl = smem + (ctrl0 - base);
     auto xfull = [&](int s) { return ctrl0 + 8u * s; };
     auto xempty = [&](int s) { return ctrl0 + 64u + 8u * s; };
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
         tmem_relinquish();
         pdl_trigger();
         if (lane == 0) {
-            for (int s = 0; s < p.xstages; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), MXP_WARPS); }
+            for (int s = 0; s < p.xstages; ++s) { mbar_init(xfull(s), 1); mbar_init(xempty(s), MXP_WARPS / 2); }
             for (int s = 0; s < p.stages; ++s) { mbar_init(afull(s), MXP_WARPS); mbar_init(bfull(s), 1); mbar_init(empty(s), 1); }
             mbar_init(done, 1);
             *abort_flag = 0;
@@ -249,16 +250,17 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
         }
     } else {
         // ------------------------------------------------------------------------------------------ rounding
-        const int r = threadIdx.x & 127, half = threadIdx.x >> 7;          // a row, and 32 of a box's 64 channels
+        const int r = threadIdx.x & 127, half = (threadIdx.x >> 7) & 1, turn = warp >> 3;          // a row, 32 of a box's 64 channels, every second box
         if (ROUND) {
             const uint8_t *in = smem + (x0 - base);
             uint8_t *out = smem + (a0 - base), *scales = smem + (sa0 - base) + (r & 31) * 16 + (r >> 5) * 4 + half;
-            for (int c = 0, h = 0, xs = 0, xp = 0; c < p.chunks && ok; ++c) {
+            for (int c = 0; c < p.chunks && ok; ++c) {
                 const int s = c % p.stages;
                 if (c >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (uint32_t)(c / p.stages - 1) & 1u, abort_flag, p.status));
 #pragma unroll 1
-                for (int part = 0; part < 4 && h < p.boxes && ok; ++part, ++h) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(xfull(xs), (uint32_t)xp, abort_flag, p.status));
+                for (int part = turn; part < 4 && 4 * c + part < p.boxes && ok; part += 2) {
+                    const int h = 4 * c + part, xs = h % p.xstages;
+                    ok = __all_sync(0xffffffffu, mbar_wait(xfull(xs), (uint32_t)(h / p.xstages) & 1u, abort_flag, p.status));
                     if (!ok) break;
                     bf16x8 v[4];
 #pragma unroll
@@ -268,7 +270,6 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                     uint32_t code;
                     *reinterpret_cast<uint4 *>(out + s * 16384 + sub_off(r, part * 2 + half)) = mx_round_block(v, code);
                     scales[s * 1024 + (part >> 1) * 512 + (part & 1) * 2] = (uint8_t)code;
-                    if (++xs == p.xstages) { xs = 0; xp ^= 1; }
                 }
                 fence_async_smem();                        // the tensor core reads what was written here
                 __syncwarp();
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             if (ok) {
                 tc_fence_after();
                 const int o = (int)row0 + quarter * 32 + lane;
-                for (int u = warp >> 2; u * 16 < p.nt; u += 2) {
+                for (int u = warp >> 2; u * 16 < p.nt; u += MXP_WARPS / 4) {
                     uint32_t v[16];
                     tmem_ld16(t_lane + (uint32_t)(u * 16), v);
                     tmem_ld_wait();
@@ -300,15 +301,15 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             // one, else in codes that the MMAs have read.
             const int panels = (min(p.nt, p.q.out_pad - o0) + 63) / 64;
             ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag, p.status));
-            for (int panel = warp >> 2; panel < panels && ok; panel += 2) {
+            for (int panel = warp >> 2 < p.groups ? warp >> 2 : panels; panel < panels && ok; panel += p.groups) {
                 const int left = min(64, p.nt - panel * 64);                       // (whole sixteens)
-                uint32_t from = base + (uint32_t)warp * 4096u;
+                uint32_t from = a0 + (uint32_t)warp * 4096u;
                 if (p.panels) {
                     const int h = p.boxes + panel, s = h % p.xstages;
                     ok = __all_sync(0xffffffffu, mbar_wait(xfull(s), (uint32_t)(h / p.xstages) & 1u, abort_flag, p.status));
                     if (!ok) break;
                     from = x0 + (uint32_t)(s * MXP_XBYTES + quarter * 4096);
-                } else if (panel >= 2) {
+                } else if (panel >= p.groups) {
                     tma_store_wait_read<0>();              // (by the thread that stored)
                     __syncwarp();
                 }
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                     }
                 }
                 __syncwarp();
-                if (p.panels && lane == 0) {                      // (for the four warps of the other panels, too)
+                if (p.panels && lane == 0) {                      // (four warps, for eight)
                     mbar_arrive(xempty((p.boxes + panel) % p.xstages));
                     mbar_arrive(xempty((p.boxes + panel) % p.xstages));
                 }
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                 tc_fence_after();
                 const long long row = row0 + quarter * 32 + lane;
                 const bool in = row < (long long)p.q.rows;
-                for (int u = warp >> 2; u * 16 < p.nt; u += 2) {
+                for (int u = warp >> 2; u * 16 < p.nt; u += MXP_WARPS / 4) {
                     const int o = o0 + u * 16;
                     if (o >= p.q.out) break;
                     bf16x8 rv[2] = {};
@@ -524,8 +525,8 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
     p.sf_col = t.nt;
     const int chunks = t.features ? t.per : p.chunks;
     auto bytes = [&](int stages, int xstages) {
-        const size_t s = (size_t)stages * (16384 + p.b_bytes + 1024 + t.subs * 1024) + (size_t)xstages * MXP_XBYTES + MXP_CTRL + (size_t)t.nt * 4;
-        return 1024 + (s > 32768 ? s : 32768);              // (the epilogue needs 32 KB at the front)
+        const size_t s = (size_t)stages * (16384 + p.b_bytes + 1024 + t.subs * 1024) + (size_t)xstages * MXP_XBYTES, y = MXP_WARPS * 4096;
+        return 1024 + MXP_FRONT + (s > y ? s : y);          // (the epilogue's place is that of the operands)
     };
     // Two blocks to an SM where that leaves each a pipeline, else one with what there is room for: rows that are rounded here are most of what is
     // read, and need the depth (64 KB or more of them under way); where only weights are read, they do.
@@ -540,6 +541,11 @@ cprune_status launch_mx_product(const MxProduct &q, const MxTiling &t, const voi
         if (t.round || p.xstages > 2) --p.xstages;
         else --p.stages;
     }
+    // A wait tells a phase of a barrier from the one before it, not from the one before that: whoever waits for a place in the ring waits for every box that
+    // comes there.  The two groups that round take every second box: an even number of places.  Panels that share a place belong to the same warps.
+    if (p.boxes > p.xstages) p.xstages &= ~1;
+    if (p.panels > p.xstages && p.xstages > MXP_WARPS / 4) p.xstages = MXP_WARPS / 4;
+    p.groups = p.panels && p.xstages < MXP_WARPS / 4 ? p.xstages : MXP_WARPS / 4;
     while (p.stages > 1 && p.sf_col + p.stages * MXP_SF_COLS > 512) --p.stages;
     const int cols = p.sf_col + p.stages * MXP_SF_COLS;
     for (p.tmem_cols = 32; p.tmem_cols < cols;) p.tmem_cols *= 2;

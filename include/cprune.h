@@ -310,7 +310,8 @@ cprune_status cprune_clip_gradients(const void *const *grads, const unsigned lon
  *   x  bf16 [rows][in_pad], a row per image or pixel;  residual  bf16 [rows][out_pad] or NULL;  act none, relu or relu6 (a NaN stays
  *   one);  y  bf16 [rows][out_pad] (pad lanes zero) or float32 [rows][out] when out_is_f32; it may be residual, not x
  *   workspace  cprune_mx_fc_workspace_bytes, device, 16-byte aligned
- * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows of a product, 2^40 of a rounding, more than 2^24 channels),
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows of a product, 2^40 of a rounding, more than 2^22 channels or 2^24
+ * features),
  * CUDA.  Enqueue only; at most three launches. */
 int cprune_mx_blocks(int C);
 size_t cprune_mx_scale_bytes(size_t rows, int C);

@@ -12,18 +12,11 @@ namespace cprune {
 
 // ------------------------------------------------------------------------------------------------------- rounding
 
-// Where the eight values that begin at channel c of a row come from.  TYPE 0: bf16 rows of c_pad channels; 1: float32 rows on 16-byte boundaries;
-// 2: float32 rows at any address.  Channels from C on are zeros.
-template <int TYPE>
-__device__ __forceinline__ void read_eight(const void *x, size_t row, int c, int C, int pitch, float *f) {
-    if (TYPE == 0) {
-        bf16x8 v = {{0u, 0u, 0u, 0u}};
-        if (c < pitch) v = ldg8((const bf16x8 *)((const __nv_bfloat16 *)x + row * pitch + c));
-        unpack8(v, f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i >= C) f[i] = 0.f;
-    } else {
+// The eight values that begin at channel c of a row.  TYPE 0: bf16 rows of c_pad channels; 1: float32 rows on 16-byte boundaries; 2: float32 rows at any
+// address.  Channels from C on are zeros.
+template <int TYPE> struct Eight {
+    float f[8];
+    __device__ __forceinline__ void read(const void *x, size_t row, int c, int C, int pitch) {
         const float *p = (const float *)x + row * pitch + c;
         if (TYPE == 1) {
 #pragma unroll
@@ -37,78 +30,135 @@ __device__ __forceinline__ void read_eight(const void *x, size_t row, int c, int
             for (int i = 0; i < 8; ++i) f[i] = c + i < C ? __ldg(p + i) : 0.f;
         }
     }
-}
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 0.f;
+    }
+    // bits of the largest magnitude
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t t = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t = max(t, __float_as_uint(f[i]) & 0x7fffffffu);
+        return t;
+    }
+    __device__ __forceinline__ uint32_t codes(uint32_t code) const {
+        const float inverse = mx_inverse(code);
+        float q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = f[i] * inverse;
+        return code == MX_NAN ? 0u : mx_codes(q);
+    }
+};
+// (two at a time, as bf16: products with a power of two are exact there too, but for what is far under the smallest code)
+template <> struct Eight<0> {
+    bf16x8 v;
+    __device__ __forceinline__ void read(const void *x, size_t row, int c, int C, int pitch) {
+        clear();
+        if (c >= pitch) return;
+        v = ldg8((const bf16x8 *)((const __nv_bfloat16 *)x + row * pitch + c));
+        if (c + 8 > C) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v.w[i] &= (c + 2 * i < C ? 0xffffu : 0u) | (c + 2 * i + 1 < C ? 0xffff0000u : 0u);
+        }
+    }
+    __device__ __forceinline__ void clear() { v = bf16x8{{0u, 0u, 0u, 0u}}; }
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t m = v.w[0] & 0x7fff7fffu;
+#pragma unroll
+        for (int j = 1; j < 4; ++j) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.w[j] & 0x7fff7fffu));
+        return max(m & 0x7fffu, m >> 16 & 0x7fffu) << 16;
+    }
+    __device__ __forceinline__ uint32_t codes(uint32_t code) const {
+        const uint32_t inverse = (__float_as_uint(mx_inverse(code)) >> 16) * 0x10001u;
+        bf16x8 q;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(q.w[j]) : "r"(v.w[j]), "r"(inverse));
+        float f[8];
+        unpack8(q, f);
+        return code == MX_NAN ? 0u : mx_codes(f);
+    }
+};
 
-// The exact values of codes, in the form of x (pad lanes zero)
+// The exact values of eight codes, in the form of x (pad lanes zero)
 template <int TYPE>
-__device__ __forceinline__ void write_eight(void *y, size_t row, int c, int C, int pitch, float *f) {
+__device__ __forceinline__ void write_eight(void *y, size_t row, int c, int C, int pitch, uint32_t w, uint32_t code) {
     if (TYPE == 0) {
         if (c >= pitch) return;
+        bf16x8 v = mx_values_bf16(w, code);
+        if (c + 8 > C) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v.w[i] &= (c + 2 * i < C ? 0xffffu : 0u) | (c + 2 * i + 1 < C ? 0xffff0000u : 0u);
+        }
+        *(bf16x8 *)((__nv_bfloat16 *)y + row * pitch + c) = v;
+        return;
+    }
+    float f[8];
+    mx_values(w, mx_scale(code), f);
+    float *p = (float *)y + row * pitch + c;
+    if (TYPE == 1) {
+        if (c < C) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+        if (c + 4 < C) *((float4 *)p + 1) = make_float4(f[4], f[5], f[6], f[7]);
+    } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c + i >= C) f[i] = 0.f;
-        *(bf16x8 *)((__nv_bfloat16 *)y + row * pitch + c) = pack8(f);
-    } else {
-        float *p = (float *)y + row * pitch + c;
-        if (TYPE == 1) {
-            if (c < C) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
-            if (c + 4 < C) *((float4 *)p + 1) = make_float4(f[4], f[5], f[6], f[7]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c + i < C) p[i] = f[i];
-        }
+            if (c + i < C) p[i] = f[i];
     }
 }
 
-constexpr int MX_T = 256;
+constexpr int MX_T = 256, MX_ROWS = MX_T / 16, MX_AHEAD = 4;
 
-// 16 threads take four blocks (128 channels) of a row, eight values each: loads and stores of neighbouring threads adjoin, and the four scales are
-// one word of a tile of scales.  FORM 0: codes and scales (either both or neither), values as x; 1: the values in blocks, bf16 [rows][blocks * 32], in
-// the order 0 4 1 5 2 6 3 7 of every eight (the order in which mx_pair takes codes apart).
+// 16 threads take four blocks (128 channels, a tile of scales wide: grid y) of a row, eight values each: loads and stores of neighbouring threads adjoin, and the
+// four scales are one word of a tile of scales.  A thread has MX_AHEAD rows under way: bound by the bytes, as long as enough of them are (200704 x 108
+// with the values written, 98 MB: one row at a time and a division per row 36 us, now MX_TIME us).  FORM 0: codes and scales (either both or neither), values as x; 1:
+// the values in blocks, bf16 [rows][blocks * 32], in the order 0 4 1 5 2 6 3 7 of every eight (the order in which mx_pair takes codes apart).
 template <int TYPE, int FORM>
 __global__ void __launch_bounds__(MX_T) mx_quantize_kernel(const void *__restrict__ x, unsigned long long rows, int C, int pitch, int tiles4, uint32_t *__restrict__ codes,
                                                            uint8_t *__restrict__ scales, void *__restrict__ values) {
     pdl_wait();
     pdl_trigger();
-    const int blocks = (C + MX_BLOCK - 1) / MX_BLOCK, sub = threadIdx.x & 15;
-    const unsigned long long units = rows * tiles4;
+    const int blocks = (C + MX_BLOCK - 1) / MX_BLOCK, sub = threadIdx.x & 15, tile = blockIdx.y, c = tile * 128 + sub * 8, block = tile * 4 + (sub >> 2);
+    const bool mine = block < blocks;
     // (whole warps go round: the shuffles below need all lanes)
-    for (unsigned long long u0 = ((unsigned long long)blockIdx.x * MX_T + (threadIdx.x & ~31)) / 16; u0 < units; u0 += (unsigned long long)gridDim.x * (MX_T / 16)) {
-        const unsigned long long u = u0 + ((threadIdx.x >> 4) & 1);
-        const bool in = u < units;
-        const size_t row = in ? u / tiles4 : 0;
-        const int tile = in ? (int)(u - row * tiles4) : 0, c = tile * 128 + sub * 8, block = tile * 4 + (sub >> 2);
-        float f[8];
+    for (unsigned long long r0 = (unsigned long long)blockIdx.x * (MX_ROWS * MX_AHEAD); r0 < rows; r0 += (unsigned long long)gridDim.x * (MX_ROWS * MX_AHEAD)) {
+        Eight<TYPE> f[MX_AHEAD];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 0.f;
-        if (in && block < blocks) read_eight<TYPE>(x, row, c, C, pitch, f);
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const uint32_t code = mx_scale_code(top);
-        const float inverse = mx_inverse(code);
-        float q[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = code == MX_NAN ? 0.f : f[i] * inverse;
-        const uint32_t w = mx_codes(q);
-        if (FORM == 0 && codes) {
-            const uint32_t s0 = __shfl_sync(0xffffffffu, code, threadIdx.x & 16), s1 = __shfl_sync(0xffffffffu, code, (threadIdx.x & 16) + 4);
-            const uint32_t s2 = __shfl_sync(0xffffffffu, code, (threadIdx.x & 16) + 8), s3 = __shfl_sync(0xffffffffu, code, (threadIdx.x & 16) + 12);
-            if (in && block < blocks) codes[(row * blocks + block) * 4 + (sub & 3)] = w;
-            if (in && sub == 0) *(uint32_t *)(scales + mx_scale_at((long long)row, tile * 4, tiles4)) = s0 | s1 << 8 | s2 << 16 | s3 << 24;
+        for (int k = 0; k < MX_AHEAD; ++k) {
+            const size_t row = r0 + k * MX_ROWS + (threadIdx.x >> 4);
+            if (mine && row < rows) f[k].read(x, row, c, C, pitch);
+            else f[k].clear();
         }
-        if (values && in && block < blocks) {
-            mx_values(w, mx_scale(code), f);
-            if (FORM == 0) write_eight<TYPE>(values, row, c, C, pitch, f);
-            else {
-                const float g[8] = {f[0], f[4], f[1], f[5], f[2], f[6], f[3], f[7]};
-                *(bf16x8 *)((__nv_bfloat16 *)values + row * ((size_t)blocks * MX_BLOCK) + c) = pack8(g);
+#pragma unroll
+        for (int k = 0; k < MX_AHEAD; ++k) {
+            if (r0 + k * MX_ROWS >= rows) break;
+            const size_t row = r0 + k * MX_ROWS + (threadIdx.x >> 4);
+            const bool in = row < rows;
+            uint32_t top = f[k].top();
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const uint32_t code = mx_scale_code(top), w = f[k].codes(code);
+            if (FORM == 0 && codes) {
+                uint32_t word = code << (8 * (sub >> 2));
+                word |= __shfl_xor_sync(0xffffffffu, word, 4);
+                word |= __shfl_xor_sync(0xffffffffu, word, 8);
+                if (in && mine) codes[(row * blocks + block) * 4 + (sub & 3)] = w;
+                if (in && sub == 0) *(uint32_t *)(scales + mx_scale_at((long long)row, tile * 4, tiles4)) = word;
+            }
+            if (values && in && mine) {
+                if (FORM == 0) write_eight<TYPE>(values, row, c, C, pitch, w, code);
+                else {
+                    const MxFactors m(code);
+                    *(bf16x8 *)((__nv_bfloat16 *)values + row * ((size_t)blocks * MX_BLOCK) + c) =
+                        bf16x8{{m.value(mx_pair<0>(w)), m.value(mx_pair<1>(w)), m.value(mx_pair<2>(w)), m.value(mx_pair<3>(w))}};
+                }
             }
         }
     }
+}
+
+// The grid of the kernel above: tiles of 128 channels by shares of the rows, together about 16 blocks to an SM
+static dim3 mx_grid(unsigned long long rows, int tiles4) {
+    const unsigned long long all = (rows + MX_ROWS * MX_AHEAD - 1) / (MX_ROWS * MX_AHEAD), most = (148 * 16 + tiles4 - 1) / tiles4;
+    return dim3((unsigned)(all < most ? all : most), (unsigned)tiles4);
 }
 
 template <int TYPE>
@@ -121,9 +171,8 @@ __global__ void __launch_bounds__(MX_T) mx_dequantize_kernel(const uint32_t *__r
     for (unsigned long long e = (unsigned long long)blockIdx.x * MX_T + threadIdx.x; e < total; e += (unsigned long long)gridDim.x * MX_T) {
         const size_t row = e / eights;
         const int c = (int)(e - row * eights) * 8, block = c / MX_BLOCK;
-        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (block < blocks) mx_values(__ldg(codes + (row * blocks + block) * 4 + (c & 31) / 8), mx_scale(__ldg(scales + mx_scale_at((long long)row, block, tiles4))), f);
-        write_eight<TYPE>(values, row, c, C, pitch, f);
+        const uint32_t w = block < blocks ? __ldg(codes + (row * blocks + block) * 4 + (c & 31) / 8) : 0u, code = block < blocks ? __ldg(scales + mx_scale_at((long long)row, block, tiles4)) : 127u;
+        write_eight<TYPE>(values, row, c, C, pitch, w, code);
     }
 }
 
@@ -195,25 +244,15 @@ __global__ void __launch_bounds__(MXF_WARPS * 32) mx_few_rows_kernel(const bf16x
             }
 #pragma unroll
             for (int f = 0; f < MXF_NT; ++f) {
-                const uint32_t code = wq[i][f].scale;
-                // 2^126 and the scale in one factor, but for scales above 2 (whose factor would leave the type)
-                const uint32_t top = min(code, 128u);
-                const uint32_t lifted = code == MX_NAN ? 0x7fffu : (top + 126u) << 7, above = code > 128u && code != MX_NAN ? (code - 1u) << 7 : 0x3f80u;
-                uint32_t m1 = lifted * 0x10001u, m2 = above * 0x10001u;
-                const bool two = code > 128u && code != MX_NAN;
-                auto value = [&](uint32_t v) {
-                    __nv_bfloat162 r = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&v), *reinterpret_cast<__nv_bfloat162 *>(&m1));
-                    if (two) r = __hmul2(r, *reinterpret_cast<__nv_bfloat162 *>(&m2));
-                    return *reinterpret_cast<uint32_t *>(&r);
-                };
+                const MxFactors m(wq[i][f].scale);
                 const uint32_t words[4] = {wq[i][f].w.x, wq[i][f].w.y, wq[i][f].w.z, wq[i][f].w.w};
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int q = 2 * hh; q < 2 * hh + 2; ++q) {
-                        mma_16816(s, xq[0][q].w[0], xq[1][q].w[0], xq[0][q].w[1], xq[1][q].w[1], value(mx_pair<0>(words[q])), value(mx_pair<1>(words[q])));
-                        mma_16816(s, xq[0][q].w[2], xq[1][q].w[2], xq[0][q].w[3], xq[1][q].w[3], value(mx_pair<2>(words[q])), value(mx_pair<3>(words[q])));
+                        mma_16816(s, xq[0][q].w[0], xq[1][q].w[0], xq[0][q].w[1], xq[1][q].w[1], m.value(mx_pair<0>(words[q])), m.value(mx_pair<1>(words[q])));
+                        mma_16816(s, xq[0][q].w[2], xq[1][q].w[2], xq[0][q].w[3], xq[1][q].w[3], m.value(mx_pair<2>(words[q])), m.value(mx_pair<3>(words[q])));
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[f][j] += s[j];
@@ -240,11 +279,6 @@ __global__ void __launch_bounds__(MXF_WARPS * 32) mx_few_rows_kernel(const bf16x
     }
 }
 
-static unsigned mx_grid(unsigned long long units, int per_block) {
-    const unsigned long long b = (units + per_block - 1) / per_block;
-    return (unsigned)(b < 1 ? 1 : b < 148 * 16 ? b : 148 * 16);
-}
-
 static int mx_type(int type, int C, uintptr_t addresses) { return type == CPRUNE_TYPE_BF16 ? 0 : C % 4 == 0 && !(addresses & 15) ? 1 : 2; }
 
 }  // namespace cprune
@@ -260,7 +294,7 @@ size_t cprune_mx_scale_bytes(size_t rows, int C) { return C > 0 ? (rows + 127) /
 static cprune_status mx_check(const void *x, int type, size_t rows, int C, const void *codes, const void *scales) {
     if (!x || (type != CPRUNE_TYPE_BF16 && type != CPRUNE_TYPE_F32) || rows == 0 || C <= 0 || !codes != !scales) return CPRUNE_ERR_INVALID_ARG;
     if (((uintptr_t)codes | (uintptr_t)scales) & 15 || (uintptr_t)x & (type == CPRUNE_TYPE_BF16 ? 15 : 3)) return CPRUNE_ERR_INVALID_ARG;
-    if (rows >> 40 || C > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
+    if (rows >> 40 || C > (1 << 22)) return CPRUNE_ERR_UNSUPPORTED;
     return CPRUNE_OK;
 }
 
@@ -269,9 +303,9 @@ cprune_status cprune_mx_quantize(const void *x, int type, size_t rows, int C, vo
     if (c != CPRUNE_OK) return c;
     if ((!codes && !values) || (uintptr_t)values & (type == CPRUNE_TYPE_BF16 ? 15 : 3)) return CPRUNE_ERR_INVALID_ARG;
     const int tiles4 = (mx_blocks(C) + 3) / 4, pitch = type == CPRUNE_TYPE_BF16 ? cprune_padded_channels(C) : C;
-    const unsigned grid = mx_grid(rows * tiles4, MX_T / 16);
+    const dim3 grid = mx_grid(rows, tiles4);
     auto launch = [&](auto kernel) {
-        return launch_chained(kernel, dim3(grid), dim3(MX_T), 0, (cudaStream_t)stream, x, (unsigned long long)rows, C, pitch, tiles4, (uint32_t *)codes, (uint8_t *)scales, values);
+        return launch_chained(kernel, grid, dim3(MX_T), 0, (cudaStream_t)stream, x, (unsigned long long)rows, C, pitch, tiles4, (uint32_t *)codes, (uint8_t *)scales, values);
     };
     switch (mx_type(type, C, (uintptr_t)x | (uintptr_t)values)) {
         case 0: CPRUNE_CUDA_CHECK(launch(mx_quantize_kernel<0, 0>)); break;
@@ -286,7 +320,8 @@ cprune_status cprune_mx_dequantize(const void *codes, const void *scales, size_t
     const cprune_status c = mx_check(values, type, rows, C, codes, scales);
     if (c != CPRUNE_OK) return c;
     const int tiles4 = (mx_blocks(C) + 3) / 4, pitch = type == CPRUNE_TYPE_BF16 ? cprune_padded_channels(C) : C;
-    const unsigned grid = mx_grid(rows * ((pitch + 7) / 8), MX_T);
+    const unsigned long long all = (rows * ((pitch + 7) / 8) + MX_T - 1) / MX_T;
+    const unsigned grid = (unsigned)(all < 148 * 16 ? all : 148 * 16);
     auto launch = [&](auto kernel) {
         return launch_chained(kernel, dim3(grid), dim3(MX_T), 0, (cudaStream_t)stream, (const uint32_t *)codes, (const uint8_t *)scales, (unsigned long long)rows, C, pitch, tiles4,
                               values);
@@ -329,7 +364,7 @@ cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes
     if (!x || !codes || !scales || !b_packed || !y || rows == 0 || in <= 0 || out <= 0 || act < CPRUNE_ACT_NONE || act > CPRUNE_ACT_RELU6) return CPRUNE_ERR_INVALID_ARG;
     if (((uintptr_t)x | (uintptr_t)codes | (uintptr_t)scales | (uintptr_t)residual | (uintptr_t)workspace) & 15 || (uintptr_t)b_packed & 3) return CPRUNE_ERR_INVALID_ARG;
     if ((uintptr_t)y & (out_is_f32 ? 3 : 15)) return CPRUNE_ERR_INVALID_ARG;
-    if (rows >> 31 || in > (1 << 24) || out > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
+    if (rows >> 31 || in > (1 << 22) || out > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
     const size_t need = cprune_mx_fc_workspace_bytes(rows, in, out);
     if (need && (!workspace || workspace_bytes < need)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t st = (cudaStream_t)stream;
@@ -341,12 +376,12 @@ cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes
     if (t.tensor && t.round) return launch_mx_product(p, t, x, nullptr, in, nullptr, chain, st);
     if (t.tensor) {
         uint8_t *xscales = (uint8_t *)workspace + mx_codes_bytes(rows, in);
-        CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 0>, dim3(mx_grid(rows * p.tiles4, MX_T / 16)), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
+        CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 0>, mx_grid(rows, p.tiles4), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
                                          cprune_padded_channels(in), p.tiles4, (uint32_t *)workspace, xscales, (void *)nullptr));
         chain.follow();
         return launch_mx_product(p, t, workspace, xscales, in, (float *)(xscales + cprune_mx_scale_bytes(rows, in)), chain, st);
     }
-    CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 1>, dim3(mx_grid(rows * p.tiles4, MX_T / 16)), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
+    CPRUNE_CUDA_CHECK(launch_chained(mx_quantize_kernel<0, 1>, mx_grid(rows, p.tiles4), dim3(MX_T), 0, st, x, (unsigned long long)rows, in,
                                      cprune_padded_channels(in), p.tiles4, (uint32_t *)nullptr, (uint8_t *)nullptr, workspace));
     chain.follow();
     const dim3 grid((p.out_pad + MXF_NT * 8 - 1) / (MXF_NT * 8), (unsigned)((rows + 15) / 16));

@@ -51,6 +51,29 @@ __device__ __forceinline__ uint32_t mx_pair(uint32_t w) {
     return (s & 0x80008000u) | (e & 0x01C001C0u);
 }
 
+// The two bf16x2 factors that make values of mx_pair's results: 2^126 and the scale in one, but for scales above 2, whose factor would leave the type
+struct MxFactors {
+    uint32_t first, second;
+    bool two;
+    __device__ __forceinline__ explicit MxFactors(uint32_t code) {
+        two = code > 128u && code != MX_NAN;
+        first = (code == MX_NAN ? 0x7fffu : (min(code, 128u) + 126u) << 7) * 0x10001u;
+        second = (two ? (code - 1u) << 7 : 0x3f80u) * 0x10001u;
+    }
+    __device__ __forceinline__ uint32_t value(uint32_t pair) const {
+        uint32_t r;
+        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(pair), "r"(first));
+        if (two) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r) : "r"(second));
+        return r;
+    }
+};
+// Eight codes to bf16 (times the scale), in their order
+__device__ __forceinline__ bf16x8 mx_values_bf16(uint32_t w, uint32_t code) {
+    const MxFactors m(code);
+    const uint32_t a = m.value(mx_pair<0>(w)), b = m.value(mx_pair<1>(w)), c = m.value(mx_pair<2>(w)), d = m.value(mx_pair<3>(w));      // (0, 4), (1, 5), (2, 6), (3, 7)
+    return bf16x8{{__byte_perm(a, b, 0x5410), __byte_perm(c, d, 0x5410), __byte_perm(a, b, 0x7632), __byte_perm(c, d, 0x7632)}};
+}
+
 // Eight codes to float32 (times the scale)
 __device__ __forceinline__ void mx_values(uint32_t w, float scale, float *f) {
     const uint32_t p[4] = {mx_pair<0>(w), mx_pair<1>(w), mx_pair<2>(w), mx_pair<3>(w)};

@@ -222,7 +222,7 @@ def test_refusals(cp):
     for call in (quantize, dequantize):
         assert call(x=None) == 1 and call(type=2) == 1 and call(type=-1) == 1 and call(rows=0) == 1 and call(C=0) == 1
         assert call(codes=None) == 1 and call(scales=None) == 1 and call(codes=0x2008) == 1 and call(scales=0x3004) == 1 and call(x=0x1002) == 1
-        assert call(type=1, x=0x1002) == 1 and call(rows=1 << 40) == 2 and call(C=(1 << 24) + 1) == 2
+        assert call(type=1, x=0x1002) == 1 and call(rows=1 << 40) == 2 and call(C=(1 << 22) + 1) == 2
     assert quantize(codes=None, scales=None, values=None) == 1 and quantize(values=0x4004) == 1 and dequantize(codes=None, scales=None) == 1
     assert L.cprune_mx_pack(vp(0x1000), vp(0), 4, 8, vp(0), vp(0), vp(0x4000), vp(0)) == 1
     assert L.cprune_mx_pack(vp(0), vp(0), 4, 8, vp(0x2000), vp(0x3000), vp(0x4000), vp(0)) == 1
@@ -237,7 +237,7 @@ def test_refusals(cp):
     assert fc(x=0x1008) == 1 and fc(codes=0x2008) == 1 and fc(scales=0x3008) == 1 and fc(res=0x7008) == 1 and fc(y=0x5008) == 1 and fc(f32=1, y=0x5002) == 1
     assert fc(b=0x4002) == 1 and fc(work=0x6008) == 1
     assert fc(work=None) == 3 and fc(size=8) == 3
-    assert fc(rows=1 << 31) == 2 and fc(inn=(1 << 24) + 1) == 2 and fc(out=(1 << 24) + 1) == 2
+    assert fc(rows=1 << 31) == 2 and fc(inn=(1 << 22) + 1) == 2 and fc(out=(1 << 24) + 1) == 2
 
 
 def test_python_refusals(cp):

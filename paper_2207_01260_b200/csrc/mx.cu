@@ -12,12 +12,12 @@ namespace cprune {
 
 // ------------------------------------------------------------------------------------------------------- rounding
 
-// The eight values that begin at channel c of a row.  TYPE 0: bf16 rows of c_pad channels; 1: float32 rows on 16-byte boundaries; 2: float32 rows at any
+// The eight values that begin at channel c of a row, at p.  TYPE 0: bf16 rows of c_pad channels; 1: float32 rows on 16-byte boundaries; 2: float32 rows at any
 // address.  Channels from C on are zeros.
 template <int TYPE> struct Eight {
     float f[8];
-    __device__ __forceinline__ void read(const void *x, size_t row, int c, int C, int pitch) {
-        const float *p = (const float *)x + row * pitch + c;
+    using Value = float;
+    __device__ __forceinline__ void read(const Value *p, int c, int C, int) {
         if (TYPE == 1) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -52,10 +52,11 @@ template <int TYPE> struct Eight {
 // (two at a time, as bf16: products with a power of two are exact there too, but for what is far under the smallest code)
 template <> struct Eight<0> {
     bf16x8 v;
-    __device__ __forceinline__ void read(const void *x, size_t row, int c, int C, int pitch) {
+    using Value = __nv_bfloat16;
+    __device__ __forceinline__ void read(const Value *p, int c, int C, int pitch) {
         clear();
         if (c >= pitch) return;
-        v = ldg8((const bf16x8 *)((const __nv_bfloat16 *)x + row * pitch + c));
+        v = ldg8((const bf16x8 *)p);
         if (c + 8 > C) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v.w[i] &= (c + 2 * i < C ? 0xffffu : 0u) | (c + 2 * i + 1 < C ? 0xffff0000u : 0u);
@@ -79,85 +80,105 @@ template <> struct Eight<0> {
     }
 };
 
-// The exact values of eight codes, in the form of x (pad lanes zero)
+// The exact values of eight codes to p, in the form of x (pad lanes zero)
 template <int TYPE>
-__device__ __forceinline__ void write_eight(void *y, size_t row, int c, int C, int pitch, uint32_t w, uint32_t code) {
-    if (TYPE == 0) {
+__device__ __forceinline__ void write_eight(typename Eight<TYPE>::Value *p, int c, int C, int pitch, uint32_t w, uint32_t code) {
+    if constexpr (TYPE == 0) {
         if (c >= pitch) return;
         bf16x8 v = mx_values_bf16(w, code);
         if (c + 8 > C) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v.w[i] &= (c + 2 * i < C ? 0xffffu : 0u) | (c + 2 * i + 1 < C ? 0xffff0000u : 0u);
         }
-        *(bf16x8 *)((__nv_bfloat16 *)y + row * pitch + c) = v;
-        return;
-    }
-    float f[8];
-    mx_values(w, mx_scale(code), f);
-    float *p = (float *)y + row * pitch + c;
-    if (TYPE == 1) {
-        if (c < C) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
-        if (c + 4 < C) *((float4 *)p + 1) = make_float4(f[4], f[5], f[6], f[7]);
+        *(bf16x8 *)p = v;
     } else {
+        float f[8];
+        mx_values(w, mx_scale(code), f);
+        if (TYPE == 1) {
+            if (c < C) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+            if (c + 4 < C) *((float4 *)p + 1) = make_float4(f[4], f[5], f[6], f[7]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < C) p[i] = f[i];
+            for (int i = 0; i < 8; ++i)
+                if (c + i < C) p[i] = f[i];
+        }
     }
 }
 
-constexpr int MX_T = 256, MX_ROWS = MX_T / 16, MX_AHEAD = 4;
+constexpr int MX_T = 256, MX_UNIT = 64;      // rows that a block takes at a time
 
-// 16 threads take four blocks (128 channels, a tile of scales wide: grid y) of a row, eight values each: loads and stores of neighbouring threads adjoin, and the
-// four scales are one word of a tile of scales.  A thread has MX_AHEAD rows under way: bound by the bytes, as long as enough of them are (200704 x 108
-// with the values written, 98 MB: one row at a time and a division per row 36 us, now MX_TIME us).  FORM 0: codes and scales (either both or neither), values as x; 1:
-// the values in blocks, bf16 [rows][blocks * 32], in the order 0 4 1 5 2 6 3 7 of every eight (the order in which mx_pair takes codes apart).
+// 16 / E threads take four blocks (128 channels, a tile of scales wide: grid y) of a row, 8 E values each (bf16: sixteen, float32: eight): loads and stores of
+// neighbouring threads adjoin, and the four scales are one word of a tile of scales.  What bounds it is the number of instructions, most of them for a block's scale, whatever the values a thread
+// has; 200704 x 108 with the values written (98 MB): eight values a thread, one row at a time 36 us, four rows under way and bf16 two at a time 26 us, sixteen
+// values 22 us.  FORM 0: codes and scales (either both or neither), values as x; 1: the values in blocks, bf16 [rows][blocks * 32], in the order
+// 0 4 1 5 2 6 3 7 of every eight (the order in which mx_pair takes codes apart).
 template <int TYPE, int FORM>
 __global__ void __launch_bounds__(MX_T) mx_quantize_kernel(const void *__restrict__ x, unsigned long long rows, int C, int pitch, int tiles4, uint32_t *__restrict__ codes,
                                                            uint8_t *__restrict__ scales, void *__restrict__ values) {
     pdl_wait();
     pdl_trigger();
-    const int blocks = (C + MX_BLOCK - 1) / MX_BLOCK, sub = threadIdx.x & 15, tile = blockIdx.y, c = tile * 128 + sub * 8, block = tile * 4 + (sub >> 2);
+    using Value = typename Eight<TYPE>::Value;
+    constexpr int E = TYPE == 0 ? 2 : 1, TEAM = 16 / E, ROWS = MX_T / TEAM, AHEAD = MX_UNIT / ROWS, OF_BLOCK = 4 / E;       // OF_BLOCK: threads of a block of 32
+    const int blocks = (C + MX_BLOCK - 1) / MX_BLOCK, sub = threadIdx.x % TEAM, own = threadIdx.x / TEAM, tile = blockIdx.y, c = tile * 128 + sub * 8 * E;
+    const int block = tile * 4 + sub / OF_BLOCK;
     const bool mine = block < blocks;
+    const int x_step = ROWS * pitch, code_step = ROWS * blocks * 4, value_step = ROWS * blocks * MX_BLOCK;
     // (whole warps go round: the shuffles below need all lanes)
-    for (unsigned long long r0 = (unsigned long long)blockIdx.x * (MX_ROWS * MX_AHEAD); r0 < rows; r0 += (unsigned long long)gridDim.x * (MX_ROWS * MX_AHEAD)) {
-        Eight<TYPE> f[MX_AHEAD];
+    for (unsigned long long r0 = (unsigned long long)blockIdx.x * MX_UNIT; r0 < rows; r0 += (unsigned long long)gridDim.x * MX_UNIT) {
+        const int left = (int)min(rows - r0, (unsigned long long)MX_UNIT);
+        const Value *from = (const Value *)x + (r0 + own) * pitch + c;
+        Eight<TYPE> f[AHEAD][E];
 #pragma unroll
-        for (int k = 0; k < MX_AHEAD; ++k) {
-            const size_t row = r0 + k * MX_ROWS + (threadIdx.x >> 4);
-            if (mine && row < rows) f[k].read(x, row, c, C, pitch);
-            else f[k].clear();
-        }
+        for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
-        for (int k = 0; k < MX_AHEAD; ++k) {
-            if (r0 + k * MX_ROWS >= rows) break;
-            const size_t row = r0 + k * MX_ROWS + (threadIdx.x >> 4);
-            const bool in = row < rows;
-            uint32_t top = f[k].top();
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const uint32_t code = mx_scale_code(top), w = f[k].codes(code);
+            for (int e = 0; e < E; ++e) {
+                if (mine && k * ROWS + own < left) f[k][e].read(from + k * x_step + 8 * e, c + 8 * e, C, pitch);
+                else f[k][e].clear();
+            }
+        uint32_t *code_to = codes + ((r0 + own) * blocks + block) * 4 + (sub % OF_BLOCK) * E;
+        // (64 rows of a tile of scales: words 16 bytes apart, the second 32 rows in the next word)
+        uint32_t *scale_to = (uint32_t *)(scales + mx_scale_at((long long)r0, tile * 4, tiles4)) + own * 4;
+        Value *value_to = (Value *)values + (FORM == 0 ? (r0 + own) * pitch + c : (r0 + own) * ((size_t)blocks * MX_BLOCK) + c);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (k * ROWS >= left) break;
+            const bool in = k * ROWS + own < left;
+            uint32_t top = f[k][0].top();
+            if (E > 1) top = max(top, f[k][E - 1].top());
+#pragma unroll
+            for (int o = 1; o < OF_BLOCK; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const uint32_t code = mx_scale_code(top);
+            uint32_t w[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) w[e] = f[k][e].codes(code);
             if (FORM == 0 && codes) {
-                uint32_t word = code << (8 * (sub >> 2));
-                word |= __shfl_xor_sync(0xffffffffu, word, 4);
-                word |= __shfl_xor_sync(0xffffffffu, word, 8);
-                if (in && mine) codes[(row * blocks + block) * 4 + (sub & 3)] = w;
-                if (in && sub == 0) *(uint32_t *)(scales + mx_scale_at((long long)row, tile * 4, tiles4)) = word;
+                uint32_t word = code << (8 * (sub / OF_BLOCK));
+                word |= __shfl_xor_sync(0xffffffffu, word, OF_BLOCK);
+                word |= __shfl_xor_sync(0xffffffffu, word, 2 * OF_BLOCK);
+                if (in && mine) {
+                    if constexpr (E == 2) *(uint2 *)(code_to + k * code_step) = make_uint2(w[0], w[1]);
+                    else code_to[k * code_step] = w[0];
+                }
+                if (in && sub == 0) scale_to[k * ROWS % 32 * 4 + k * ROWS / 32] = word;
             }
             if (values && in && mine) {
-                if (FORM == 0) write_eight<TYPE>(values, row, c, C, pitch, w, code);
-                else {
-                    const MxFactors m(code);
-                    *(bf16x8 *)((__nv_bfloat16 *)values + row * ((size_t)blocks * MX_BLOCK) + c) =
-                        bf16x8{{m.value(mx_pair<0>(w)), m.value(mx_pair<1>(w)), m.value(mx_pair<2>(w)), m.value(mx_pair<3>(w))}};
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if constexpr (FORM == 0) write_eight<TYPE>(value_to + k * x_step + 8 * e, c + 8 * e, C, pitch, w[e], code);
+                    else {
+                        const MxFactors m(code);
+                        *(bf16x8 *)(value_to + k * value_step + 8 * e) =
+                            bf16x8{{m.value(mx_pair<0>(w[e])), m.value(mx_pair<1>(w[e])), m.value(mx_pair<2>(w[e])), m.value(mx_pair<3>(w[e]))}};
+                    }
                 }
             }
         }
     }
 }
 
-// The grid of the kernel above: tiles of 128 channels by shares of the rows, together about 16 blocks to an SM
+// The grid of the kernel above: tiles of 128 channels by shares of the rows
 static dim3 mx_grid(unsigned long long rows, int tiles4) {
-    const unsigned long long all = (rows + MX_ROWS * MX_AHEAD - 1) / (MX_ROWS * MX_AHEAD), most = (148 * 16 + tiles4 - 1) / tiles4;
+    const unsigned long long all = (rows + MX_UNIT - 1) / MX_UNIT, most = 1 << 20;
     return dim3((unsigned)(all < most ? all : most), (unsigned)tiles4);
 }
 
@@ -172,7 +193,7 @@ __global__ void __launch_bounds__(MX_T) mx_dequantize_kernel(const uint32_t *__r
         const size_t row = e / eights;
         const int c = (int)(e - row * eights) * 8, block = c / MX_BLOCK;
         const uint32_t w = block < blocks ? __ldg(codes + (row * blocks + block) * 4 + (c & 31) / 8) : 0u, code = block < blocks ? __ldg(scales + mx_scale_at((long long)row, block, tiles4)) : 127u;
-        write_eight<TYPE>(values, row, c, C, pitch, w, code);
+        write_eight<TYPE>((typename Eight<TYPE>::Value *)values + row * pitch + c, c, C, pitch, w, code);
     }
 }
 

@@ -87,11 +87,12 @@ class BlockInfo(ctypes.Structure):
 
 
 _lib = None
+_calls = None                              # the module of csrc/torch_calls.cpp, once the library is loaded
 
 
 def lib():
     """The loaded library.  Raises if it has not been built: there is no fallback path."""
-    global _lib
+    global _lib, _calls
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError("libcprune.so is missing; build it with `python -m paper_2207_01260_b200.build`")
@@ -160,7 +161,14 @@ def lib():
         L.cprune_mx_fc_workspace_bytes.restype = c_size_t
         L.cprune_mx_fc_workspace_bytes.argtypes = [c_size_t, c_int, c_int]
         L.cprune_mx_fc.argtypes = [c_void_p, c_size_t, c_int] + [c_void_p] * 3 + [c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
-        _lib = L
+        try:
+            from . import _torch_calls
+        except ImportError as e:
+            raise RuntimeError("_torch_calls.so is missing; build it with `python -m paper_2207_01260_b200.build`") from e
+        _torch_calls.load(*(ctypes.cast(getattr(L, n), c_void_p).value for n in (
+            "cprune_padded_channels", "cprune_group_norm_workspace_bytes", "cprune_group_norm", "cprune_group_norm_backward", "cprune_gradient_workspace_bytes",
+            "cprune_clip_gradients", "cprune_mx_quantize", "cprune_mx_fc_workspace_bytes", "cprune_mx_fc")))
+        _lib, _calls = L, _torch_calls
     return _lib
 
 
@@ -481,12 +489,17 @@ def cprune_fc(x, in_features, w_packed, b_packed, out_features, activation="none
 
 # The operators below check what they are given before they hand addresses on: a tensor of another type, shape or device would be read out of
 # bounds.  What they allocate belongs to the stream that they run on, so that a workspace is not handed out again while it is in use there.
-# The checks are most of what a small call costs on the host, and are written for that: a tensor that is in order passes one expression,
-# what depends on sizes alone is remembered by sizes.
+# A call with nothing but its inputs, which allocates its results and runs on the current stream, is tried by csrc/torch_calls.cpp first: the same
+# steps in compiled code, which gives up (None) where anything is not in order.  What depends on sizes alone is remembered by sizes.
 TYPE = {torch.bfloat16: 0, torch.float32: 1}
 _BF16, _F32, _U8 = torch.bfloat16, torch.float32, torch.uint8
 _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _SIZES = 4096                              # sizes remembered
+
+
+def _load():
+    lib()
+    return _calls
 
 
 def _refuse(where, why):
@@ -551,6 +564,10 @@ def cprune_group_norm(x, C, groups, gamma=None, beta=None, eps=1e-5, activation=
     """Group norm of a channels-last activation x (bf16 [N, H, W, c_pad] or float32 [N, H, W, C]) with C channels in `groups` groups, its scale
     and shift (float32 [C]), a tensor added to it and an activation (none, relu, relu6, silu).  Returns (y, stats); stats, float32
     [N, groups, 2], holds mean and 1 / sqrt(variance + eps) for cprune_group_norm_backward.  y may be x."""
+    if y is None and stats is None and workspace is None and stream is None:
+        got = (_calls or _load()).group_norm(x, C, groups, gamma, beta, eps, NORM_ACT.get(activation, -1), residual)
+        if got is not None:
+            return got
     where = "cprune_group_norm"
     dtype, shape, dev = x.dtype, x.shape, _current_device()
     geometry, act, need = _norm_geometry(where, dtype, shape, C, groups, activation, 0)
@@ -573,6 +590,10 @@ def cprune_group_norm_backward(dy, x, C, groups, stats, gamma=None, beta=None, a
                                dresidual=None, workspace=None, stream=None):
     """Gradients of cprune_group_norm's y, given dy and the stats of the forward pass.  Returns (dx, dgamma, dbeta, dresidual); dresidual is None
     where there is no residual."""
+    if dx is None and dgamma is None and dbeta is None and dresidual is None and workspace is None and stream is None:
+        got = (_calls or _load()).group_norm_backward(dy, x, C, groups, stats, gamma, beta, NORM_ACT.get(activation, -1), residual)
+        if got is not None:
+            return got
     where = "cprune_group_norm_backward"
     dtype, shape, dev = x.dtype, x.shape, _current_device()
     geometry, act, need = _norm_geometry(where, dtype, shape, C, groups, activation, 1)
@@ -639,7 +660,7 @@ def cprune_gradient_norm(grads, norm=None, workspace=None, stream=None):
     """The global 2-norm of a list of contiguous bf16 or float32 tensors, as a float32 tensor [1]."""
     where = "cprune_gradient_norm"
     dev = torch.cuda.current_device()
-    a, c, t = _gradient_list(where, grads, dev)
+    a, c, t = _gradient_list(where, list(grads), dev)
     norm = _norm_buffer(where, norm, stream, dev)
     pw, size, workspace = _workspace(where, workspace, _gradient_bytes(len(a)), stream, dev, norm)
     _check(_lib.cprune_gradient_norm(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), norm.data_ptr(), pw, size, _stream(stream)), where)
@@ -649,12 +670,16 @@ def cprune_gradient_norm(grads, norm=None, workspace=None, stream=None):
 def cprune_clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, stream=None):
     """Scales the gradients, a list of contiguous bf16 or float32 tensors, by min(1, max_norm / (norm + 1e-6)) with their global 2-norm: in place, or
     into the tensors of `out` (same sizes and types).  Returns the norm before, a float32 tensor [1]."""
+    if norm is None and workspace is None and stream is None:
+        got = (_calls or _load()).clip_gradients(grads, max_norm, out)
+        if got is not None:
+            return got
     where = "cprune_clip_gradients"
     dev = torch.cuda.current_device()
-    a, c, t = _gradient_list(where, grads, dev)
+    a, c, t = _gradient_list(where, list(grads), dev)
     o = None
     if out is not None:
-        o, oc, ot = _gradient_list(where, out, dev)
+        o, oc, ot = _gradient_list(where, list(out), dev)
         if oc != c or ot != t:
             _refuse(where, "out has to have the gradients' sizes and types")
     norm = _norm_buffer(where, norm, stream, dev)
@@ -686,6 +711,10 @@ def cprune_mx_quantize(x, C, codes=None, scales=None, values=False, stream=None)
     """x (bf16 [..., c_pad] or float32 [..., C]) rounded to MXFP4 along its channels.  Returns (codes uint8 [rows, blocks * 16], scales uint8
     [rows / 128, blocks / 4, 32, 4, 4], values): values is None, or with values=True (or a tensor like x, which may be x) what the codes
     stand for, in the form of x."""
+    if codes is None and scales is None and (values is True or values is False) and stream is None:
+        got = (_calls or _load()).mx_quantize(x, C, values)
+        if got is not None:
+            return got
     where = "cprune_mx_quantize"
     dtype, shape, dev = x.dtype, x.shape, _current_device()
     rows, typ, shape_c, shape_s = _mx_geometry(where, dtype, shape, C)
@@ -756,6 +785,10 @@ def _mx_fc_geometry(where, dtype, shape, in_features, out_features, activation, 
 def cprune_mx_fc(x, in_features, codes, scales, b_packed, out_features, activation="none", residual=None, out_f32=False, y=None, workspace=None, stream=None):
     """act(q(x) W^T + b + residual): x bf16 [..., in_pad], a row per image or pixel, rounded to MXFP4 on the way in; W and b from cprune_mx_pack;
     residual bf16 [..., out_pad].  Returns y, bf16 [..., out_pad] or float32 [..., out_features]; y may be residual."""
+    if y is None and workspace is None and stream is None:
+        got = (_calls or _load()).mx_fc(x, in_features, codes, scales, b_packed, out_features, ACT.get(activation, -1), residual, out_f32)
+        if got is not None:
+            return got
     where = "cprune_mx_fc"
     shape, dev = x.shape, _current_device()
     rows, shape_c, shape_s, shape_b, shape_r, shape_y, dtype, act, need = _mx_fc_geometry(where, x.dtype, shape, in_features, out_features, activation, bool(out_f32))

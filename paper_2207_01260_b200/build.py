@@ -1,15 +1,18 @@
-"""Builds libcprune.so (all CUDA sources, sm_100a only) next to this file with nvcc."""
+"""Builds libcprune.so (all CUDA sources, sm_100a only) next to this file with nvcc, and _torch_calls.so, the Python module that makes the
+operators' calls on torch tensors, with the host compiler."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libcprune.so")
+CALLS = os.path.join(HERE, "_torch_calls.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -20,15 +23,27 @@ def _newest(paths):
     return max(os.path.getmtime(p) for p in paths)
 
 
+def _calls_command(out):
+    import torch
+    root = os.path.dirname(torch.__file__)
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+               os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"), INCLUDE]
+    libs = os.path.join(root, "lib")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", *["-I" + p for p in include],
+            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, os.path.join(CSRC, "torch_calls.cpp"), "-o", out, "-L" + libs,
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath," + libs]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
-    deps = srcs + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + \
+    deps = srcs + glob.glob(os.path.join(CSRC, "*.cpp")) + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + \
         glob.glob(os.path.join(INCLUDE, "*.h"))
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest(deps):
+    if not force and all(os.path.exists(p) and os.path.getmtime(p) >= _newest(deps) for p in (LIB, CALLS)):
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     os.makedirs(BUILD_DIR, exist_ok=True)
-    objs, procs = [], []
+    tmp_calls = CALLS + ".tmp%d" % os.getpid()
+    objs, procs = [], [("torch_calls.cpp", subprocess.Popen(_calls_command(tmp_calls), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))]
     for s in srcs:
         o = os.path.join(BUILD_DIR, os.path.basename(s)[:-3] + ".o")
         objs.append(o)
@@ -43,9 +58,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
             print(out, file=sys.stderr)
         if p.returncode != 0:
             failed = True
-            print("nvcc failed on %s" % s, file=sys.stderr)
+            print("the compiler failed on %s" % s, file=sys.stderr)
     if failed:
-        raise RuntimeError("nvcc failed")
+        raise RuntimeError("the compiler failed")
+    os.replace(tmp_calls, CALLS)
     tmp = LIB + ".tmp%d" % os.getpid()
     subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", tmp, *objs,
                            "-cudart", "static"])

@@ -98,6 +98,19 @@ def test_values_that_are_no_numbers(cp):
 
 
 @pytest.mark.gpu
+def test_the_list_may_be_any_iterable(cp):
+    grads = tensors(6, [100, 5000], ["f32", "bf16"])
+    norm = cp.cprune_gradient_norm(grads)
+    into = [torch.empty_like(t) for t in grads]
+    for lists in ((grads, into), (tuple(grads), tuple(into)), (iter(grads), (t for t in into))):
+        assert torch.equal(cp.cprune_clip_gradients(lists[0], 1.0, out=lists[1]), norm)
+    assert torch.equal(cp.cprune_gradient_norm(iter(grads)), norm)
+    want = [t.clone() for t in into]
+    cp.cprune_clip_gradients((t for t in grads), 1.0)
+    assert all(torch.equal(a, b) for a, b in zip(grads, want))
+
+
+@pytest.mark.gpu
 def test_no_gradients(cp):
     assert float(cp.cprune_clip_gradients([], 1.0)) == 0.0 and float(cp.cprune_gradient_norm([torch.zeros(0, device="cuda")])) == 0.0
 

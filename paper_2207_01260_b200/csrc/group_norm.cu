@@ -426,8 +426,8 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" 
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait_but() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// pixels of a thread under way: 48 to 64 KB a block, three blocks to an SM
-__host__ __device__ constexpr int ring_of(int tensors) { return tensors == 1 ? 12 : tensors == 2 ? 8 : 5; }
+// pixels of a thread under way: 48 to 60 KB a block
+__host__ __device__ constexpr int ring_of(int tensors) { return tensors == 1 ? 12 : tensors == 2 ? 6 : 5; }
 
 // Chunk k of an image: every chunks-th round of the block's rows, from the k-th on (blocks of an image read neighbouring rows at the same time).  The first
 // `last` chunks have a round more, chunk `last` the rows that fill none.
@@ -464,7 +464,7 @@ struct Chunk {
 };
 
 // A thread's pixels of T tensors, first to last or last to first, through a ring in shared memory.  (What bounded these loops was their own bookkeeping, 75 of
-// 110 instructions a vector, as long as places in the ring and addresses were worked out pixel by pixel: 64 x 112x112x44 TWO_BEFORE us, now TWO_NOW us.)
+// 110 instructions a vector, as long as places in the ring and addresses were worked out pixel by pixel: 64 x 112x112x44 42 us, now 38 us.)
 template <typename Raw, int T, bool BACK> struct Stream {
     static constexpr int RING = ring_of(T);
     Raw *ring;
@@ -513,7 +513,7 @@ template <typename Raw, int T, bool BACK> struct Stream {
 
 // Mean and squared deviations of a chunk of pixels, channel by channel
 template <int KIND>
-__global__ void __launch_bounds__(NORM_T) norm_partial_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(NORM_T, 4) norm_partial_kernel(const __grid_constant__ NormParams p) {
     constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP;
     using Raw = typename Lanes<KIND>::Raw;
     extern __shared__ __align__(16) unsigned char norm_smem[];
@@ -559,7 +559,7 @@ template <int L>
 __device__ __forceinline__ int slot(int q, int sv) { return q % L * sv + q / L; }
 
 template <int KIND, int ACT, bool RES>
-__global__ void __launch_bounds__(NORM_T, 3) norm_apply_kernel(const __grid_constant__ NormParams p, int lanes) {
+__global__ void __launch_bounds__(NORM_T, 4) norm_apply_kernel(const __grid_constant__ NormParams p, int lanes) {
     constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP, T = RES ? 2 : 1;
     using Raw = typename Lanes<KIND>::Raw;
     extern __shared__ __align__(16) unsigned char norm_smem[];
@@ -1095,11 +1095,10 @@ static int norm_kind(int type, int C, uintptr_t addresses) {
     return C % 4 == 0 && (addresses & 15) == 0 ? 1 : 2;
 }
 
-// Chunks of pixels: as many blocks as are resident at a time (three to an SM), so that none waits for a second round, and at most as many
+// Chunks of pixels: as many blocks as are resident at a time (four to an SM, the gradients' three), so that none waits for a second round, and at most as many
 // an image as the threads of a block of the second pass read at once
-constexpr int NORM_RESIDENT = 3 * 148;
 
-static NormTiling norm_tiling(int kind, int N, int HW, int C, int G) {
+static NormTiling norm_tiling(int kind, int N, int HW, int C, int G, bool backward) {
     NormTiling t;
     const int L = kind == 0 ? 8 : kind == 1 ? 4 : 1;
     t.lanes = kind == 0 ? cprune_padded_channels(C) : C;
@@ -1108,7 +1107,7 @@ static NormTiling norm_tiling(int kind, int N, int HW, int C, int G) {
     t.sv = (pv + t.slices - 1) / t.slices;
     t.slices = (pv + t.sv - 1) / t.sv;
     t.rows = NORM_T / t.sv;
-    long long chunks = NORM_RESIDENT / ((long long)N * t.slices);
+    long long chunks = (backward ? 3 : 4) * 148 / ((long long)N * t.slices);
     const long long rounds = (HW + t.rows - 1) / t.rows, most = (rounds + 3) / 4;         // (four rounds of a block's threads at least)
     if (chunks > most) chunks = most;
     int readers = 1;                       // threads to a channel (of the groups that a slice touches)
@@ -1121,7 +1120,7 @@ static NormTiling norm_tiling(int kind, int N, int HW, int C, int G) {
 }
 
 static size_t norm_part_bytes(int N, int HW, int C, int G, int kind) {
-    const NormTiling t = norm_tiling(kind, N, HW, C, G);
+    const NormTiling t = norm_tiling(kind, N, HW, C, G, false);          // (the most of the two)
     return ((size_t)N * t.chunks * t.lanes * sizeof(float2) + 255) / 256 * 256;
 }
 
@@ -1150,10 +1149,10 @@ static cprune_status by_kind(int kind, int act, bool residual, F f) {
     return kind == 0 ? second(std::integral_constant<int, 0>()) : kind == 1 ? second(std::integral_constant<int, 1>()) : second(std::integral_constant<int, 2>());
 }
 
-static NormParams norm_params(int kind, int N, int H, int W, int C, int groups, int act) {
+static NormParams norm_params(int kind, int N, int H, int W, int C, int groups, int act, bool backward) {
     NormParams p = {};
     p.N = N; p.HW = H * W; p.C = C; p.G = groups; p.cpg = C / groups; p.act = act;
-    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
+    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups, backward);
     p.pv = t.lanes / (kind == 0 ? 8 : kind == 1 ? 4 : 1);
     p.sv = t.sv; p.rows = t.rows; p.chunks = t.chunks;
     const int touched = (t.sv * L_of(kind) + p.cpg - 1) / p.cpg + 1;
@@ -1191,10 +1190,10 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
     const int kind = norm_kind(type, C, tensors);
     const NormCluster c = norm_cluster(kind, N, H * W, C, groups);
     if (!c.ranks && (workspace_bytes < norm_part_bytes(N, H * W, C, groups, kind) || !workspace)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
-    NormParams p = norm_params(kind, N, H, W, C, groups, act);
+    NormParams p = norm_params(kind, N, H, W, C, groups, act, false);
     p.x = x; p.res = residual; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats; p.eps = eps;
     p.part = (float2 *)workspace;
-    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
+    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups, false);
     cudaStream_t st = (cudaStream_t)stream;
     return by_kind(kind, act, residual != nullptr, [&](auto k, auto a, auto r) -> cprune_status {
         constexpr int K = decltype(k)::value, A = decltype(a)::value;
@@ -1225,11 +1224,11 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
     const int kind = norm_kind(type, C, tensors);
     const size_t part_bytes = norm_part_bytes(N, H * W, C, groups, kind);
     if (workspace_bytes < part_bytes || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
-    NormParams p = norm_params(kind, N, H, W, C, groups, act);
+    NormParams p = norm_params(kind, N, H, W, C, groups, act, true);
     p.x = x; p.dy = dy; p.res = residual; p.out = dx; p.dres = dresidual; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float *>(stats);
     p.dgamma = dgamma; p.dbeta = dbeta;
     p.part = (float2 *)workspace;
-    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups);
+    const NormTiling t = norm_tiling(kind, N, p.HW, C, groups, true);
     cudaStream_t st = (cudaStream_t)stream;
     return by_kind(kind, act, residual != nullptr, [&](auto k, auto a, auto r) -> cprune_status {
         constexpr int K = decltype(k)::value, A = decltype(a)::value;

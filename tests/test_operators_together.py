@@ -1,0 +1,104 @@
+"""The operators around the convolutions in one run, as they are used: a pruned conv task, group norm and activation, a 1x1 layer and the classifier in 4-bit
+weights; then the gradients of the norm's parameters, clipped together with others."""
+import numpy as np
+import pytest
+import torch
+
+import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def cp():
+    import paper_2207_01260_b200 as m
+    m.lib()
+    return m
+
+
+class Candidate:
+    """One pruned layer and what follows it.  64 filters of which 48 are kept, 6 groups, a 1x1 layer of 72 features with a shortcut, 10 classes."""
+
+    def __init__(self, cp, batch):
+        self.cp, self.batch = cp, batch
+        m = wl.single_task()
+        w, b = (torch.from_numpy(np.ascontiguousarray(v)).cuda() for v in wl.model_weights(m)["conv"])
+        _, w, b, _ = cp.cprune_select_filters(w, 48, b)
+        self.plan = cp.cprune_task_plan(batch, 64, 32, 32, 48, 3, 3, 1, 1, activation="none")
+        self.conv = cp.cprune_pack_weights(self.plan, w, b)
+        g = torch.Generator(device="cuda").manual_seed(5)
+        r = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+        self.gamma, self.beta = 1 + 0.2 * r(48), 0.2 * r(48)
+        self.w1, self.b1, self.w2, self.b2 = r(72, 48, 1, 1) / 7, 0.1 * r(72), r(10, 72) / 8, 0.1 * r(10)
+        self.mx1, self.mx2 = cp.cprune_mx_pack(self.w1, self.b1), cp.cprune_mx_pack(self.w2, self.b2)
+        self.shortcut = torch.zeros((batch, 32, 32, 72), dtype=torch.bfloat16, device="cuda")
+        self.shortcut[..., :72] = r(batch, 32, 32, 72)
+
+    def forward(self, x):
+        cp = self.cp
+        a = cp.cprune_task_run(self.plan, cp.cprune_cast_input(x), *self.conv)
+        n, stats = cp.cprune_group_norm(a, 48, 6, self.gamma, self.beta, 1e-5, "silu")
+        p = cp.cprune_mx_fc(n, 48, *self.mx1, 72, "relu", self.shortcut)
+        q = cp.cprune_global_avgpool(p, 72)
+        return a, n, stats, p, q, cp.cprune_mx_fc(q, 72, *self.mx2, 10, out_f32=True)
+
+
+def values(cp, t, C):
+    """What a tensor's rows, or weights, stand for after the rounding to 4 bits, in 64 bits."""
+    c, s, _ = cp.cprune_mx_quantize(t, C)
+    return cp.cprune_mx_dequantize(c, s, C).double()
+
+
+@pytest.mark.parametrize("batch", [2, 16])
+def test_a_run_of_them(cp, batch):
+    net = Candidate(cp, batch)
+    x = torch.from_numpy(wl.model_input(wl.single_task(), batch)).cuda()
+    a, n, stats, p, q, logits = net.forward(x)
+    cp.cprune_poll_device_status()
+    # every step against 64 bits of its own input: half a step of the stored type, and float32 sums
+    v = a[..., :48].double().reshape(batch, 1024, 6, 8)
+    mean, var = v.mean((1, 3), keepdim=True), v.var((1, 3), correction=0, keepdim=True)
+    z = ((v - mean) / (var + 1e-5).sqrt()).reshape(batch, 32, 32, 48) * net.gamma.double() + net.beta.double()
+    want = z * torch.sigmoid(z)
+    assert torch.all((n[..., :48].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5 * (1 + z.abs()))
+    rows = values(cp, n, 48)
+    w1, w2 = values(cp, net.w1.reshape(72, 48).contiguous(), 48), values(cp, net.w2, 72)
+    z = (rows @ w1.t() + net.b1.double()).reshape(batch, 32, 32, 72) + net.shortcut[..., :72].double()
+    size = (rows.abs() @ w1.abs().t() + net.b1.double().abs()).reshape(z.shape) + net.shortcut[..., :72].double().abs()
+    want = z.clamp(min=0)
+    assert torch.all((p[..., :72].double() - want).abs() <= 2.0 ** -8 * want.abs() + 64 * 2.0 ** -23 * size)
+    want = p[..., :72].double().mean((1, 2))
+    assert torch.all((q[:, :72].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5)
+    rows = values(cp, q, 72)
+    want, size = rows @ w2.t() + net.b2.double(), rows.abs() @ w2.abs().t() + net.b2.double().abs()
+    assert torch.all((logits.double() - want).abs() <= 2.0 ** -24 * want.abs() + 100 * 2.0 ** -23 * size)
+    # a short training's step behind it
+    g = torch.Generator(device="cuda").manual_seed(6)
+    dy = torch.randn(n.shape, generator=g, device="cuda").bfloat16()
+    da, dgamma, dbeta, _ = cp.cprune_group_norm_backward(dy, a, 48, 6, stats, net.gamma, net.beta, "silu")
+    dw = torch.randn((48, 64, 3, 3), generator=g, device="cuda").bfloat16()
+    grads = [dgamma, dbeta, dw, da]
+    total = float(torch.sqrt(sum(t.double().square().sum() for t in grads)))
+    before = [t.double().clone() for t in grads]
+    norm = cp.cprune_clip_gradients(grads, 2.0)
+    assert abs(float(norm) - total) <= 2.0 ** -23 * total and total > 2.0
+    for t, b in zip(grads, before):
+        want = b * (2.0 / (total + 1e-6))
+        assert torch.all((t.double() - want).abs() <= (2.0 ** -8 if t.dtype == torch.bfloat16 else 2.0 ** -24) * want.abs() + 2.0 ** -22 * want.abs())
+
+
+def test_a_run_of_them_captured_and_replayed(cp):
+    net = Candidate(cp, 8)
+    m = wl.single_task()
+    x = torch.from_numpy(wl.model_input(m, 8)).cuda()
+    other = torch.from_numpy(wl.model_input(m, 9)[1:]).cuda()
+    want = [net.forward(v)[5].clone() for v in (x, other)]
+    given = x.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        logits = net.forward(given)[5]
+    for v, w in ((x, want[0]), (other, want[1]), (x, want[0])):
+        given.copy_(v)
+        graph.replay()
+        assert torch.equal(logits, w)
+    cp.cprune_poll_device_status()

@@ -266,8 +266,8 @@ cprune_status cprune_fc(const void *x, int N, int in, const void *w_packed, cons
  * dresidual (NULL, or wanted, with residual given).  The slope of relu is 0 at 0, of relu6 0 at 0 and at 6; it is taken of the
  * z that x, stats, gamma, beta and residual give.  dx and dresidual may be dy or x, but not each other.
  * Results do not depend on timing (no atomics).  bf16 tensors are 16-byte aligned, all others to their elements.
- * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (an image of 2^31 values or more, N > 65534, a group of more
- * than 8192 channels), CUDA.  Enqueue only; at most two launches. */
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (an image of 2^31 values or more, N > 65534, C > 2^20, a
+ * group of more than 8192 channels), CUDA.  Enqueue only; at most two launches. */
 size_t cprune_group_norm_workspace_bytes(int type, int N, int H, int W, int C, int groups, int backward);
 cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, int C, int groups, const float *gamma, const float *beta,
                                 float eps, int act, const void *residual, void *y, float *stats, void *workspace, size_t workspace_bytes,
@@ -311,8 +311,8 @@ cprune_status cprune_clip_gradients(const void *const *grads, const unsigned lon
  *   one);  y  bf16 [rows][out_pad] (pad lanes zero) or float32 [rows][out] when out_is_f32; it may be residual, not x
  *   workspace  cprune_mx_fc_workspace_bytes, device, 16-byte aligned
  * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows of a product, 2^40 of a rounding, more than 2^22 channels or 2^24
- * features),
- * CUDA.  Enqueue only; at most three launches. */
+ * features), CUDA; a wait of the product's that ran out is reported by cprune_poll_device_status.  Enqueue only; at most three
+ * launches. */
 int cprune_mx_blocks(int C);
 size_t cprune_mx_scale_bytes(size_t rows, int C);
 cprune_status cprune_mx_quantize(const void *x, int type, size_t rows, int C, void *codes, void *scales, void *values, void *stream);

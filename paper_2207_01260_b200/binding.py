@@ -633,12 +633,22 @@ def _gradient_list(where, tensors, device):
     if not set(map(torch.Tensor.get_device, tensors)) <= {device}:
         _refuse(where, "a gradient is not on the current device")
     addresses, counts = list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors))
-    if len(set(addresses)) != len(addresses):
-        there = [a for a, n in zip(addresses, counts) if n]
-        if len(set(there)) != len(there):
-            _refuse(where, "a tensor is in the list twice")
     types = array("i", [TYPE[next(iter(dtypes))]]) * len(counts) if len(dtypes) == 1 else array("i", [TYPE[t.dtype] for t in tensors])
     return array("Q", addresses), array("Q", counts), types
+
+
+def _refuse_overlap(where, a, c, t, out=None):
+    """Refuses gradients that share memory, with one another or with results that are not in their own place."""
+    runs = []
+    for i, (at, n) in enumerate(zip(a, c)):
+        if n:
+            size = n * (2 if t[i] == TYPE[_BF16] else 4)
+            runs.append((at, at + size))
+            if out is not None and out[i] != at:
+                runs.append((out[i], out[i] + size))
+    runs.sort()
+    if any(y[0] < x[1] for x, y in zip(runs, runs[1:])):
+        _refuse(where, "tensors of the list overlap")
 
 
 def _norm_buffer(where, norm, stream, device):
@@ -661,6 +671,7 @@ def cprune_gradient_norm(grads, norm=None, workspace=None, stream=None):
     where = "cprune_gradient_norm"
     dev = torch.cuda.current_device()
     a, c, t = _gradient_list(where, list(grads), dev)
+    _refuse_overlap(where, a, c, t)
     norm = _norm_buffer(where, norm, stream, dev)
     pw, size, workspace = _workspace(where, workspace, _gradient_bytes(len(a)), stream, dev, norm)
     _check(_lib.cprune_gradient_norm(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), norm.data_ptr(), pw, size, _stream(stream)), where)
@@ -682,6 +693,7 @@ def cprune_clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, 
         o, oc, ot = _gradient_list(where, list(out), dev)
         if oc != c or ot != t:
             _refuse(where, "out has to have the gradients' sizes and types")
+    _refuse_overlap(where, a, c, t, o)
     norm = _norm_buffer(where, norm, stream, dev)
     pw, size, workspace = _workspace(where, workspace, _gradient_bytes(len(a)), stream, dev, norm)
     _check(_lib.cprune_clip_gradients(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), max_norm, None if o is None else o.buffer_info()[0],

@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <utility>
 #include <vector>
 
 #include "cprune.h"
@@ -156,7 +157,7 @@ PyObject *group_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// Addresses, counts and types of a list of gradients; whether all are in order
+// Addresses, counts and types of a list of gradients; whether all are in order (by themselves)
 struct GradientList {
     std::vector<void *> addresses;
     std::vector<unsigned long long> counts;
@@ -176,15 +177,25 @@ struct GradientList {
             counts.push_back((unsigned long long)g.t->numel());
             types.push_back(type);
         }
-        // the same tensor twice
-        std::vector<void *> there;
-        there.reserve(n);
-        for (size_t i = 0; i < addresses.size(); ++i)
-            if (counts[i]) there.push_back(addresses[i]);
-        std::sort(there.begin(), there.end());
-        return std::adjacent_find(there.begin(), there.end()) == there.end();
+        return true;
     }
 };
+
+// Whether tensors of the list share memory, with one another or with results that are not in their own place
+bool overlap(const GradientList &g, const GradientList *out) {
+    std::vector<std::pair<uintptr_t, uintptr_t>> runs;
+    runs.reserve(2 * g.addresses.size());
+    for (size_t i = 0; i < g.addresses.size(); ++i) {
+        if (!g.counts[i]) continue;
+        const uintptr_t bytes = g.counts[i] * (g.types[i] == CPRUNE_TYPE_BF16 ? 2 : 4), at = (uintptr_t)g.addresses[i];
+        runs.emplace_back(at, at + bytes);
+        if (out && out->addresses[i] != g.addresses[i]) runs.emplace_back((uintptr_t)out->addresses[i], (uintptr_t)out->addresses[i] + bytes);
+    }
+    std::sort(runs.begin(), runs.end());
+    for (size_t i = 1; i < runs.size(); ++i)
+        if (runs[i].first < runs[i - 1].second) return true;
+    return false;
+}
 
 // clip_gradients(grads, max_norm, out) -> norm
 PyObject *clip_gradients(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -196,6 +207,7 @@ PyObject *clip_gradients(PyObject *, PyObject *const *a, Py_ssize_t n) {
         GradientList g, o;
         if (!g.read(a[0], device) || g.addresses.empty()) return none();
         if (a[2] != Py_None && (!o.read(a[2], device) || o.counts != g.counts || o.types != g.types)) return none();
+        if (overlap(g, a[2] != Py_None ? &o : nullptr)) return none();
         const int count = (int)g.addresses.size();
         const size_t need = lib.gradient_workspace_bytes(count);
         const auto like = at::TensorOptions().device(at::kCUDA, device);

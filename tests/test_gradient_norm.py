@@ -178,3 +178,25 @@ def test_python_refusals_on_the_device(cp):
         with pytest.raises(cp.CpruneError) as e:
             cp.cprune_clip_gradients(grads, 1.0, **kw)
         assert e.value.status == 1
+
+
+@pytest.mark.gpu
+def test_tensors_that_overlap_are_refused(cp):
+    flat = torch.ones(64, device="cuda")
+    a, b, c, d = flat[:16], flat[15:32], flat[32:48], flat[48:]
+    for grads, kw in (([a, b], {}), ([c, b, a], {}), ([a, c], {"out": [a, b]}), ([a, c], {"out": [flat[1:17], c]}), ([a, c], {"out": [c, a]}),
+                      ([a, c], {"out": [d, d]}), ([a, c[:0], b], {"norm": torch.zeros(1, device="cuda")})):
+        with pytest.raises(cp.CpruneError) as e:
+            cp.cprune_clip_gradients(grads, 1.0, **kw)
+        assert e.value.status == 1 and (flat == 1).all()
+    cp.cprune_clip_gradients([a, c, c[:0]], 1.0, out=[a, d, d[:0]])
+    assert (c == 1).all() and torch.equal(a, d) and (a < 1).all()
+
+
+def test_overlap_by_the_steps_in_python(cp):
+    refuse = cp.binding._refuse_overlap
+    refuse("f", [100, 164, 0], [16, 3, 0], [1, 0, 1])
+    refuse("f", [100, 164], [16, 3], [1, 0], [100, 170])
+    for a, c, t, o in (([100, 160], [16, 3], [1, 0], None), ([164, 100], [3, 17], [0, 1], None), ([100, 164], [16, 3], [1, 0], [100, 166]), ([100, 200], [4, 4], [1, 1], [200, 300])):
+        with pytest.raises(cp.CpruneError):
+            refuse("f", a, c, t, o)

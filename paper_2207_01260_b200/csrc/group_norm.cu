@@ -9,16 +9,15 @@
 // A block owns whole columns: a thread holds the same 16 bytes of channels (8 bf16, 4 float32; single float32 where rows are not multiples of
 // 16 bytes) of every R-th pixel, so that what belongs to a channel stays in its registers, and groups of any number of channels are put
 // together from channels.  Two ways through the data:
-//   - on chip: one cluster of up to 16 blocks holds the groups of one image, or a range of them, in shared memory; its blocks exchange
-//     their sums, and the data is read once.
-//   - in three launches (what does not fit): partial sums of chunks of pixels per channel; their combination; a second pass over the data.
+//   - on chip (forward, what fits): one cluster of up to 16 blocks holds the groups of one image, or a range of them, in shared memory; its blocks
+//     exchange their sums, and the data is read once.
+//   - two passes, a launch each: partial results of chunks of pixels per channel; every block of the second launch puts those of its groups together for
+//     itself, in the same order, and goes over the data again, last pixels first, so that part of it still comes from the cache.
 // The variance is never a difference of large sums: a thread takes the deviations from its own mean, and means and deviations are put
 // together pairwise (Chan, Golub, LeVeque 1979), in float32.
 #include <cmath>
 #include <mutex>
-#include <set>
 #include <type_traits>
-#include <utility>
 
 #include "common.cuh"
 #include "sm100_ptx.cuh"
@@ -621,7 +620,8 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_apply_kernel(const __grid_cons
         if (g < range.n && i == 0) {
             const float2 result = make_float2(a, 1.f / sqrtf(b + p.eps));
             image[g] = result;
-            if (blockIdx.x == 0) ((float2 *)p.stats)[(size_t)blockIdx.z * p.G + range.g0 + g] = result;       // (a group of two slices: the same twice)
+            // (a group of two slices is written by the one in which it begins)
+            if (blockIdx.x == 0 && (range.g0 + g) * p.cpg >= c.v0 * L) ((float2 *)p.stats)[(size_t)blockIdx.z * p.G + range.g0 + g] = result;
         }
     });
     __syncthreads();
@@ -1030,17 +1030,18 @@ static NormCluster norm_cluster(int kind, int N, int HW, int C, int G) {
 }
 
 // The limits of a kernel are attributes of a device
-template <typename K>
-static cprune_status make_ready(K kernel, bool cluster) {
+template <auto KERNEL>
+static cprune_status make_ready(bool cluster) {
+    static std::mutex mu;
+    static bool ready[64] = {false};
     int dev = 0;
     CPRUNE_CUDA_CHECK(cudaGetDevice(&dev));
-    static std::mutex mu;
-    static std::set<std::pair<int, const void *>> ready;
+    if (dev < 0 || dev >= 64) return CPRUNE_ERR_UNSUPPORTED;
     std::lock_guard<std::mutex> lock(mu);
-    if (ready.count({dev, (const void *)kernel})) return CPRUNE_OK;
-    CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_SMEM));
-    if (cluster) CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    ready.insert({dev, (const void *)kernel});
+    if (ready[dev]) return CPRUNE_OK;
+    CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)NORM_SMEM));
+    if (cluster) CPRUNE_CUDA_CHECK(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    ready[dev] = true;
     return CPRUNE_OK;
 }
 
@@ -1052,18 +1053,18 @@ static int norm_ring_bytes(int kind, int tensors) {
 // Behind it: results of the groups that a slice touches and of their channels (or, later, of its own), constants of its channels
 static size_t norm_pass_bytes(const NormParams &p, int L) { return (size_t)p.range * 8 + (size_t)p.room * 8 + (size_t)p.sv * L * 16; }
 
-template <typename K>
-static cprune_status launch_pass(K kernel, dim3 grid, size_t smem, cudaStream_t st, const NormParams &p, int lanes) {
-    const cprune_status s = make_ready(kernel, false);
+template <auto KERNEL>
+static cprune_status launch_pass(dim3 grid, size_t smem, cudaStream_t st, const NormParams &p, int lanes) {
+    const cprune_status s = make_ready<KERNEL>(false);
     if (s != CPRUNE_OK) return s;
-    if constexpr (std::is_invocable_v<K, NormParams, int>) CPRUNE_CUDA_CHECK(launch_chained(kernel, grid, dim3(NORM_T), smem, st, p, lanes));
-    else CPRUNE_CUDA_CHECK(launch_chained(kernel, grid, dim3(NORM_T), smem, st, p));
+    if constexpr (std::is_invocable_v<decltype(KERNEL), NormParams, int>) CPRUNE_CUDA_CHECK(launch_chained(KERNEL, grid, dim3(NORM_T), smem, st, p, lanes));
+    else CPRUNE_CUDA_CHECK(launch_chained(KERNEL, grid, dim3(NORM_T), smem, st, p));
     return CPRUNE_OK;
 }
 
-template <typename K>
-static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaStream_t st, const NormParams &p) {
-    const cprune_status s = make_ready(kernel, true);
+template <auto KERNEL>
+static cprune_status launch_cluster(const NormCluster &c, int N, cudaStream_t st, const NormParams &p) {
+    const cprune_status s = make_ready<KERNEL>(true);
     if (s != CPRUNE_OK) return s;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(c.ranks, c.slices, N);
@@ -1081,7 +1082,7 @@ static cprune_status launch_cluster(K kernel, const NormCluster &c, int N, cudaS
         attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.numAttrs = 2;
     }
-    CPRUNE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, p));
+    CPRUNE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, KERNEL, p));
     return CPRUNE_OK;
 }
 
@@ -1097,7 +1098,6 @@ static int norm_kind(int type, int C, uintptr_t addresses) {
 
 // Chunks of pixels: as many blocks as are resident at a time (four to an SM, the gradients' three), so that none waits for a second round, and at most as many
 // an image as the threads of a block of the second pass read at once
-
 static NormTiling norm_tiling(int kind, int N, int HW, int C, int G, bool backward) {
     NormTiling t;
     const int L = kind == 0 ? 8 : kind == 1 ? 4 : 1;
@@ -1130,7 +1130,7 @@ static cprune_status norm_check(int type, int N, int H, int W, int C, int groups
     if ((type != CPRUNE_TYPE_BF16 && type != CPRUNE_TYPE_F32) || N <= 0 || H <= 0 || W <= 0 || C <= 0 || groups <= 0 || C % groups) return CPRUNE_ERR_INVALID_ARG;
     if (act < CPRUNE_ACT_NONE || act > CPRUNE_ACT_SILU) return CPRUNE_ERR_INVALID_ARG;
     const long long hw = (long long)H * W;
-    if (C / groups > NORM_GROUP || hw * (C + 16LL) > 0x7fffffffLL || N > 65534 || (long long)N * groups > 0x7fffffffLL) return CPRUNE_ERR_UNSUPPORTED;
+    if (C > (1 << 20) || C / groups > NORM_GROUP || hw * (C + 16LL) > 0x7fffffffLL || N > 65534 || (long long)N * groups > 0x7fffffffLL) return CPRUNE_ERR_UNSUPPORTED;
     return CPRUNE_OK;
 }
 
@@ -1200,15 +1200,15 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
         constexpr bool R = decltype(r)::value;
         if (c.ranks) {
             p.gs = c.gs; p.sv = c.widest; p.per = c.per; p.data_bytes = (int)c.data_bytes;
-            return launch_cluster(norm_cluster_kernel<K, A, R>, c, N, st, p);
+            return launch_cluster<norm_cluster_kernel<K, A, R>>(c, N, st, p);
         }
         const dim3 grid(t.chunks, t.slices, N);
         ChainScope chain;
-        const cprune_status e = launch_pass(norm_partial_kernel<K>, grid, norm_ring_bytes(K, 1), st, p, t.lanes);
+        const cprune_status e = launch_pass<norm_partial_kernel<K>>(grid, norm_ring_bytes(K, 1), st, p, t.lanes);
         if (e != CPRUNE_OK) return e;
         chain.follow();
         p.ring_bytes = ring_of(R + 1) * (R + 1) * NORM_T * (K == 2 ? 4 : 16);
-        return launch_pass(norm_apply_kernel<K, A, R>, grid, p.ring_bytes + norm_pass_bytes(p, L_of(K)), st, p, t.lanes);
+        return launch_pass<norm_apply_kernel<K, A, R>>(grid, p.ring_bytes + norm_pass_bytes(p, L_of(K)), st, p, t.lanes);
     });
 }
 
@@ -1236,10 +1236,10 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
         ChainScope chain;
         const dim3 grid(t.chunks, t.slices, N);
         p.ring_bytes = norm_ring_bytes(K, R + 2);
-        const cprune_status e = launch_pass(norm_grad_partial_kernel<K, A, R>, grid, p.ring_bytes + (size_t)p.sv * L_of(K) * 16, st, p, t.lanes);
+        const cprune_status e = launch_pass<norm_grad_partial_kernel<K, A, R>>(grid, p.ring_bytes + (size_t)p.sv * L_of(K) * 16, st, p, t.lanes);
         if (e != CPRUNE_OK) return e;
         chain.follow();
-        return launch_pass(norm_grad_apply_kernel<K, A, R>, dim3(t.chunks, t.slices, N + (dgamma || dbeta ? 1 : 0)), p.ring_bytes + norm_pass_bytes(p, L_of(K)), st, p, t.lanes);
+        return launch_pass<norm_grad_apply_kernel<K, A, R>>(dim3(t.chunks, t.slices, N + (dgamma || dbeta ? 1 : 0)), p.ring_bytes + norm_pass_bytes(p, L_of(K)), st, p, t.lanes);
     });
 }
 

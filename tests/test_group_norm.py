@@ -89,6 +89,10 @@ CASES = [
     (70, 4, 4, 32, 4, "bf16", "relu", True),
     (1, 112, 112, 36, 4, "bf16", "relu6", True),       # a large image
     (2, 160, 150, 40, 2, "f32", "silu", False),
+    (2, 120, 100, 44, 4, "bf16", "silu", True),
+    (300, 5, 7, 72, 9, "bf16", "relu6", False),        # more images than blocks run at a time
+    (1, 3, 500, 2056, 4, "bf16", "relu", True),        # slices of the channels that groups straddle
+    (1, 31, 33, 16382, 2, "f32", "none", False),       # the widest groups, nearly
 ]
 
 
@@ -193,8 +197,9 @@ def test_mean_far_from_the_spread(cp):
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_values_that_are_no_numbers_stay_in_their_group(cp, dtype, bad):
-    x = activation(cp, 13, 2, 6, 5, 24, dtype)
+@pytest.mark.parametrize("W", [5, 6000])                    # on chip, in two passes
+def test_values_that_are_no_numbers_stay_in_their_group(cp, dtype, bad, W):
+    x = activation(cp, 13, 2, 6, W, 24, dtype)
     clean = cp.cprune_group_norm(x.cuda(), 24, 4, activation="relu")[0].cpu()
     x[1, 3, 2, 7] = bad                                     # image 1, group 1
     y = cp.cprune_group_norm(x.cuda(), 24, 4, activation="relu")[0].cpu()
@@ -204,7 +209,18 @@ def test_values_that_are_no_numbers_stay_in_their_group(cp, dtype, bad):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("hw", [6, 60])
+@pytest.mark.parametrize("C, G, dtype", [(1030, 103, "f32"), (4120, 10, "bf16")])
+def test_groups_of_two_slices_have_one_mean(cp, C, G, dtype):
+    """Blocks of both slices work such a group out: what is written and what is used does not depend on their timing."""
+    x = activation(cp, 21, 1, 40, 40, C, dtype).cuda()
+    first = cp.cprune_group_norm(x, C, G)
+    for _ in range(30):
+        again = cp.cprune_group_norm(x, C, G)
+        assert torch.equal(again[1], first[1]) and torch.equal(again[0], first[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hw", [6, 60, 190])
 def test_in_place_and_other_streams_and_graphs(cp, hw):
     """The same bits in place, on another stream, captured and replayed, and twice in a row."""
     C, G = 40, 5
@@ -272,7 +288,7 @@ def test_refusals(cp):
         assert call(x=0x1008) == 1 and call(res=0x1002) == 1 and call(stats=0x4004) == 1 and call(work=0x5004) == 1
         assert call(type=1, x=0x1002) == 1
         assert call(size=16) == 3 and call(work=None) == 3
-        assert call(N=70000) == 2 and call(C=16400, G=2) == 2
+        assert call(N=70000) == 2 and call(C=16400, G=2) == 2 and call(C=(1 << 20) + 8, G=1 << 17 | 1) == 2
     assert forward(y=None) == 1 and forward(eps=0.0) == 1 and forward(eps=-1.0) == 1 and forward(eps=float("nan")) == 1 and forward(eps=float("inf")) == 1
     assert forward(H=0) == 1 and forward(H=1 << 15, W=1 << 12) == 2
     assert backward(dy=None) == 1 and backward(dx=None) == 1 and backward(dres=0x6000) == 1

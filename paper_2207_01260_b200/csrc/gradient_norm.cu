@@ -8,6 +8,9 @@
 // tensor's address rounded down: a tensor may lie at any address of its type, and only its first and last vector are taken value by value.
 // Squares and their sums are float64: a float32 square loses gradients below 1e-19 and overflows above 1e19, and the sum runs over
 // millions of values.
+// What bounds it is memory for large lists, launches for small ones.  62 float32 tensors of 11.7 million values 15.2 us (read once and written: 14.3 us at a
+// copy's rate; the second reading comes from the L2 cache), pieces of 8 KB 17.4 us, eight blocks to an SM 15.9 us; 50 tensors of 2 million 78 us; 12 small ones
+// 4.0 us.
 #include <cmath>
 
 #include "common.cuh"
@@ -17,7 +20,7 @@ namespace cprune {
 constexpr int GRAD_T = 256, GRAD_AHEAD = 4;
 constexpr int GRAD_PIECE = GRAD_T * GRAD_AHEAD;     // vectors
 constexpr int GRAD_BLOCKS = 148 * 4;
-constexpr int GRAD_TABLE_SMALL = 64, GRAD_TABLE = 512;
+constexpr int GRAD_TABLE_SMALL = 64, GRAD_TABLE = 512;       // (a short list in the small table: 7.1 us a call on the host, in the large one 8.8)
 
 template <int MOST> struct GradTable {
     const void *g[MOST];

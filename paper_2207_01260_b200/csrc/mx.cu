@@ -211,8 +211,8 @@ __global__ void mx_pad_bias_kernel(const float *__restrict__ b, int n, int n_pad
 // takes the same 32 channels of its two rows: eight MMA steps, in an order of the channels that both sides share.
 // The tensor core truncates where it adds to an accumulator; four steps start from zero and are added to the running sum by a rounded
 // addition, and the warps' sums meet in float64.
-constexpr int MXF_WARPS = 8, MXF_NT = 2, MXF_AHEAD = 2, MXF_ROWS = 32;
-constexpr long long MXF_WEIGHTS = 4 << 20;
+constexpr int MXF_WARPS = 8, MXF_NT = 2, MXF_AHEAD = 2;
+constexpr int MXF_BLOCKS = 2 * 148, MXF_IN = 2048;
 
 // (one float32 of y, in its form)
 __device__ __forceinline__ void mx_store(const MxProduct &p, unsigned long long n, int o, float v) {
@@ -366,10 +366,14 @@ cprune_status cprune_mx_pack(const float *w, const float *b, int out, int in, vo
     return CPRUNE_OK;
 }
 
-// Few rows and weights that are read in no time: one kernel behind the rounding, not two
+// Whether the kernel for few rows takes a product: where all its blocks run at the same time and none has many channels to go through.  It needs no tensor
+// memory, no maps and no third launch.  us there / on the block-scaled path:  1 x 1280 -> 1000 4.4 / 6.4, 64 rows of that 6.9 / 7.7, 96 rows (378 blocks)
+// 9.3 / 8.0;  196 x 384 -> 64 4.9 / 7.9;  1568 x 144 -> 24 (196 blocks) 5.4 / 6.4, 3136 rows of that 7.3 / 6.4;  32 x 2048 -> 2048 7.2 / 7.6;
+// 64 x 4096 -> 1000 10.9 / 8.5;  8 x 25088 -> 4096 36 / 18.
 static MxTiling mx_product_tiling(size_t rows, int in, int out) {
     MxTiling t = {};
-    return rows <= MXF_ROWS && (long long)in * out <= MXF_WEIGHTS ? t : mx_tiling(rows, in, out);
+    const unsigned long long most = MXF_BLOCKS, wide = ((unsigned long long)out + MXF_NT * 8 - 1) / (MXF_NT * 8);
+    return in <= MXF_IN && rows <= most * 16 && (rows + 15) / 16 * wide <= most ? t : mx_tiling(rows, in, out);
 }
 static size_t mx_codes_bytes(size_t rows, int in) { return (rows * (size_t)mx_blocks(in) * 16 + 255) / 256 * 256; }
 

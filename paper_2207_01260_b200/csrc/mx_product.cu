@@ -460,17 +460,21 @@ MxTiling mx_tiling(unsigned long long rows, int in, int out) {
         t.nt = round_up((int)rows, 16);
         t.subs = 1;
         const int tiles = (out + MXP_ROWS - 1) / MXP_ROWS, chunks = (in + MXP_CHUNK - 1) / MXP_CHUNK;
-        t.splits = 2 * 148 / tiles;                        // two blocks to an SM
-        if (t.splits < 1) t.splits = 1;
-        if (t.splits > chunks) t.splits = chunks;
+        // Two blocks to an SM (8 x 25088 -> 4096: 17.6 us, with one 19.0), but three chunks or more to a share and 16 shares or fewer: each has its start to pay
+        // for and sums to leave behind (64 x 4096 -> 1000 with a chunk a share 10.3 us, three 8.5; 16 x 16384 -> 512 18.2, three 11.2, four 10.4).
+        t.splits = 2 * 148 / tiles;
+        t.splits = t.splits < 1 ? 1 : t.splits > 16 ? 16 : t.splits;
         t.per = (chunks + t.splits - 1) / t.splits;
+        if (t.per < 3) t.per = 3 < chunks ? 3 : chunks;
         t.splits = (chunks + t.per - 1) / t.per;
         return t;
     }
     const long long tiles_m = (long long)((rows + MXP_ROWS - 1) / MXP_ROWS);
     const int all = round_up(out, 16);
     t.nt = all <= MXP_MOST ? all : 256;
-    // fewer features to a block while that leaves SMs without one
+    // (384: rows are rounded here as long as one block covers all features.  12544 x 960 -> 320 16.7 us, already rounded 21.9, already rounded and in parts of 256
+    // 26.2; 200704 x 144 -> 24 38 us, already rounded 52.)
+    // Fewer features to a block while that leaves half the SMs without one: 784 x 960 -> 320 14.9 -> 7.9 us, 1024 x 4096 -> 1000 18.6 -> 15.1 us.
     while (t.nt > 64 && tiles_m * ((all + t.nt - 1) / t.nt) * 2 <= 148) t.nt = t.nt > 256 ? 256 : t.nt > 128 ? 128 : 64;
     t.tiles_n = (all + t.nt - 1) / t.nt;
     t.subs = (t.nt + 127) / 128;

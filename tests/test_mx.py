@@ -142,7 +142,7 @@ PRODUCTS = [
     # rows, in, out
     (1, 1, 1), (1, 1280, 1000), (2, 512, 10), (16, 33, 24), (17, 100, 129), (5, 4096, 33), (40, 72, 300), (127, 256, 128), (128, 32, 8), (129, 257, 136),
     (300, 960, 320), (64, 1280, 1000), (784, 24, 144), (1000, 144, 24), (513, 512, 512), (200, 31, 257), (2048, 130, 40), (260, 2100, 260), (3000, 64, 1100), (19000, 24, 144), (9600, 1, 40), (10000, 500, 384), (19100, 33, 320), (200, 8192, 500),
-    (33, 700, 1000), (100, 5000, 200), (128, 64, 130),
+    (33, 700, 1000), (100, 5000, 200), (128, 64, 130), (128, 257, 1000), (100, 64, 1000), (17, 2100, 24), (4700, 40, 8), (16, 16384, 100),
 ]
 
 

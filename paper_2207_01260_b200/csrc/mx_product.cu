@@ -146,7 +146,15 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
-    } else if (warp < MXP_WARPS && !FEATURES) {
+    } else if (warp == MXP_WARPS + 1) {
+        if (elect_one()) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_x) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_w) : "memory");
+            if (!FEATURES) asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_y) : "memory");
+            if (!FEATURES) asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_res) : "memory");
+        }
+        __syncwarp();
+    } else if (!FEATURES) {
         for (int e = threadIdx.x; e < p.nt; e += MXP_WARPS * 32) bias_s[e] = o0 + e < p.q.out ? __ldg(p.q.bias + o0 + e) : 0.f;
     }
     tc_fence_before();
@@ -155,22 +163,29 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
     const uint32_t tmem_base = *tmem_slot;
     bool ok = true;
 
+    // The weights are nobody's result: those of the first chunks are asked for before the preceding kernel has finished, in the form that rounds by the warp
+    // that multiplies, so that the rows' boxes need not queue behind them.
+    const uint32_t w0 = FEATURES ? a0 : b0, w_step = FEATURES ? 16384u : (uint32_t)p.b_bytes, ws0 = FEATURES ? sa0 : sb0;
+    const int w_first = FEATURES ? (int)row0 : o0, w_box = FEATURES ? MXP_ROWS : p.box, w_rows = FEATURES ? MXP_ROWS : p.nt;
+    const int w_parts = FEATURES ? 1 : p.subs, w_tiles = min(w_parts, (p.q.out + 127) / 128 - w_first / 128);         // tiles of scales that there are
+    auto scale_tiles = [&](int c) { return min(2, p.q.tiles4 - 2 * c); };
+    auto load_w = [&](int c, int s) {
+        const int tiles = scale_tiles(c);
+        const uint32_t rows = ROUND ? 0u : (uint32_t)((FEATURES ? p.box * 128 : 16384) + tiles * 512);
+        mbar_expect_tx(bfull(s), (uint32_t)(w_rows * 128 + w_tiles * tiles * 512) + rows);
+        for (int n = 0; n < w_rows; n += w_box) tma_load_2d(w0 + (uint32_t)s * w_step + (uint32_t)n * 128u, &tm_w, bfull(s), c * 64, w_first + n);
+        for (int n = 0; n < w_tiles; ++n)
+            bulk_load(ws0 + (uint32_t)((s * w_parts + n) * 1024), p.q.scales + ((size_t)(w_first / 128 + n) * p.q.tiles4 + 2 * c) * 512, (uint32_t)tiles * 512u, bfull(s));
+    };
+    const int ahead = min(p.stages, c_end - c_begin);
+    auto load_first = [&]() {
+        if (elect_one())
+            for (int i = 0; i < ahead; ++i) load_w(c_begin + i, i);
+        __syncwarp();
+    };
+
     if (warp == MXP_WARPS) {
         // -------------------------------------------------------------------------------------------- loads
-        // The weights are nobody's result: those of the first chunks are asked for before the preceding kernel has finished.
-        const uint32_t w0 = FEATURES ? a0 : b0, w_step = FEATURES ? 16384u : (uint32_t)p.b_bytes, ws0 = FEATURES ? sa0 : sb0;
-        const int w_first = FEATURES ? (int)row0 : o0, w_box = FEATURES ? MXP_ROWS : p.box, w_rows = FEATURES ? MXP_ROWS : p.nt;
-        const int w_parts = FEATURES ? 1 : p.subs, w_tiles = min(w_parts, (p.q.out + 127) / 128 - w_first / 128);         // tiles of scales that there are
-        int box = 0;
-        auto scale_tiles = [&](int c) { return min(2, p.q.tiles4 - 2 * c); };
-        auto load_w = [&](int c, int s) {
-            const int tiles = scale_tiles(c);
-            const uint32_t rows = ROUND ? 0u : (uint32_t)((FEATURES ? p.box * 128 : 16384) + tiles * 512);
-            mbar_expect_tx(bfull(s), (uint32_t)(w_rows * 128 + w_tiles * tiles * 512) + rows);
-            for (int n = 0; n < w_rows; n += w_box) tma_load_2d(w0 + (uint32_t)s * w_step + (uint32_t)n * 128u, &tm_w, bfull(s), c * 64, w_first + n);
-            for (int n = 0; n < w_tiles; ++n)
-                bulk_load(ws0 + (uint32_t)((s * w_parts + n) * 1024), p.q.scales + ((size_t)(w_first / 128 + n) * p.q.tiles4 + 2 * c) * 512, (uint32_t)tiles * 512u, bfull(s));
-        };
         auto load_rows = [&](int c, int s) {
             if (ROUND) return;
             const int first = FEATURES ? 0 : (int)row0;
@@ -187,26 +202,26 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
             }
             __syncwarp();
         };
-        const int ahead = min(p.stages, c_end - c_begin);
-        if (elect_one())
-            for (int i = 0; i < ahead; ++i) load_w(c_begin + i, i);
-        __syncwarp();
+        if (!ROUND) load_first();
         pdl_wait();
+        int box = 0;
         for (int i = 0; c_begin + i < c_end && ok; ++i) {
             const int c = c_begin + i, s = i % p.stages;
-            if (i >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (uint32_t)(i / p.stages - 1) & 1u, abort_flag, p.status));
+            // (a chunk's boxes before its weights, which wait for MMAs of boxes that were asked for long ago)
+            if (ROUND)
+                for (; box < p.boxes && box < 4 * c + 4 && ok; ++box) load_x(box);
+            if (i >= p.stages && ok) ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (uint32_t)(i / p.stages - 1) & 1u, abort_flag, p.status));
             if (ok && elect_one()) {
                 if (i >= ahead) load_w(c, s);
                 load_rows(c, s);
             }
             __syncwarp();
-            if (ROUND)
-                for (; box < p.boxes && box < 4 * c + 4 && ok; ++box) load_x(box);
         }
         const int panels = min(p.panels, (p.q.out_pad - o0 + 63) / 64);
         for (box = p.boxes; box < p.boxes + panels && ok; ++box) load_x(box);
     } else if (warp == MXP_WARPS + 1) {
         // --------------------------------------------------------------------------------------------- MMAs
+        if (ROUND) load_first();
         // E2M1 operands, scales that are powers of two; 64 channels of every 128 under scales 0 or 2 of a column
         const uint32_t idesc = (1u << 7) | (1u << 10) | (1u << 23) | (1u << 27), idesc_128 = idesc | 16u << 17;
         const uint32_t idesc_last = idesc | (uint32_t)((p.nt - (p.subs - 1) * 128) >> 3) << 17;
@@ -315,7 +330,7 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                 }
                 uint8_t *stage = smem + (from - base);
                 tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                 for (int u2 = 0; u2 < 2; ++u2) {
                     if (u2 * 32 >= left) break;
                     uint32_t v[32];

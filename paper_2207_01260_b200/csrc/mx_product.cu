@@ -283,11 +283,13 @@ __global__ void __launch_bounds__(MXP_THREADS) mx_product_kernel(const __grid_co
                     bf16x8 v[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const bf16x8 *>(in + xs * MXP_XBYTES + sub_off(r, half * 4 + i));
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(xempty(xs));
                     uint32_t code;
                     *reinterpret_cast<uint4 *>(out + s * 16384 + sub_off(r, part * 2 + half)) = mx_round_block(v, code);
                     scales[s * 1024 + (part >> 1) * 512 + (part & 1) * 2] = (uint8_t)code;
+                    // (The place is given back once the codes are written, that is, once all values are in registers: given back between the loads and their
+                    // first use, the next box overtook loads of warps that had to wait for the scheduler.)
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(xempty(xs));
                 }
                 fence_async_smem();                        // the tensor core reads what was written here
                 __syncwarp();

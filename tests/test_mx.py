@@ -268,3 +268,22 @@ def test_python_refusals_on_the_device(cp):
     with pytest.raises(cp.CpruneError) as e:
         cp.cprune_mx_fc(**ok, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows, inn, out", [(28636, 667, 25), (28636, 512, 25), (45922, 261, 31), (27735, 471, 292), (22063, 706, 66), (38000, 320, 384), (12544, 960, 320)])
+def test_rows_are_read_before_their_place_is_filled_again(cp, rows, inn, out):
+    """Weights that add up one block of 32 channels each.  The values of a block are multiples of half its scale, at most 6 of it: their sums are exact in
+    float32, and every bit counts.  Repeated, with the rows in the cache: the faster they come, the sooner their places are filled again."""
+    x = torch.zeros(rows, cp.cprune_padded_channels(inn), device="cuda", dtype=torch.bfloat16)
+    x[:, :inn] = torch.randn(rows, inn, generator=torch.Generator("cuda").manual_seed(31), device="cuda")
+    w = torch.zeros(out, inn, device="cuda")
+    w[torch.arange(inn) // 32 % out, torch.arange(inn)] = 1.0
+    packed = cp.cprune_mx_pack(w)
+    values = torch.zeros(rows, -(-inn // 32) * 32, device="cuda", dtype=torch.float64)
+    values[:, :inn] = cp.cprune_mx_quantize(x, inn, values=True)[2][:, :inn]
+    want = values.view(rows, -1, 32).sum(2)
+    assert want.shape[1] <= out
+    for _ in range(10):
+        y = cp.cprune_mx_fc(x, inn, *packed, out, out_f32=True)
+        assert torch.equal(y[:, :want.shape[1]].double(), want) and not y[:, want.shape[1]:].any()

@@ -8,9 +8,9 @@
 // tensor's address rounded down: a tensor may lie at any address of its type, and only its first and last vector are taken value by value.
 // Squares and their sums are float64: a float32 square loses gradients below 1e-19 and overflows above 1e19, and the sum runs over
 // millions of values.
-// What bounds it is memory for large lists, launches for small ones.  62 float32 tensors of 11.7 million values 15.2 us (read once and written: 14.3 us at a
-// copy's rate; the second reading comes from the L2 cache), pieces of 8 KB 17.4 us, eight blocks to an SM 15.9 us; 50 tensors of 2 million 78 us; 12 small ones
-// 4.0 us.
+// What bounds it is memory for large lists, launches for small ones.  62 float32 tensors of 11.7 million values in all 24.7 us (read once and written: 14.3 us at
+// a copy's rate; 12.7 of them for the norm alone), of 40 million, which do not stay in the cache, 85 us (read twice and written: 73); 12 small ones 5 us.
+// Eight blocks to an SM 24.9 and 84 us (bf16 17.2 us for 16.5), pieces of 32 KB 26.6 and 85; the sums in float32 would save 0.3 and 2 us.
 #include <cmath>
 
 #include "common.cuh"
@@ -45,6 +45,8 @@ struct GradSpan {
     }
     // whether vector v is partly outside
     __device__ __forceinline__ bool edge(unsigned long long v) const { return (v == 0 && skip) || (v + 1) * 16 > bytes; }
+    // whether the whole piece that begins at vector v is inside
+    __device__ __forceinline__ bool whole(unsigned long long v) const { return (v > 0 || !skip) && (v + GRAD_PIECE) * 16 <= bytes; }
     // its values, 0 in place of those outside
     __device__ __forceinline__ uint4 read(unsigned long long v) const {
         if (!edge(v)) return *(const uint4 *)(base + v * 16);
@@ -109,6 +111,19 @@ __device__ __forceinline__ int tensor_of(const GradTable<MOST> &t, unsigned piec
     return lo;
 }
 
+// This thread's vectors of a piece, zeros behind the tensor's end.  (Whole pieces without a test per vector: its branches would keep the loads from being under
+// way together.)
+__device__ __forceinline__ void read_piece(const GradSpan &span, unsigned long long first, uint4 *u) {
+    const unsigned long long v0 = first + threadIdx.x;
+    if (span.whole(first)) {
+#pragma unroll
+        for (int i = 0; i < GRAD_AHEAD; ++i) u[i] = *(const uint4 *)(span.base + (v0 + i * GRAD_T) * 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < GRAD_AHEAD; ++i) u[i] = (v0 + i * GRAD_T) * 16 < span.bytes ? span.read(v0 + i * GRAD_T) : make_uint4(0, 0, 0, 0);
+    }
+}
+
 template <int MOST>
 __global__ void __launch_bounds__(GRAD_T) gradient_squares_kernel(const __grid_constant__ GradTable<MOST> t, double *__restrict__ part) {
     pdl_wait();
@@ -121,10 +136,8 @@ __global__ void __launch_bounds__(GRAD_T) gradient_squares_kernel(const __grid_c
         for (; piece < end; ++piece) {
             while (t.first[k + 1] <= piece) ++k;
             const GradSpan span(t.g[k], t.count[k]);
-            const unsigned long long v0 = (unsigned long long)(piece - t.first[k]) * GRAD_PIECE + threadIdx.x;
             uint4 u[GRAD_AHEAD];
-#pragma unroll
-            for (int i = 0; i < GRAD_AHEAD; ++i) u[i] = (v0 + i * GRAD_T) * 16 < span.bytes ? span.read(v0 + i * GRAD_T) : make_uint4(0, 0, 0, 0);
+            read_piece(span, (unsigned long long)(piece - t.first[k]) * GRAD_PIECE, u);
 #pragma unroll
             for (int i = 0; i < GRAD_AHEAD; ++i) s += squares(u[i], span.bf16);
         }
@@ -169,21 +182,25 @@ __global__ void __launch_bounds__(GRAD_T) gradient_scale_kernel(const __grid_con
     if (last && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     const double c = (double)max_norm / (n + 1e-6);
     const float f = (float)(c > 1.0 ? 1.0 : c);            // (a NaN stays one)
-    unsigned piece, end;
-    share_of(t.first[t.n], piece, end);
-    if (piece >= end) return;
-    int k = tensor_of(t, piece);
-    for (; piece < end; ++piece) {
-        while (t.first[k + 1] <= piece) ++k;
+    unsigned begin, piece;
+    share_of(t.first[t.n], begin, piece);
+    if (begin >= piece) return;
+    // (backwards: what was read last is still in the cache)
+    int k = tensor_of(t, piece - 1);
+    while (piece-- > begin) {
+        while (t.first[k] > piece) --k;
         if (f == 1.f && t.out[k] == t.g[k]) continue;
         const GradSpan span(t.g[k], t.count[k]);
         const bool same = ((uintptr_t)t.out[k] & 15) == (uintptr_t)span.skip;      // vectors of the result are vectors of the gradient
         char *out = (char *)t.out[k] - span.skip;
-        const unsigned long long v0 = (unsigned long long)(piece - t.first[k]) * GRAD_PIECE + threadIdx.x;
+        const unsigned long long first = (unsigned long long)(piece - t.first[k]) * GRAD_PIECE, v0 = first + threadIdx.x;
         uint4 u[GRAD_AHEAD];
+        read_piece(span, first, u);
+        if (same && span.whole(first)) {
 #pragma unroll
-        for (int i = 0; i < GRAD_AHEAD; ++i)
-            if ((v0 + i * GRAD_T) * 16 < span.bytes) u[i] = span.read(v0 + i * GRAD_T);
+            for (int i = 0; i < GRAD_AHEAD; ++i) *(uint4 *)(out + (v0 + i * GRAD_T) * 16) = scaled(u[i], f, span.bf16);
+            continue;
+        }
 #pragma unroll
         for (int i = 0; i < GRAD_AHEAD; ++i) {
             const unsigned long long v = v0 + i * GRAD_T;

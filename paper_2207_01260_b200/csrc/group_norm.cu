@@ -15,6 +15,9 @@
 //     itself, in the same order, and goes over the data again, last pixels first, so that part of it still comes from the cache.
 // The variance is never a difference of large sums: a thread takes the deviations from its own mean, and means and deviations are put
 // together pairwise (Chan, Golub, LeVeque 1979), in float32.
+// What bounds it (us, with buffers that do not stay in the cache): small images the launch and the exchange, 1 x 7x7x352 4.5, 8 x 28x28x91 float32 6.4; large ones
+// the two passes, whose loads, arithmetic and stores wait for one another, 64 x 112x112x44 38 (read once and written: 22 at a copy's rate); gradients instructions
+// too, 64 x 56x56x108 with silu and a shortcut 67 (33), 8 x 14x14x180 7.4.
 #include <cmath>
 #include <mutex>
 #include <type_traits>
@@ -97,7 +100,6 @@ struct NormParams {
     int chunks;                         // two passes: blocks that share an image
     int gs, data_bytes;                 // on chip: groups of a slice, bytes of a tensor's share of a block
     int range, room, ring_bytes;        // two passes: groups that a slice touches at most, channels of these or of the slice (both even), bytes of the ring
-    int act;
     float eps;
 };
 
@@ -166,16 +168,6 @@ __device__ __forceinline__ void fill_column(Column<Lanes<KIND>::NP> &k, F of) {
         k.a[i] = two(v[2 * i].y, v[2 * i + 1].y);
         k.beta[i] = two(v[2 * i].z, v[2 * i + 1].z);
     }
-}
-// from global memory
-template <int KIND>
-__device__ __forceinline__ void load_column(const NormParams &p, Column<Lanes<KIND>::NP> &k, int n, int c0) {
-    fill_column<KIND>(k, [&](int l) {
-        const int c = c0 + l;
-        if (c >= p.C) return make_float3(0.f, 0.f, 0.f);
-        const float2 s = __ldcg((const float2 *)p.stats + (size_t)n * p.G + c / p.cpg);
-        return make_float3(-s.x, s.y * (p.gamma ? __ldg(p.gamma + c) : 1.f), p.beta ? __ldg(p.beta + c) : 0.f);
-    });
 }
 
 // x - mean, and z
@@ -987,7 +979,9 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
 
 // ------------------------------------------------------------------------------------------------------------- host
 
-// How the on-chip kernel shares out an image; ranks == 0: it does not take it.
+// How the on-chip kernel shares out an image; ranks == 0: it does not take it.  It takes what all fits at once, in two blocks to an SM of up to 12 pixels a thread.
+// us there / in two passes:  1 x 7x7x352 4.5 / 6.7, 8 x 28x28x128 5.8 / 7.8, 8 x 56x56x64 7.7 / 10.2, 64 x 14x14x360 9.0 / 17.8, 256 x 7x7x352 9.4 / 16.1,
+// 1 x 112x112x44 7.1 / 7.1;  with four blocks to an SM and 20 pixels 8 x 28x28x128 7.5, 8 x 56x56x64 9.0, 64 x 14x14x360 11.8.
 struct NormCluster {
     int ranks = 0, gs = 0, slices = 0, per = 0, widest = 0;
     size_t data_bytes = 0, smem = 0;
@@ -1149,9 +1143,9 @@ static cprune_status by_kind(int kind, int act, bool residual, F f) {
     return kind == 0 ? second(std::integral_constant<int, 0>()) : kind == 1 ? second(std::integral_constant<int, 1>()) : second(std::integral_constant<int, 2>());
 }
 
-static NormParams norm_params(int kind, int N, int H, int W, int C, int groups, int act, bool backward) {
+static NormParams norm_params(int kind, int N, int H, int W, int C, int groups, bool backward) {
     NormParams p = {};
-    p.N = N; p.HW = H * W; p.C = C; p.G = groups; p.cpg = C / groups; p.act = act;
+    p.N = N; p.HW = H * W; p.C = C; p.G = groups; p.cpg = C / groups;
     const NormTiling t = norm_tiling(kind, N, p.HW, C, groups, backward);
     p.pv = t.lanes / (kind == 0 ? 8 : kind == 1 ? 4 : 1);
     p.sv = t.sv; p.rows = t.rows; p.chunks = t.chunks;
@@ -1190,7 +1184,7 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
     const int kind = norm_kind(type, C, tensors);
     const NormCluster c = norm_cluster(kind, N, H * W, C, groups);
     if (!c.ranks && (workspace_bytes < norm_part_bytes(N, H * W, C, groups, kind) || !workspace)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
-    NormParams p = norm_params(kind, N, H, W, C, groups, act, false);
+    NormParams p = norm_params(kind, N, H, W, C, groups, false);
     p.x = x; p.res = residual; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats; p.eps = eps;
     p.part = (float2 *)workspace;
     const NormTiling t = norm_tiling(kind, N, p.HW, C, groups, false);
@@ -1224,7 +1218,7 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
     const int kind = norm_kind(type, C, tensors);
     const size_t part_bytes = norm_part_bytes(N, H * W, C, groups, kind);
     if (workspace_bytes < part_bytes || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
-    NormParams p = norm_params(kind, N, H, W, C, groups, act, true);
+    NormParams p = norm_params(kind, N, H, W, C, groups, true);
     p.x = x; p.dy = dy; p.res = residual; p.out = dx; p.dres = dresidual; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float *>(stats);
     p.dgamma = dgamma; p.dbeta = dbeta;
     p.part = (float2 *)workspace;

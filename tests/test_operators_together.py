@@ -1,5 +1,7 @@
 """The operators around the convolutions in one run, as they are used: a pruned conv task, group norm and activation, a 1x1 layer and the classifier in 4-bit
 weights; then the gradients of the norm's parameters, clipped together with others."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -101,4 +103,57 @@ def test_a_run_of_them_captured_and_replayed(cp):
         given.copy_(v)
         graph.replay()
         assert torch.equal(logits, w)
+    cp.cprune_poll_device_status()
+
+
+def work_of(cp, seed):
+    """A call of every kernel, at sizes that share an SM with other work: the results, and a function that makes them again."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    x, dy = (r(4, 56, 56, 56).bfloat16() for _ in range(2))
+    small, gamma, beta = r(2, 14, 14, 30), r(56), r(56)
+    rows, few = r(20000, 192).bfloat16(), r(8, 8192).bfloat16()
+    wide, deep, mid = cp.cprune_mx_pack(r(40, 192)), cp.cprune_mx_pack(r(256, 8192)), cp.cprune_mx_pack(r(600, 192))
+    grads = [r(3000), r(70000).bfloat16(), r(11)]
+
+    def again():
+        y, stats = cp.cprune_group_norm(x, 56, 7, gamma, beta, 1e-5, "relu", dy)
+        got = [y, stats, *cp.cprune_group_norm_backward(dy, x, 56, 7, stats, gamma, beta, "relu", y), *cp.cprune_group_norm(small, 30, 5)]
+        got += [cp.cprune_mx_fc(rows, 192, *wide, 40), cp.cprune_mx_fc(few, 8192, *deep, 256, "relu"), cp.cprune_mx_fc(rows, 192, *mid, 600, out_f32=True)]
+        got += [cp.cprune_mx_fc(few[:, :192].contiguous(), 192, *wide, 40)]
+        into = [torch.empty_like(t) for t in grads]
+        return got + [cp.cprune_clip_gradients(grads, 1.0, out=into), *into]
+
+    return again
+
+
+def test_threads_and_graphs_side_by_side(cp):
+    """Two threads on their own streams, then two graphs replayed on two streams at once: the bits of each alone."""
+    jobs = [work_of(cp, s) for s in (1, 2)]
+    want = [[t.clone() for t in j()] for j in jobs]
+    torch.cuda.synchronize()
+    wrong = [[], []]
+
+    def run(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(15):
+                wrong[k] += [i for i, (a, b) in enumerate(zip(jobs[k](), want[k])) if not torch.equal(a, b)]
+
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert wrong == [[], []]
+    graphs, got = [torch.cuda.CUDAGraph() for _ in jobs], []
+    for graph, job in zip(graphs, jobs):
+        with torch.cuda.graph(graph):
+            got.append(job())
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(10):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for k in range(2) for a, b in zip(got[k], want[k]))
     cp.cprune_poll_device_status()

@@ -13,8 +13,8 @@
 //     exchange their sums, and the data is read once.
 //   - two passes, a launch each: partial results of chunks of pixels per channel; every block of the second launch puts those of its groups together for
 //     itself, in the same order, and goes over the data again, last pixels first, so that part of it still comes from the cache.
-// The variance is never a difference of large sums: a thread takes the deviations from its own mean, and means and deviations are put
-// together pairwise (Chan, Golub, LeVeque 1979), in float32.
+// The variance is never a difference of large sums: a thread takes squares of differences from a value near its mean, in runs of a few dozen pixels, and means
+// and deviations of threads, chunks and channels are put together pairwise (Chan, Golub, LeVeque 1979), in float32.
 // What bounds it (us, with buffers that do not stay in the cache): small images the launch and the exchange, 1 x 7x7x352 4.5, 8 x 28x28x91 float32 6.4; large ones
 // the two passes, whose loads, arithmetic and stores wait for one another, 64 x 112x112x44 38 (read once and written: 22 at a copy's rate); gradients instructions
 // too, 64 x 56x56x108 with silu and a shortcut 67 (33), 8 x 14x14x180 7.4.
@@ -360,8 +360,9 @@ __device__ __forceinline__ void combine_rows(const float *v, int sv, int rows, i
     }
 }
 
-// A thread's sum and squared deviations, value by value.  The shift is its first value: a value that lies D from the mean of n has itself D^2 of the deviations
-// and leaves D^2 / (n - 1) to the others, so that n D^2, which the shift adds to the squares, is at most n - 1 times what is wanted.
+// A thread's sum and squared deviations, value by value, as differences from a shift that is worth n D^2 in the squares if it lies D from the mean of n values.
+// For few values (on chip: 12 at most) the first will do: it has itself D^2 of the deviations and leaves D^2 / (n - 1) to the others, so that n D^2 is at most n - 1
+// times what is wanted.
 template <int NP> struct Spread {
     f2 minus_shift[NP], s[NP], q[NP];
     __device__ __forceinline__ void begin(const f2 *first) {
@@ -390,6 +391,49 @@ template <int NP> struct Spread {
             v[l * NORM_PITCH + threadIdx.x] = n > 0 ? sum - shift * (float)n : 0.f;
             v[(L + l) * NORM_PITCH + threadIdx.x] = n > 0 ? (dev < 0.f ? 0.f : dev) : 0.f;         // (a NaN stays one: no maximum)
         }
+    }
+};
+
+// The same of any number of values, in runs: at the end of one, its squares are taken from the mean of all values so far, which becomes the shift of the next, and
+// added to those of the runs before.  The mean of the first four is where it begins: with the first of 1568 values as the only shift, and that
+// one far from a flat rest (1 x 112x112x1280, a group per channel), 1 / sqrt(variance) was off by 4.5e-3.  A run's squares are then at most twice what they add to the deviations (n of the first run's 12: three times), and
+// runs of about the root of n keep the additions in a row few.
+template <int NP> struct LongSpread : Spread<NP> {
+    using Spread<NP>::minus_shift;
+    using Spread<NP>::s;
+    using Spread<NP>::q;
+    f2 total[NP];
+    // f: the values, n of them (four at most)
+    __device__ __forceinline__ void begin(const f2 (*f)[NP], int n) {
+        const float part = n > 0 ? -inverse(n) : 0.f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            f2 sum = f[0][i];
+#pragma unroll
+            for (int k = 1; k < 4; ++k) sum = add2(sum, f[k][i]);
+            minus_shift[i] = fma2(sum, two(part, part), 0ull);
+            s[i] = q[i] = total[i] = 0ull;
+        }
+    }
+    // n: values so far
+    __device__ __forceinline__ void close(int n) {
+        const float inv = -inverse(n);
+        const f2 part = two(inv, inv), minus_one = two(-1.f, -1.f), count = two((float)n, (float)n);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const f2 to = fma2(s[i], part, minus_shift[i]);
+            const f2 by = fma2(minus_shift[i], minus_one, to);         // minus the way that the shift goes
+            const f2 rest = fma2(count, by, s[i]);                     // the sum of the differences from the new one
+            total[i] = add2(total[i], fma2(by, add2(s[i], rest), q[i]));
+            minus_shift[i] = to;
+            s[i] = rest;
+            q[i] = 0ull;
+        }
+    }
+    template <int L> __device__ __forceinline__ void store(float *v, int n) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) q[i] = add2(q[i], total[i]);
+        Spread<NP>::template store<L>(v, n);
     }
 };
 
@@ -485,8 +529,11 @@ template <typename Raw, int T, bool BACK> struct Stream {
 #pragma unroll
         for (int i = 0; i < RING - 1; ++i) issue(i);
     }
-    // f(where the pixel lies, places of its vectors, NORM_T apart)
-    template <typename F> __device__ __forceinline__ void run(F f) {
+    // f(where the pixel lies, places of its vectors, NORM_T apart); close(pixels so far) between runs of them: the first is a round of the ring, the others
+    // as many rounds as are next to the root of their number
+    template <typename F, typename G> __device__ __forceinline__ void run(F f, G close) {
+        const int rounds = max(1, __float2int_rn(sqrtf((float)cnt) * (1.f / RING)));
+        int run = 1;
 #pragma unroll 1
         for (int i = cnt; i > 0; i -= RING) {
 #pragma unroll
@@ -497,8 +544,15 @@ template <typename Raw, int T, bool BACK> struct Stream {
                 at += step;
                 issue((j + RING - 1) % RING);
             }
+            if (--run == 0 && i > RING) {
+                close(cnt - i + RING);
+                run = rounds;
+            }
         }
         copy_wait();
+    }
+    template <typename F> __device__ __forceinline__ void run(F f) {
+        run(f, [](int) {});
     }
 };
 
@@ -514,17 +568,20 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_partial_kernel(const __grid_co
     pdl_trigger();
     Stream<Raw, 1, false> x(norm_smem, c, p.x);
     x.begin();
-    Spread<NP> own;
+    LongSpread<NP> own;
     {
-        f2 f[NP];
-        Lanes<KIND>::unpack(c.cnt > 0 ? ((const Raw *)p.x)[c.at(0)] : Raw(), f);
-        own.begin(f);
+        f2 f[4][NP];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Lanes<KIND>::unpack(i < c.cnt ? ((const Raw *)p.x)[c.at(i)] : Raw(), f[i]);
+        own.begin(f, min(c.cnt, 4));
     }
-    x.run([&](size_t, const Raw *v) {
-        f2 f[NP];
-        Lanes<KIND>::unpack(*v, f);
-        own.add(f);                    // (its first value adds nothing)
-    });
+    x.run(
+        [&](size_t, const Raw *v) {
+            f2 f[NP];
+            Lanes<KIND>::unpack(*v, f);
+            own.add(f);
+        },
+        [&](int n) { own.close(n); });
     __syncthreads();
     if (c.r < c.rows) own.template store<L>(v, c.cnt);
     __syncthreads();

@@ -321,3 +321,35 @@ def test_python_refusals_on_the_device(cp):
     with pytest.raises(cp.CpruneError) as e:
         cp.cprune_group_norm_backward(x, x, 16, 2, torch.zeros((1, 2, 2), device="cuda"), workspace=torch.zeros(64, dtype=torch.uint8, device="cuda")[:16])
     assert e.value.status == 3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["first pixel", "top row", "steps", "normal"])
+@pytest.mark.parametrize("H,W,C,G,dtype", [
+    (112, 112, 512, 512, "bf16"), (112, 112, 512, 32, "bf16"), (224, 224, 256, 256, "bf16"), (112, 112, 1280, 1280, "bf16"), (112, 112, 1280, 32, "bf16"),
+    (112, 112, 512, 512, "f32"), (113, 111, 129, 129, "f32"), (112, 112, 44, 4, "bf16"), (56, 56, 12, 12, "f32"), (25, 25, 16, 16, "bf16")])
+def test_variance_of_images_with_a_border(cp, H, W, C, G, dtype, kind):
+    """Flat images but for their first pixel or row, as behind a convolution with padding, and steps: what is far from the rest is what a thread sees first, or many
+    times over.  At most 2^-24 a rounding: a thread's squares in runs of up to 40, of which up to half count in the mean and twice in what they add to the
+    deviations, 44 runs, half of them in the mean, 16 levels of sums of threads and chunks, 8 for the differences themselves: 94 units of the variance, 47 of rstd."""
+    g = torch.Generator(device="cuda").manual_seed(31)
+    x = torch.zeros((2, H, W, lanes(cp, C, dtype)), dtype=TYPES[dtype], device="cuda")
+    v = x[..., :C]
+    if kind == "normal":
+        v.copy_(torch.randn((2, H, W, C), generator=g, device="cuda") * 1.7 + 0.6)
+    else:
+        v.copy_(0.25 + torch.rand(C, generator=g, device="cuda"))
+        if kind == "first pixel":
+            v[0, 0, 0], v[1, -1, -1] = 40.0, -70.0
+        elif kind == "top row":
+            v[0, 0], v[1, :, 0] = 40.0, -70.0
+        else:
+            v[0, H // 2:], v[1, ::2] = 7.7, -0.3
+    for image in (x, x[:1]):
+        stats = cp.cprune_group_norm(image.contiguous(), C, G)[1]
+        w = image[..., :C].double().reshape(-1, H * W, G, C // G)
+        mean = w.mean((1, 3), keepdim=True)
+        rstd = 1 / (((w - mean) ** 2).mean((1, 3)) + EPS).sqrt()
+        mean = mean.reshape(rstd.shape)
+        close("mean", stats[..., 0], mean, UNITS * (mean.abs() + 1 / rstd))
+        close("rstd", stats[..., 1], rstd, UNITS * rstd)

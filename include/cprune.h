@@ -261,6 +261,8 @@ cprune_status cprune_fc(const void *x, int N, int in, const void *w_packed, cons
  *   y         may be x or residual;   stats  float32 [N][groups][2], written: mean and rstd, which the gradients need
  *   workspace cprune_group_norm_workspace_bytes, 16-byte aligned (0: none is needed, or the arguments are not in order)
  * A NaN in a group, or an infinity, makes its outputs NaN; the activations hand a NaN on.  Other groups keep their values.
+ * The sums of a group's values and of their squared deviations have to be float32 numbers, the values themselves may be larger than
+ * such a number's root.
  *
  * Gradients, given dy = dL/dy and the stats of the forward pass: dx, dgamma [C], dbeta [C] (either may be NULL) and
  * dresidual (NULL, or wanted, with residual given).  The slope of relu is 0 at 0, of relu6 0 at 0 and at 6; it is taken of the

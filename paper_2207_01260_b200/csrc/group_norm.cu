@@ -396,8 +396,8 @@ template <int NP> struct Spread {
 
 // The same of any number of values, in runs: at the end of one, its squares are taken from the mean of all values so far, which becomes the shift of the next, and
 // added to those of the runs before.  The mean of the first four is where it begins: with the first of 1568 values as the only shift, and that
-// one far from a flat rest (1 x 112x112x1280, a group per channel), 1 / sqrt(variance) was off by 4.5e-3.  A run's squares are then at most twice what they add to the deviations (n of the first run's 12: three times), and
-// runs of about the root of n keep the additions in a row few.
+// one far from a flat rest (1 x 112x112x1280, a group per channel), 1 / sqrt(variance) was off by 4.5e-3.  A run's squares are then at most twice what they add
+// to the deviations (the first run's three times), and runs of about the root of n keep the additions in a row few.
 template <int NP> struct LongSpread : Spread<NP> {
     using Spread<NP>::minus_shift;
     using Spread<NP>::s;
@@ -646,7 +646,7 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_apply_kernel(const __grid_cons
             const float mean = sum_sharers(s, log2) * inv_hw;
 #pragma unroll
             for (int i = 0; i < CHUNK_BATCH; ++i) {
-                const float d = w[i].x - mean;
+                const float d = pixels[i] > 0.f ? w[i].x - mean : 0.f;         // (the square of a mean past 2^64, times no pixels, is no number)
                 m2 += w[i].y + d * d * pixels[i];
             }
             m2 = sum_sharers(m2, log2);
@@ -999,7 +999,7 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
     // the ranks' groups to the image's
     const float pixels = (float)max(0, min(p.per, p.HW - (t & 15) * p.per));
     over_ranks(m.inbox, p.gs, s.sg, ranks, [&](int g, float2 w) {
-        const float mean = sum16(w.x * pixels) * inv_hw, d = w.x - mean;
+        const float mean = sum16(w.x * pixels) * inv_hw, d = pixels > 0.f ? w.x - mean : 0.f;
         const float m2 = sum16(w.y + d * d * pixels * (float)p.cpg);
         if (g < s.sg && (t & 15) == 0) {
             const float2 result = make_float2(mean, 1.f / sqrtf(m2 * inv_hw * inv_cpg + p.eps));

@@ -353,3 +353,16 @@ def test_variance_of_images_with_a_border(cp, H, W, C, G, dtype, kind):
         mean = mean.reshape(rstd.shape)
         close("mean", stats[..., 0], mean, UNITS * (mean.abs() + 1 / rstd))
         close("rstd", stats[..., 1], rstd, UNITS * rstd)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,H,W", [(2, 1, 1), (2, 5, 5), (2, 6, 6000), (40, 60, 60)])      # on chip, fewer blocks than an image can have; in two passes
+def test_means_whose_square_leaves_float32(cp, N, H, W):
+    """4e19, 1000 spreads: the deviations' squares are numbers."""
+    x = activation(cp, 32, N, H, W, 24, "f32", 4e16, 4e19)
+    y, stats = cp.cprune_group_norm(x.cuda(), 24, 24)
+    want, mean, rstd, _, _, size = reference(x, 24, 24, torch.ones(24), torch.zeros(24), "none", None)
+    close("mean", stats.cpu()[..., 0], mean, UNITS * (mean.abs() + 1 / rstd))
+    # (of a single value the variance is 0 in 64 bits; here its mean is rounded, which leaves it as it is)
+    close("rstd", stats.cpu()[..., 1], rstd, UNITS * rstd)
+    close("y", y.cpu(), want, STEP["f32"] * want.abs() + UNITS * size)

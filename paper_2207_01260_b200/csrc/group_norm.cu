@@ -529,11 +529,11 @@ template <typename Raw, int T, bool BACK> struct Stream {
 #pragma unroll
         for (int i = 0; i < RING - 1; ++i) issue(i);
     }
-    // f(where the pixel lies, places of its vectors, NORM_T apart); close(pixels so far) between runs of them: the first is a round of the ring, the others
-    // as many rounds as are next to the root of their number
-    template <typename F, typename G> __device__ __forceinline__ void run(F f, G close) {
-        const int rounds = max(1, __float2int_rn(sqrtf((float)cnt) * (1.f / RING)));
-        int run = 1;
+    // f(where the pixel lies, places of its vectors, NORM_T apart); close(pixels so far) between runs of them: the first has `first` rounds of the ring, the others
+    // as many as are next to the root of the number of pixels, and `first` at least
+    template <typename F, typename G> __device__ __forceinline__ void run(F f, int first, G close) {
+        const int rounds = max(first, __float2int_rn(sqrtf((float)cnt) * (1.f / RING)));
+        int run = first;
 #pragma unroll 1
         for (int i = cnt; i > 0; i -= RING) {
 #pragma unroll
@@ -552,7 +552,7 @@ template <typename Raw, int T, bool BACK> struct Stream {
         copy_wait();
     }
     template <typename F> __device__ __forceinline__ void run(F f) {
-        run(f, [](int) {});
+        run(f, 1, [](int) {});
     }
 };
 
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_partial_kernel(const __grid_co
             Lanes<KIND>::unpack(*v, f);
             own.add(f);
         },
-        [&](int n) { own.close(n); });
+        1, [&](int n) { own.close(n); });
     __syncthreads();
     if (c.r < c.rows) own.template store<L>(v, c.cnt);
     __syncthreads();
@@ -691,12 +691,16 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_apply_kernel(const __grid_cons
     x.run([&](size_t at, const Raw *v) { apply_one<KIND, ACT, RES>(p, k, v[0], v[RES ? NORM_T : 0], at); });
 }
 
-// Sums of dz and dz (x - mean) of a thread
-template <int NP> struct GradientSums {
-    f2 a[NP], b[NP];
-    __device__ __forceinline__ GradientSums() {
+// Sums of dz and dz (x - mean) of a thread.  RUNS: of many pixels, run by run; the sums of the runs before are kept in local memory, for which there are no registers
+// left.  In a single run 784 equal values were off by 8e-6 of their sum, 1568 by 1.1e-5.  (us with / without, which is why few pixels do without: 64 x 56x56x108 silu and shortcut, 30
+// pixels a thread, 70.8 / 68.9; 64 x 112x112x44 relu, 50 of them, 71.7 / 70.0; the sums before in registers, with spills, 72.6 and 73.7.)
+constexpr int GRADIENT_RUN = 30, GRADIENT_SINGLE = 64;         // pixels: of a run at least, of a single one at most
+template <int NP, bool RUNS> struct GradientSums {
+    f2 a[NP], b[NP], *before;
+    __device__ __forceinline__ explicit GradientSums(f2 (&place)[2 * NP]) : before(place) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) a[i] = b[i] = 0ull;
+        for (int i = 0; i < NP; ++i) a[i] = b[i] = before[i] = before[NP + i] = 0ull;
+        if (RUNS) asm volatile("" ::"l"(before) : "memory");   // (the address is out: the place stays in memory)
     }
     __device__ __forceinline__ void add(const f2 *d, const f2 *dz) {
 #pragma unroll
@@ -705,11 +709,21 @@ template <int NP> struct GradientSums {
             b[i] = fma2(dz[i], d[i], b[i]);
         }
     }
+    __device__ __forceinline__ void close() {
+        if (!RUNS) return;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            before[i] = add2(before[i], a[i]);
+            before[NP + i] = add2(before[NP + i], b[i]);
+            a[i] = b[i] = 0ull;
+        }
+    }
     template <int L> __device__ __forceinline__ void store(float *v) const {
 #pragma unroll
         for (int l = 0; l < L; ++l) {
-            v[l * NORM_PITCH + threadIdx.x] = l % 2 ? one_by_one(a[l / 2]).y : one_by_one(a[l / 2]).x;
-            v[(L + l) * NORM_PITCH + threadIdx.x] = l % 2 ? one_by_one(b[l / 2]).y : one_by_one(b[l / 2]).x;
+            const float2 s = one_by_one(RUNS ? add2(before[l / 2], a[l / 2]) : a[l / 2]), w = one_by_one(RUNS ? add2(before[NP + l / 2], b[l / 2]) : b[l / 2]);
+            v[l * NORM_PITCH + threadIdx.x] = l % 2 ? s.y : s.x;
+            v[(L + l) * NORM_PITCH + threadIdx.x] = l % 2 ? w.y : w.x;
         }
     }
 };
@@ -731,7 +745,7 @@ __device__ __forceinline__ void fetch_constants(const NormParams &p, const Chunk
 }
 
 // Sums of dz and dz xhat over a chunk of pixels, channel by channel
-template <int KIND, int ACT, bool RES>
+template <int KIND, int ACT, bool RES, bool RUNS>
 __global__ void __launch_bounds__(NORM_T, 3) norm_grad_partial_kernel(const __grid_constant__ NormParams p) {
     constexpr int L = Lanes<KIND>::L, NP = Lanes<KIND>::NP, T = RES ? 3 : 2;
     using Raw = typename Lanes<KIND>::Raw;
@@ -746,18 +760,21 @@ __global__ void __launch_bounds__(NORM_T, 3) norm_grad_partial_kernel(const __gr
     x.begin();
     fetch_constants<L>(p, c, constants);
     __syncthreads();
-    GradientSums<NP> sums;
+    f2 runs[2 * NP];
+    GradientSums<NP, RUNS> sums(runs);
     Column<NP> k;
     fill_column<KIND>(k, [&](int l) {
         const float4 w = constants[l * c.sv + c.col];
         return make_float3(w.x, w.y, w.z);
     });
-    x.run([&](size_t, const Raw *v) {
-        f2 d[NP], dz[NP];
-        const Raw *res = v + (RES ? 2 * NORM_T : 0);
-        gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, c0, v[0], v[NORM_T], *res, v, res, d, dz);
-        sums.add(d, dz);
-    });
+    x.run(
+        [&](size_t, const Raw *v) {
+            f2 d[NP], dz[NP];
+            const Raw *res = v + (RES ? 2 * NORM_T : 0);
+            gradient_one<KIND, ACT, RES>(p, k, blockIdx.z, c0, v[0], v[NORM_T], *res, v, res, d, dz);
+            sums.add(d, dz);
+        },
+        GRADIENT_RUN / Stream<Raw, T, false>::RING, [&](int) { sums.close(); });
     __syncthreads();
     if (c.r < c.rows) sums.template store<L>(v);
     __syncthreads();
@@ -1287,7 +1304,10 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
         ChainScope chain;
         const dim3 grid(t.chunks, t.slices, N);
         p.ring_bytes = norm_ring_bytes(K, R + 2);
-        const cprune_status e = launch_pass<norm_grad_partial_kernel<K, A, R>>(grid, p.ring_bytes + (size_t)p.sv * L_of(K) * 16, st, p, t.lanes);
+        const size_t smem = p.ring_bytes + (size_t)p.sv * L_of(K) * 16;
+        const bool runs = (p.HW / p.rows + p.chunks - 1) / p.chunks >= GRADIENT_SINGLE;           // (and one more pixel behind the last full round)
+        const cprune_status e = runs ? launch_pass<norm_grad_partial_kernel<K, A, R, true>>(grid, smem, st, p, t.lanes)
+                                     : launch_pass<norm_grad_partial_kernel<K, A, R, false>>(grid, smem, st, p, t.lanes);
         if (e != CPRUNE_OK) return e;
         chain.follow();
         return launch_pass<norm_grad_apply_kernel<K, A, R>>(dim3(t.chunks, t.slices, N + (dgamma || dbeta ? 1 : 0)), p.ring_bytes + norm_pass_bytes(p, L_of(K)), st, p, t.lanes);

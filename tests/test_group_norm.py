@@ -366,3 +366,37 @@ def test_means_whose_square_leaves_float32(cp, N, H, W):
     # (of a single value the variance is 0 in 64 bits; here its mean is rounded, which leaves it as it is)
     close("rstd", stats.cpu()[..., 1], rstd, UNITS * rstd)
     close("y", y.cpu(), want, STEP["f32"] * want.abs() + UNITS * size)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,W,C,G,dtype,act,with_res", [
+    (112, 112, 512, 32, "f32", "none", False), (113, 111, 129, 3, "f32", "relu", True), (112, 112, 1280, 1280, "bf16", "silu", False), (112, 112, 512, 512, "bf16", "relu6", True),
+    (40, 40, 44, 4, "f32", "silu", True), (97, 101, 24, 24, "f32", "none", True)])
+def test_gradients_of_one_sign(cp, H, W, C, G, dtype, act, with_res):
+    """The same dy everywhere, as of a mean: every addition of a thread rounds the same way.  Half of the additions of a run (64 at most, or 40 and 40 runs) count in the
+    mean of the partial sums, 13 for the sums over threads, 12 for chunks and channels: 65 roundings at most, some of them the other way."""
+    g = torch.Generator(device="cuda").manual_seed(33)
+    x, res, dy = (torch.zeros((1, H, W, lanes(cp, C, dtype)), dtype=TYPES[dtype], device="cuda") for _ in range(3))
+    x[..., :C] = torch.randn((1, H, W, C), generator=g, device="cuda")
+    res[..., :C] = torch.randn((1, H, W, C), generator=g, device="cuda")
+    dy[..., :C] = 0.1
+    gamma, beta = torch.rand(C, generator=g, device="cuda") + 0.5, torch.randn(C, generator=g, device="cuda")
+    if not with_res:
+        res = None
+    stats = torch.empty((1, G, 2), device="cuda")
+    _, mean, rstd, _, _, _ = reference(x, C, G, gamma, beta, act, res)
+    stats[..., 0], stats[..., 1] = mean, rstd
+    dx, dgamma, dbeta, _ = cp.cprune_group_norm_backward(dy, x, C, G, stats, gamma, beta, act, res)
+    _, _, rstd, z, xhat, size = reference(x, C, G, gamma, beta, act, res, stats)
+    dz = dy[..., :C].double() * slope64(z, act)
+    dz_off = UNITS * dy[..., :C].double() * (1.1 + 0.5 * size) if act == "silu" else torch.zeros_like(dz)
+    close("dbeta", dbeta, dz.sum((0, 1, 2)), (dz_off + UNITS * dz.abs()).sum((0, 1, 2)))
+    h_off = UNITS * (size / gamma.double())
+    close("dgamma", dgamma, (dz * xhat).sum((0, 1, 2)), (dz_off * xhat.abs() + dz.abs() * h_off + UNITS * (dz * xhat).abs()).sum((0, 1, 2)))
+    t, t_off, h, h_off = ((v.reshape(H * W, G, C // G)) for v in (dz * gamma.double(), (dz_off + UNITS * dz.abs()) * gamma.double(), xhat, h_off))
+    m1, m2 = t.mean((0, 2), keepdim=True), (t * h).mean((0, 2), keepdim=True)
+    m1_off, m2_off = t_off.mean((0, 2), keepdim=True) + UNITS * t.abs().mean((0, 2), keepdim=True), (t_off * h.abs() + t.abs() * h_off + UNITS * (t * h).abs()).mean((0, 2), keepdim=True)
+    r = rstd.reshape(1, G, 1)
+    want = r * (t - m1 - h * m2)
+    off = r * (t_off + m1_off + h.abs() * m2_off + h_off * m2.abs() + UNITS * (t.abs() + m1.abs() + (h * m2).abs()))
+    close("dx", dx[..., :C].reshape(want.shape), want, STEP[dtype] * want.abs() + off)

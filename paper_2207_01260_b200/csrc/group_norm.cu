@@ -710,9 +710,8 @@ template <int NP, bool RUNS> struct GradientSums {
         }
     }
     __device__ __forceinline__ void close() {
-        if (!RUNS) return;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
+        for (int i = 0; RUNS && i < NP; ++i) {
             before[i] = add2(before[i], a[i]);
             before[NP + i] = add2(before[NP + i], b[i]);
             a[i] = b[i] = 0ull;

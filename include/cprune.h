@@ -280,7 +280,8 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
 
 /* Global norm of the gradients of many tensors and clipping to a largest norm (the same training):
  *   norm = sqrt(sum of g^2 over all values of all tensors),   out = g min(1, max_norm / (norm + 1e-6))
- * Sums in float64, in a fixed order; out is rounded once.  A NaN anywhere makes the norm and every result NaN, an infinity the
+ * Sums in float64, in a fixed order; the factor and the products are rounded to float32, bf16 results once more; a norm that no
+ * float32 holds is infinite, the results are right all the same.  A NaN anywhere makes the norm and every result NaN, an infinity the
  * norm infinite and the results 0 (NaN where the infinity was): look at *norm before an update.
  *   grads   HOST array of n device addresses, counts and types (CPRUNE_TYPE_*) HOST arrays; a tensor is one run of counts[i]
  *           values at any address of its type; no two of them overlap; n and counts may be 0

@@ -159,9 +159,21 @@ __global__ void __launch_bounds__(GRAD_T) gradient_norm_kernel(const double *par
     if (threadIdx.x == 0) *norm = (float)n;
 }
 
-__device__ __forceinline__ uint4 scaled(const uint4 &u, float f, bool bf16) {
+// The values times the factor c, f in float32.  A factor next to or below the smallest normal number has not the digits (or is 0 where the results are not): such
+// products are taken in 64 bits.
+__device__ __forceinline__ uint4 scaled(const uint4 &u, float f, double c, bool bf16) {
     uint4 r = u;
     uint32_t *w = &r.x;
+    if (f < 1e-36f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (bf16) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn((float)(__uint_as_float(w[i] << 16) * c), (float)(__uint_as_float(w[i] & 0xffff0000u) * c));
+                w[i] = *reinterpret_cast<const uint32_t *>(&b);
+            } else w[i] = __float_as_uint((float)(__uint_as_float(w[i]) * c));
+        }
+        return r;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (bf16) {
@@ -180,8 +192,9 @@ __global__ void __launch_bounds__(GRAD_T) gradient_scale_kernel(const __grid_con
     pdl_trigger();
     const double n = total_norm(part, parts);
     if (last && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
-    const double c = (double)max_norm / (n + 1e-6);
-    const float f = (float)(c > 1.0 ? 1.0 : c);            // (a NaN stays one)
+    double c = (double)max_norm / (n + 1e-6);
+    c = c > 1.0 ? 1.0 : c;                                 // (a NaN stays one)
+    const float f = (float)c;
     unsigned begin, piece;
     share_of(t.first[t.n], begin, piece);
     if (begin >= piece) return;
@@ -198,14 +211,14 @@ __global__ void __launch_bounds__(GRAD_T) gradient_scale_kernel(const __grid_con
         read_piece(span, first, u);
         if (same && span.whole(first)) {
 #pragma unroll
-            for (int i = 0; i < GRAD_AHEAD; ++i) *(uint4 *)(out + (v0 + i * GRAD_T) * 16) = scaled(u[i], f, span.bf16);
+            for (int i = 0; i < GRAD_AHEAD; ++i) *(uint4 *)(out + (v0 + i * GRAD_T) * 16) = scaled(u[i], f, c, span.bf16);
             continue;
         }
 #pragma unroll
         for (int i = 0; i < GRAD_AHEAD; ++i) {
             const unsigned long long v = v0 + i * GRAD_T;
             if (v * 16 >= span.bytes) break;
-            const uint4 r = scaled(u[i], f, span.bf16);
+            const uint4 r = scaled(u[i], f, c, span.bf16);
             if (same && !span.edge(v)) {
                 *(uint4 *)(out + v * 16) = r;
                 continue;

@@ -200,3 +200,20 @@ def test_overlap_by_the_steps_in_python(cp):
     for a, c, t, o in (([100, 160], [16, 3], [1, 0], None), ([164, 100], [3, 17], [0, 1], None), ([100, 164], [16, 3], [1, 0], [100, 166]), ([100, 200], [4, 4], [1, 1], [200, 300])):
         with pytest.raises(cp.CpruneError):
             refuse("f", a, c, t, o)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtypes", [["f32"], ["bf16"], ["f32", "bf16"]])
+def test_factors_below_the_smallest_normal_number(cp, dtypes):
+    """2e37 a value, clipped to 1e-2: a factor of 3e-43, results of 6e-6 (and one of 1e-12, results of some hundred times 2^-149)."""
+    for scale, max_norm in ((2e37, 1e-2), (1e30, 1e-42), (1e-3, 1e-42)):
+        grads = tensors(7, [2_000_000, 33, 1_000_001], dtypes, 1, scale)
+        want_norm, want = expected(grads, max_norm)
+        norm = cp.cprune_clip_gradients(grads, max_norm)
+        assert torch.isinf(norm) if want_norm > 3.5e38 else abs(float(norm) - want_norm) <= 2.0 ** -23 * want_norm
+        for t, w in zip(grads, want):
+            step = STEP["bf16" if t.dtype == torch.bfloat16 else "f32"]
+            # max_norm itself becomes a float32; below the smallest normal number a multiple of 2^-149, of 2^-133 as bf16, which is half a step off at most
+            w = w * (ctypes.c_float(max_norm).value / max_norm)
+            off = (t.cpu().double() - w).abs()
+            assert torch.all(off <= (step + 2.0 ** -22) * w.abs() + (2.0 ** -134 + 2.0 ** -149 if t.dtype == torch.bfloat16 else 2.0 ** -149)), scale

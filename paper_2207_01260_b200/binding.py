@@ -165,11 +165,18 @@ def lib():
             from . import _torch_calls
         except ImportError as e:
             raise RuntimeError("_torch_calls.so is missing; build it with `python -m paper_2207_01260_b200.build`") from e
-        _torch_calls.load(*(ctypes.cast(getattr(L, n), c_void_p).value for n in (
-            "cprune_padded_channels", "cprune_group_norm_workspace_bytes", "cprune_group_norm", "cprune_group_norm_backward", "cprune_gradient_workspace_bytes",
-            "cprune_clip_gradients", "cprune_mx_quantize", "cprune_mx_fc_workspace_bytes", "cprune_mx_fc")))
+        _hand_over(_torch_calls, L)
         _lib, _calls = L, _torch_calls
     return _lib
+
+
+# What csrc/torch_calls.cpp calls, in its order
+_HANDED_OVER = ("cprune_padded_channels", "cprune_group_norm_workspace_bytes", "cprune_group_norm", "cprune_group_norm_backward", "cprune_gradient_workspace_bytes",
+                "cprune_clip_gradients", "cprune_mx_quantize", "cprune_mx_fc_workspace_bytes", "cprune_mx_fc")
+
+
+def _hand_over(calls, L):
+    calls.load(_check, *(ctypes.cast(getattr(L, n), c_void_p).value for n in _HANDED_OVER))
 
 
 def _check(status: int, where: str):
@@ -490,7 +497,7 @@ def cprune_fc(x, in_features, w_packed, b_packed, out_features, activation="none
 # The operators below check what they are given before they hand addresses on: a tensor of another type, shape or device would be read out of
 # bounds.  What they allocate belongs to the stream that they run on, so that a workspace is not handed out again while it is in use there.
 # A call with nothing but its inputs, which allocates its results and runs on the current stream, is tried by csrc/torch_calls.cpp first: the same
-# steps in compiled code, which gives up (None) where anything is not in order.  What depends on sizes alone is remembered by sizes.
+# steps in compiled code, which gives up (None) where anything is not in order, and raises where the library fails on the way.  What depends on sizes alone is remembered by sizes.
 TYPE = {torch.bfloat16: 0, torch.float32: 1}
 _BF16, _F32, _U8 = torch.bfloat16, torch.float32, torch.uint8
 _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device

@@ -1,6 +1,7 @@
 // The operators' calls as programs make them most of the time (tensors that are in order, results allocated by the call, the current stream), without
 // the interpreter between the checks: what a small call costs is spent on the host.  A function here checks its tensors, allocates the results and calls the C
-// ABI; where anything is not in order, or the library refuses, it returns None, and binding.py goes through the same steps itself and says what is wrong.
+// ABI; where anything is not in order, or the library refuses, it returns None, and binding.py goes through the same steps itself and says what is wrong.  Where
+// the library fails on the way (CUDA), part of the work may be under way: that is raised here, and nothing is tried again.
 // (us a call of a 7x7x352 image's group norm: 12.7 by binding.py's own steps, 5.8 here.)
 #include <Python.h>
 
@@ -51,17 +52,27 @@ struct Argument {
 
 int library_type(at::ScalarType t) { return t == at::kBFloat16 ? CPRUNE_TYPE_BF16 : t == at::kFloat ? CPRUNE_TYPE_F32 : -1; }
 
-// Runs f without the interpreter's lock, so that a launch that has to wait holds up nobody else; None unless it succeeded
-template <typename F> bool call(F f) {
-    cprune_status s;
-    Py_BEGIN_ALLOW_THREADS
-    s = f();
-    Py_END_ALLOW_THREADS
-    return s == CPRUNE_OK;
+// Runs f without the interpreter's lock, so that a launch that has to wait holds up nobody else (an exception takes the lock back first)
+template <typename F> cprune_status call(F f) {
+    struct Unlocked {
+        PyThreadState *state = PyEval_SaveThread();
+        ~Unlocked() { PyEval_RestoreThread(state); }
+    } unlocked;
+    return f();
 }
 PyObject *none() {
     PyErr_Clear();
     Py_RETURN_NONE;
+}
+PyObject *raise_for;                    // binding.py's function that raises for a status
+
+// What a call returns that has not succeeded: None where its arguments were refused (nothing is under way), else an exception
+PyObject *failed(cprune_status s, const char *where) {
+    if (s == CPRUNE_ERR_INVALID_ARG || s == CPRUNE_ERR_UNSUPPORTED || s == CPRUNE_ERR_WORKSPACE_TOO_SMALL) return none();
+    PyObject *r = PyObject_CallFunction(raise_for, "is", (int)s, where);
+    Py_XDECREF(r);
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, where);
+    return nullptr;
 }
 PyObject *pack(std::initializer_list<PyObject *> items) {
     PyObject *r = PyTuple_New((Py_ssize_t)items.size());
@@ -122,10 +133,11 @@ PyObject *group_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int N = (int)x.size(0), H = (int)x.size(1), W = (int)x.size(2);
         const size_t need = lib.group_norm_workspace_bytes(v.type, N, H, W, C, groups, 0);
         at::Tensor y = at::empty(x.sizes(), x.options()), stats = at::empty({N, groups, 2}, x.options().dtype(at::kFloat)), work = bytes_like(x, need);
-        if (!call([&] {
-                return lib.group_norm(x.data_ptr(), v.type, N, H, W, C, groups, (const float *)gamma.address(), (const float *)beta.address(), (float)eps, act, res.address(),
-                                      y.data_ptr(), (float *)stats.data_ptr(), need ? work.data_ptr() : nullptr, need, stream());
-            })) return none();
+        const cprune_status st = call([&] {
+            return lib.group_norm(x.data_ptr(), v.type, N, H, W, C, groups, (const float *)gamma.address(), (const float *)beta.address(), (float)eps, act, res.address(),
+                                  y.data_ptr(), (float *)stats.data_ptr(), need ? work.data_ptr() : nullptr, need, stream());
+        });
+        if (st != CPRUNE_OK) return failed(st, "cprune_group_norm");
         return pack({THPVariable_Wrap(y), THPVariable_Wrap(stats)});
     });
 }
@@ -148,11 +160,12 @@ PyObject *group_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const auto f32 = x.options().dtype(at::kFloat);
         at::Tensor dx = at::empty(x.sizes(), x.options()), dgamma = at::empty({C}, f32), dbeta = at::empty({C}, f32), work = bytes_like(x, need), dres;
         if (res.t) dres = at::empty(x.sizes(), x.options());
-        if (!call([&] {
-                return lib.group_norm_backward(dy.address(), x.data_ptr(), v.type, N, H, W, C, groups, (const float *)stats.address(), (const float *)gamma.address(),
-                                               (const float *)beta.address(), act, res.address(), dx.data_ptr(), (float *)dgamma.data_ptr(), (float *)dbeta.data_ptr(),
-                                               res.t ? dres.data_ptr() : nullptr, need ? work.data_ptr() : nullptr, need, stream());
-            })) return none();
+        const cprune_status st = call([&] {
+            return lib.group_norm_backward(dy.address(), x.data_ptr(), v.type, N, H, W, C, groups, (const float *)stats.address(), (const float *)gamma.address(),
+                                           (const float *)beta.address(), act, res.address(), dx.data_ptr(), (float *)dgamma.data_ptr(), (float *)dbeta.data_ptr(),
+                                           res.t ? dres.data_ptr() : nullptr, need ? work.data_ptr() : nullptr, need, stream());
+        });
+        if (st != CPRUNE_OK) return failed(st, "cprune_group_norm_backward");
         return pack({THPVariable_Wrap(dx), THPVariable_Wrap(dgamma), THPVariable_Wrap(dbeta), res.t ? THPVariable_Wrap(dres) : no_object()});
     });
 }
@@ -212,10 +225,11 @@ PyObject *clip_gradients(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const size_t need = lib.gradient_workspace_bytes(count);
         const auto like = at::TensorOptions().device(at::kCUDA, device);
         at::Tensor norm = at::empty({1}, like.dtype(at::kFloat)), work = at::empty({(int64_t)need}, like.dtype(at::kByte));
-        if (!call([&] {
-                return lib.clip_gradients(g.addresses.data(), g.counts.data(), g.types.data(), count, (float)max_norm, a[2] != Py_None ? o.addresses.data() : nullptr,
-                                          (float *)norm.data_ptr(), work.data_ptr(), need, stream());
-            })) return none();
+        const cprune_status st = call([&] {
+            return lib.clip_gradients(g.addresses.data(), g.counts.data(), g.types.data(), count, (float)max_norm, a[2] != Py_None ? o.addresses.data() : nullptr,
+                                      (float *)norm.data_ptr(), work.data_ptr(), need, stream());
+        });
+        if (st != CPRUNE_OK) return failed(st, "cprune_clip_gradients");
         return THPVariable_Wrap(norm);
     });
 }
@@ -240,8 +254,10 @@ PyObject *mx_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const bool with_values = a[2] == Py_True;
         at::Tensor codes = at::empty({rows, blocks * 16}, u8), scales = at::empty({(rows + 127) / 128, (blocks + 3) / 4, 32, 4, 4}, u8), values;
         if (with_values) values = at::empty(x.sizes(), x.options());
-        if (!call([&] { return lib.mx_quantize(x.data_ptr(), v.type, (size_t)rows, C, codes.data_ptr(), scales.data_ptr(), with_values ? values.data_ptr() : nullptr, stream()); }))
-            return none();
+        const cprune_status st = call([&] {
+            return lib.mx_quantize(x.data_ptr(), v.type, (size_t)rows, C, codes.data_ptr(), scales.data_ptr(), with_values ? values.data_ptr() : nullptr, stream());
+        });
+        if (st != CPRUNE_OK) return failed(st, "cprune_mx_quantize");
         return pack({THPVariable_Wrap(codes), THPVariable_Wrap(scales), with_values ? THPVariable_Wrap(values) : no_object()});
     });
 }
@@ -265,24 +281,31 @@ PyObject *mx_fc(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (f32) shape.back() = out;
         const size_t need = lib.mx_fc_workspace_bytes((size_t)rows, in, out);
         at::Tensor y = at::empty(shape, x.options().dtype(f32 ? at::kFloat : at::kBFloat16)), work = bytes_like(x, need);
-        if (!call([&] {
-                return lib.mx_fc(x.data_ptr(), (size_t)rows, in, codes.address(), scales.address(), (const float *)bias.address(), out, act, res.address(), f32, y.data_ptr(),
-                                 need ? work.data_ptr() : nullptr, need, stream());
-            })) return none();
+        const cprune_status st = call([&] {
+            return lib.mx_fc(x.data_ptr(), (size_t)rows, in, codes.address(), scales.address(), (const float *)bias.address(), out, act, res.address(), f32, y.data_ptr(),
+                             need ? work.data_ptr() : nullptr, need, stream());
+        });
+        if (st != CPRUNE_OK) return failed(st, "cprune_mx_fc");
         return THPVariable_Wrap(y);
     });
 }
 
-// load(addresses of the library's functions, in the order of `Library`)
+// load(function that raises for a status, addresses of the library's functions in the order of `Library`)
 PyObject *load(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != (Py_ssize_t)(sizeof(Library) / sizeof(void *))) {
-        PyErr_SetString(PyExc_TypeError, "load: the library's functions, one by one");
+    if (n != 1 + (Py_ssize_t)(sizeof(Library) / sizeof(void *))) {
+        PyErr_SetString(PyExc_TypeError, "load: a function that raises, the library's functions, one by one");
         return nullptr;
     }
     void *f[sizeof(Library) / sizeof(void *)];
-    for (Py_ssize_t i = 0; i < n; ++i)
-        if (!(f[i] = PyLong_AsVoidPtr(a[i]))) return nullptr;
+    for (Py_ssize_t i = 1; i < n; ++i)
+        if (!(f[i - 1] = PyLong_AsVoidPtr(a[i]))) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "load: a function without an address");
+            return nullptr;
+        }
     std::memcpy(&lib, f, sizeof(Library));
+    Py_INCREF(a[0]);
+    Py_XDECREF(raise_for);
+    raise_for = a[0];
     Py_RETURN_NONE;
 }
 

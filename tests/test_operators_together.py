@@ -157,3 +157,42 @@ def test_threads_and_graphs_side_by_side(cp):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for k in range(2) for a, b in zip(got[k], want[k]))
     cp.cprune_poll_device_status()
+
+
+def test_a_call_that_failed_on_the_way_is_not_made_again(cp, monkeypatch):
+    """Functions that say that a launch failed, in the library's place: a clipping in place has perhaps scaled a part of the list by then."""
+    import ctypes
+    b, made = cp.binding, []
+
+    class Failing:
+        def __getattr__(self, name):
+            real = getattr(b._lib, name)
+            if name.endswith("_bytes") or name == "cprune_padded_channels":
+                return real
+            fake = ctypes.CFUNCTYPE(ctypes.c_int, *real.argtypes)(lambda *a: made.append(name) or 4)
+            keep.append(fake)
+            return fake
+
+    keep = []
+    x = torch.zeros((2, 5, 5, 16), dtype=torch.bfloat16, device="cuda")
+    _, stats = cp.cprune_group_norm(x, 16, 2)
+    packed = cp.cprune_mx_pack(torch.zeros((8, 16), device="cuda"))
+    calls = {"cprune_group_norm": lambda: cp.cprune_group_norm(x, 16, 2), "cprune_group_norm_backward": lambda: cp.cprune_group_norm_backward(x, x, 16, 2, stats),
+             "cprune_clip_gradients": lambda: cp.cprune_clip_gradients([x], 1.0), "cprune_mx_quantize": lambda: cp.cprune_mx_quantize(x, 16),
+             "cprune_mx_fc": lambda: cp.cprune_mx_fc(x, 16, *packed, 8)}
+    real, failing = b._lib, Failing()
+    try:
+        b._hand_over(b._calls, failing)
+        for name, call in calls.items():
+            # a second try, by the steps in Python, would reach the real function: count it there as well
+            monkeypatch.setattr(real, name, lambda *a, name=name: made.append(name) or 4)
+            made.clear()
+            with pytest.raises(cp.CpruneError) as e:
+                call()
+            assert e.value.status == 4 and name in str(e.value) and made == [name]
+            monkeypatch.undo()
+    finally:
+        b._hand_over(b._calls, real)
+    for call in calls.values():
+        call()
+    torch.cuda.synchronize()

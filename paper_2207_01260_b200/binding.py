@@ -7,6 +7,7 @@ import functools
 import math
 import operator
 import os
+import warnings
 from array import array
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_longlong, c_size_t, c_void_p
 
@@ -90,6 +91,13 @@ _lib = None
 _calls = None                              # the module of csrc/torch_calls.cpp, once the library is loaded
 
 
+class _NoCalls:
+    """In the place of _torch_calls where that does not load (built for another version of torch, or not at all): every call gives up, and the steps below make it."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 def lib():
     """The loaded library.  Raises if it has not been built: there is no fallback path."""
     global _lib, _calls
@@ -162,11 +170,13 @@ def lib():
         L.cprune_mx_fc_workspace_bytes.argtypes = [c_size_t, c_int, c_int]
         L.cprune_mx_fc.argtypes = [c_void_p, c_size_t, c_int] + [c_void_p] * 3 + [c_int, c_int, c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p]
         try:
-            from . import _torch_calls
-        except ImportError as e:
-            raise RuntimeError("_torch_calls.so is missing; build it with `python -m paper_2207_01260_b200.build`") from e
-        _hand_over(_torch_calls, L)
-        _lib, _calls = L, _torch_calls
+            from . import _torch_calls as calls
+            _hand_over(calls, L)
+        except (ImportError, TypeError) as e:
+            warnings.warn("_torch_calls.so does not load (%s): the operators' calls take their steps in Python; build it with "
+                          "`python -m paper_2207_01260_b200.build`" % e, RuntimeWarning, stacklevel=2)
+            calls = _NoCalls()
+        _lib, _calls = L, calls
     return _lib
 
 

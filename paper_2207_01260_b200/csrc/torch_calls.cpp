@@ -315,4 +315,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__torch_calls() { return PyModule_Create(&module); }
+// (build.py looks for this text in the built file)
+PyMODINIT_FUNC PyInit__torch_calls() {
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built", BUILT_FOR) < 0) Py_CLEAR(m);
+    return m;
+}

@@ -266,7 +266,8 @@ cprune_status cprune_fc(const void *x, int N, int in, const void *w_packed, cons
  *
  * Gradients, given dy = dL/dy and the stats of the forward pass: dx, dgamma [C], dbeta [C] (either may be NULL) and
  * dresidual (NULL, or wanted, with residual given).  The slope of relu is 0 at 0, of relu6 0 at 0 and at 6; it is taken of the
- * z that x, stats, gamma, beta and residual give.  dx and dresidual may be dy or x, but not each other.
+ * z that x, stats, gamma, beta and residual give.  dx and dresidual may be dy, x or residual, but not each other.
+ * Results that overlap an input, or one another, in any other way are refused (INVALID_ARG).
  * Results do not depend on timing (no atomics).  bf16 tensors are 16-byte aligned, all others to their elements.
  * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (an image of 2^31 values or more, N > 65534, C > 2^20, a
  * group of more than 8192 channels), CUDA.  Enqueue only; at most two launches. */
@@ -313,6 +314,7 @@ cprune_status cprune_clip_gradients(const void *const *grads, const unsigned lon
  *   x  bf16 [rows][in_pad], a row per image or pixel;  residual  bf16 [rows][out_pad] or NULL;  act none, relu or relu6 (a NaN stays
  *   one);  y  bf16 [rows][out_pad] (pad lanes zero) or float32 [rows][out] when out_is_f32; it may be residual, not x
  *   workspace  cprune_mx_fc_workspace_bytes, device, 16-byte aligned
+ * Results that overlap an input, or one another, in any other way than said are refused (INVALID_ARG).
  * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows of a product, 2^40 of a rounding, more than 2^22 channels or 2^24
  * features), CUDA; a wait of the product's that ran out is reported by cprune_poll_device_status.  Enqueue only; at most three
  * launches. */

@@ -81,6 +81,18 @@ struct ChainScope {
     ~ChainScope() { set_chain_launch(before); }
 };
 
+// A buffer of an operator; what is written lies apart from the others, or (where a block reads its own places before it writes them) in exactly the same place.
+struct Buffer {
+    const void *at;
+    size_t bytes;
+};
+inline bool apart(const Buffer &a, const Buffer &b) {
+    const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+    return !a.at || !b.at || !a.bytes || !b.bytes || x + a.bytes <= y || y + b.bytes <= x;
+}
+inline bool same_or_apart(const Buffer &a, const Buffer &b) { return a.at == b.at || apart(a, b); }
+template <typename... Others> bool apart_from(const Buffer &a, const Others &...others) { return (apart(a, others) && ...); }
+
 inline int round_up(int v, int m) { return (v + m - 1) / m * m; }
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 

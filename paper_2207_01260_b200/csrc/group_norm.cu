@@ -1191,6 +1191,10 @@ static size_t norm_part_bytes(int N, int HW, int C, int G, int kind) {
     return ((size_t)N * t.chunks * t.lanes * sizeof(float2) + 255) / 256 * 256;
 }
 
+static size_t norm_bytes(int type, int N, int H, int W, int C) {
+    return (size_t)N * H * W * (type == CPRUNE_TYPE_BF16 ? cprune_padded_channels(C) * sizeof(__nv_bfloat16) : C * sizeof(float));
+}
+
 constexpr int NORM_GROUP = 8192;          // channels of a group: the second pass holds two groups' results in shared memory
 
 static cprune_status norm_check(int type, int N, int H, int W, int C, int groups, int act) {
@@ -1257,6 +1261,11 @@ cprune_status cprune_group_norm(const void *x, int type, int N, int H, int W, in
     const int kind = norm_kind(type, C, tensors);
     const NormCluster c = norm_cluster(kind, N, H * W, C, groups);
     if (!c.ranks && (workspace_bytes < norm_part_bytes(N, H * W, C, groups, kind) || !workspace)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    const size_t bytes = norm_bytes(type, N, H, W, C), channels = (size_t)C * 4;
+    const Buffer bx{x, bytes}, br{residual, bytes}, by{y, bytes}, bg{gamma, channels}, bb{beta, channels}, bs{stats, (size_t)N * groups * 8};
+    const Buffer bw{c.ranks ? nullptr : workspace, norm_part_bytes(N, H * W, C, groups, kind)};
+    if (!same_or_apart(by, bx) || !same_or_apart(by, br) || !apart_from(by, bg, bb) || !apart_from(bs, bx, br, by, bg, bb) || !apart_from(bw, bx, br, by, bg, bb, bs))
+        return CPRUNE_ERR_INVALID_ARG;
     NormParams p = norm_params(kind, N, H, W, C, groups, false);
     p.x = x; p.res = residual; p.out = y; p.gamma = gamma; p.beta = beta; p.stats = stats; p.eps = eps;
     p.part = (float2 *)workspace;
@@ -1291,6 +1300,14 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
     const int kind = norm_kind(type, C, tensors);
     const size_t part_bytes = norm_part_bytes(N, H * W, C, groups, kind);
     if (workspace_bytes < part_bytes || !workspace) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    const size_t bytes = norm_bytes(type, N, H, W, C), channels = (size_t)C * 4;
+    const Buffer bx{x, bytes}, br{residual, bytes}, by{dy, bytes}, bdx{dx, bytes}, bdr{dresidual, bytes}, bw{workspace, part_bytes};
+    const Buffer bg{gamma, channels}, bb{beta, channels}, bdg{dgamma, channels}, bdb{dbeta, channels}, bs{stats, (size_t)N * groups * 8};
+    for (const Buffer &b : {bdx, bdr})
+        if (!same_or_apart(b, bx) || !same_or_apart(b, br) || !same_or_apart(b, by) || !apart_from(b, bg, bb, bs)) return CPRUNE_ERR_INVALID_ARG;
+    for (const Buffer &b : {bdg, bdb, bw})
+        if (!apart_from(b, bx, br, by, bdx, bdr, bg, bb, bs)) return CPRUNE_ERR_INVALID_ARG;
+    if (!apart(bdx, bdr) || !apart(bdg, bdb) || !apart_from(bw, bdg, bdb)) return CPRUNE_ERR_INVALID_ARG;
     NormParams p = norm_params(kind, N, H, W, C, groups, true);
     p.x = x; p.dy = dy; p.res = residual; p.out = dx; p.dres = dresidual; p.gamma = gamma; p.beta = beta; p.stats = const_cast<float *>(stats);
     p.dgamma = dgamma; p.dbeta = dbeta;

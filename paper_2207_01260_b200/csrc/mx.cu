@@ -319,11 +319,15 @@ static cprune_status mx_check(const void *x, int type, size_t rows, int C, const
     return CPRUNE_OK;
 }
 
+static size_t mx_matrix_bytes(int type, size_t rows, int pitch) { return rows * pitch * (type == CPRUNE_TYPE_BF16 ? 2 : 4); }
+
 cprune_status cprune_mx_quantize(const void *x, int type, size_t rows, int C, void *codes, void *scales, void *values, void *stream) {
     const cprune_status c = mx_check(x, type, rows, C, codes, scales);
     if (c != CPRUNE_OK) return c;
     if ((!codes && !values) || (uintptr_t)values & (type == CPRUNE_TYPE_BF16 ? 15 : 3)) return CPRUNE_ERR_INVALID_ARG;
     const int tiles4 = (mx_blocks(C) + 3) / 4, pitch = type == CPRUNE_TYPE_BF16 ? cprune_padded_channels(C) : C;
+    const Buffer bx{x, mx_matrix_bytes(type, rows, pitch)}, bv{values, bx.bytes}, bc{codes, rows * mx_blocks(C) * 16}, bs{scales, cprune_mx_scale_bytes(rows, C)};
+    if (!same_or_apart(bv, bx) || !apart_from(bc, bx, bv, bs) || !apart_from(bs, bx, bv)) return CPRUNE_ERR_INVALID_ARG;
     const dim3 grid = mx_grid(rows, tiles4);
     auto launch = [&](auto kernel) {
         return launch_chained(kernel, grid, dim3(MX_T), 0, (cudaStream_t)stream, x, (unsigned long long)rows, C, pitch, tiles4, (uint32_t *)codes, (uint8_t *)scales, values);
@@ -341,6 +345,8 @@ cprune_status cprune_mx_dequantize(const void *codes, const void *scales, size_t
     const cprune_status c = mx_check(values, type, rows, C, codes, scales);
     if (c != CPRUNE_OK) return c;
     const int tiles4 = (mx_blocks(C) + 3) / 4, pitch = type == CPRUNE_TYPE_BF16 ? cprune_padded_channels(C) : C;
+    if (!apart_from(Buffer{values, mx_matrix_bytes(type, rows, pitch)}, Buffer{codes, rows * mx_blocks(C) * 16}, Buffer{scales, cprune_mx_scale_bytes(rows, C)}))
+        return CPRUNE_ERR_INVALID_ARG;
     const unsigned long long all = (rows * ((pitch + 7) / 8) + MX_T - 1) / MX_T;
     const unsigned grid = (unsigned)(all < 148 * 16 ? all : 148 * 16);
     auto launch = [&](auto kernel) {
@@ -357,11 +363,15 @@ cprune_status cprune_mx_dequantize(const void *codes, const void *scales, size_t
 
 cprune_status cprune_mx_pack(const float *w, const float *b, int out, int in, void *codes, void *scales, float *b_packed, void *stream) {
     if (!codes || !b_packed || out <= 0 || ((uintptr_t)b | (uintptr_t)b_packed) & 3) return CPRUNE_ERR_INVALID_ARG;
+    const int out_pad = cprune_padded_channels(out);
+    if (in > 0 && !apart_from(Buffer{b_packed, (size_t)out_pad * 4}, Buffer{w, (size_t)out * in * 4}, Buffer{b, (size_t)out * 4}, Buffer{codes, (size_t)out * mx_blocks(in) * 16},
+                              Buffer{scales, cprune_mx_scale_bytes(out, in)})) return CPRUNE_ERR_INVALID_ARG;
+    for (const Buffer &r : {Buffer{codes, (size_t)out * cprune_mx_blocks(in) * 16}, Buffer{scales, cprune_mx_scale_bytes(out, in)}})
+        if (!apart(r, Buffer{b, (size_t)out * 4})) return CPRUNE_ERR_INVALID_ARG;
     ChainScope chain;
     const cprune_status s = cprune_mx_quantize(w, CPRUNE_TYPE_F32, out, in, codes, scales, nullptr, stream);
     if (s != CPRUNE_OK) return s;
     chain.follow();
-    const int out_pad = cprune_padded_channels(out);
     CPRUNE_CUDA_CHECK(launch_chained(mx_pad_bias_kernel, dim3((out_pad + 255) / 256), dim3(256), 0, (cudaStream_t)stream, b, out, out_pad, b_packed));
     return CPRUNE_OK;
 }
@@ -392,6 +402,10 @@ cprune_status cprune_mx_fc(const void *x, size_t rows, int in, const void *codes
     if (rows >> 31 || in > (1 << 22) || out > (1 << 24)) return CPRUNE_ERR_UNSUPPORTED;
     const size_t need = cprune_mx_fc_workspace_bytes(rows, in, out);
     if (need && (!workspace || workspace_bytes < need)) return CPRUNE_ERR_WORKSPACE_TOO_SMALL;
+    const size_t out_bytes = rows * cprune_padded_channels(out) * 2;
+    const Buffer bx{x, rows * cprune_padded_channels(in) * 2}, br{residual, out_bytes}, by{y, out_is_f32 ? rows * out * 4 : out_bytes}, bb{b_packed, (size_t)cprune_padded_channels(out) * 4};
+    const Buffer bc{codes, (size_t)out * mx_blocks(in) * 16}, bs{scales, cprune_mx_scale_bytes(out, in)}, bw{need ? workspace : nullptr, need};
+    if (!(out_is_f32 ? apart(by, br) : same_or_apart(by, br)) || !apart_from(by, bx, bb, bc, bs) || !apart_from(bw, bx, br, by, bb, bc, bs)) return CPRUNE_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)stream;
     MxProduct p = {};
     p.codes = (const uint4 *)codes; p.scales = (const uint8_t *)scales; p.bias = b_packed; p.res = (const __nv_bfloat16 *)residual; p.y = y; p.rows = rows;

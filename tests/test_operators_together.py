@@ -196,3 +196,24 @@ def test_a_call_that_failed_on_the_way_is_not_made_again(cp, monkeypatch):
     for call in calls.values():
         call()
     torch.cuda.synchronize()
+
+
+def test_threads_that_count(cp):
+    """As above, and an exception in a thread ends the test, and every round is counted."""
+    from concurrent.futures import ThreadPoolExecutor
+    jobs = [work_of(cp, s) for s in (3, 4)]
+    want = [[t.clone() for t in j()] for j in jobs]
+    torch.cuda.synchronize()
+
+    def run(k):
+        equal = 0
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(15):
+                got = jobs[k]()
+                assert len(got) == len(want[k])
+                equal += all(torch.equal(a, b) for a, b in zip(got, want[k]))
+        return equal
+
+    with ThreadPoolExecutor(2) as pool:
+        assert [f.result(timeout=300) for f in [pool.submit(run, k) for k in range(2)]] == [15, 15]
+    cp.cprune_poll_device_status()

@@ -287,3 +287,26 @@ def test_rows_are_read_before_their_place_is_filled_again(cp, rows, inn, out):
     for _ in range(10):
         y = cp.cprune_mx_fc(x, inn, *packed, out, out_f32=True)
         assert torch.equal(y[:, :want.shape[1]].double(), want) and not y[:, want.shape[1]:].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,inn,out", [(129, 25088, 10), (300, 16384, 64), (129, 65536, 24), (200, 131072, 400), (129, 1 << 20, 8), (20, 1 << 20, 8), (8, 25088, 4096)])
+def test_product_of_many_channels_of_one_sign(cp, rows, inn, out):
+    """Values and weights that are positive, in blocks of any scale: every addition to the accumulator truncates the same way, at most 2^-23 of the sum so far; a step takes 64 channels, so that n
+    steps are off by n 2^-24 of the sum in the mean of their partial sums.  What a step itself cuts off (64 products, each exact) and the rest count 16 such units."""
+    g = torch.Generator(device="cuda").manual_seed(41)
+    x = torch.zeros((rows, cp.cprune_padded_channels(inn)), dtype=torch.bfloat16, device="cuda")
+    by = lambda n: torch.exp2(torch.randint(-8, 1, (n, inn // 32), generator=g, device="cuda").float()).repeat_interleave(32, 1)  # noqa: E731
+    x[:, :inn] = (torch.rand((rows, inn), generator=g, device="cuda") + 0.1) * by(rows)
+    w = (torch.rand((out, inn), generator=g, device="cuda") + 0.1) * by(out)
+    codes, scales, bias = cp.cprune_mx_pack(w)
+    got = cp.cprune_mx_fc(x, inn, codes, scales, bias, out, out_f32=True).double()
+    cp.cprune_poll_device_status()
+    want = torch.zeros((rows, out), dtype=torch.float64, device="cuda")
+    qw = cp.cprune_mx_dequantize(codes, scales, inn)
+    qx = cp.cprune_mx_quantize(x, inn, values=True)[2]
+    for c in range(0, inn, 16384):
+        want += qx[:, c:min(c + 16384, inn)].double() @ qw[:, c:c + 16384].double().t()
+    off = ((got - want).abs() / want).max().item()
+    steps = -(-inn // 64)
+    assert off <= (steps / 2 + 16) * 2.0 ** -23

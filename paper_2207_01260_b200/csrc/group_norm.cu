@@ -333,13 +333,14 @@ __device__ __forceinline__ void sum_rows(const float *v, int sv, int rows, F don
     }
 }
 
-// Means and squared deviations of the rows' values put together per lane: v holds every thread's sum and its deviations from its own mean over
-// its `few`, or one more, of the n pixels
+// Means and squared deviations of the rows' values put together per lane: v holds every thread's mean and its deviations from it over its `few`, or one more, of
+// the n pixels.  A sum divided by its number is off by two units of the mean, here and below, so the mean of the differences from it is added, and taken out of
+// their squares: equal means stay what they are.  (Without, the variance of two flat channels 1 % apart was off by 2e-5, of equal ones by the square of those units.)
 template <int L, typename F>
 __device__ __forceinline__ void combine_rows(const float *v, int sv, int rows, int n, int few, F done) {
     const int lanes = sv * L, log2 = sharers_log2(lanes), sub = 1 << log2, sl = threadIdx.x & (sub - 1);
     const int more = n - few * rows;                           // rows below `more` have few + 1 pixels
-    const float inv = n > 0 ? inverse(n) : 0.f, inv_few = few > 0 ? inverse(few) : 0.f, inv_more = inverse(few + 1);
+    const float inv = n > 0 ? inverse(n) : 0.f, count_few = (float)few, count_more = (float)(few + 1);
     const int used = few > 0 ? rows : more;
     for (int q0 = 0; q0 < lanes; q0 += NORM_T >> log2) {
         const int q = q0 + (threadIdx.x >> log2);
@@ -347,16 +348,19 @@ __device__ __forceinline__ void combine_rows(const float *v, int sv, int rows, i
         float s = 0.f, m2 = 0.f;
         if (q < lanes)
 #pragma unroll 4
-            for (int r = sl; r < used; r += sub) s += w[r * sv];
-        const float mean = sum_sharers(s, log2) * inv;
+            for (int r = sl; r < used; r += sub) s += w[r * sv] * (r < more ? count_more : count_few);
+        const float about = sum_sharers(s, log2) * inv;
+        s = 0.f;
         if (q < lanes)
 #pragma unroll 4
             for (int r = sl; r < used; r += sub) {
-                const float d = w[r * sv] * (r < more ? inv_more : inv_few) - mean;
-                m2 += w[L * NORM_PITCH + r * sv] + d * d * (float)(r < more ? few + 1 : few);
+                const float d = w[r * sv] - about, e = d * (r < more ? count_more : count_few);
+                s += e;
+                m2 += w[L * NORM_PITCH + r * sv] + d * e;
             }
+        s = sum_sharers(s, log2);
         m2 = sum_sharers(m2, log2);
-        if (q < lanes && sl == 0) done(q, mean, m2);
+        if (q < lanes && sl == 0) done(q, fmaf(s, inv, about), m2 - s * (s * inv));
     }
 }
 
@@ -380,7 +384,7 @@ template <int NP> struct Spread {
             q[i] = fma2(d, d, q[i]);
         }
     }
-    // sums and deviations from the means of n values, per lane
+    // means of n values and deviations from them, per lane
     template <int L> __device__ __forceinline__ void store(float *v, int n) const {
         const float inv = n > 0 ? inverse(n) : 0.f;
 #pragma unroll
@@ -388,16 +392,16 @@ template <int NP> struct Spread {
             const float2 k = one_by_one(minus_shift[l / 2]), a = one_by_one(s[l / 2]), b = one_by_one(q[l / 2]);
             const float shift = l % 2 ? k.y : k.x, sum = l % 2 ? a.y : a.x, square = l % 2 ? b.y : b.x;
             const float dev = square - sum * (sum * inv);
-            v[l * NORM_PITCH + threadIdx.x] = n > 0 ? sum - shift * (float)n : 0.f;
+            v[l * NORM_PITCH + threadIdx.x] = n > 0 ? fmaf(sum, inv, -shift) : 0.f;
             v[(L + l) * NORM_PITCH + threadIdx.x] = n > 0 ? (dev < 0.f ? 0.f : dev) : 0.f;         // (a NaN stays one: no maximum)
         }
     }
 };
 
 // The same of any number of values, in runs: at the end of one, its squares are taken from the mean of all values so far, which becomes the shift of the next, and
-// added to those of the runs before.  The mean of the first four is where it begins: with the first of 1568 values as the only shift, and that
-// one far from a flat rest (1 x 112x112x1280, a group per channel), 1 / sqrt(variance) was off by 4.5e-3.  A run's squares are then at most twice what they add
-// to the deviations (the first run's three times), and runs of about the root of n keep the additions in a row few.
+// added to those of the runs before.  The mean of the first four is where it begins (of a single run, the first): with the first of 1568 values as the only shift,
+// and that one far from a flat rest (1 x 112x112x1280, a group per channel), 1 / sqrt(variance) was off by 4.5e-3.  A run's squares are then at most twice what
+// they add to the deviations (the first run's three times), and runs of about the root of n keep the additions in a row few.
 template <int NP> struct LongSpread : Spread<NP> {
     using Spread<NP>::minus_shift;
     using Spread<NP>::s;
@@ -571,9 +575,10 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_partial_kernel(const __grid_co
     LongSpread<NP> own;
     {
         f2 f[4][NP];
+        const int first = c.cnt > ring_of(1) ? 4 : min(c.cnt, 1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) Lanes<KIND>::unpack(i < c.cnt ? ((const Raw *)p.x)[c.at(i)] : Raw(), f[i]);
-        own.begin(f, min(c.cnt, 4));
+        for (int i = 0; i < 4; ++i) Lanes<KIND>::unpack(i < first ? ((const Raw *)p.x)[c.at(i)] : Raw(), f[i]);
+        own.begin(f, first);
     }
     x.run(
         [&](size_t, const Raw *v) {
@@ -643,29 +648,36 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_apply_kernel(const __grid_cons
             }
 #pragma unroll
             for (int i = 0; i < CHUNK_BATCH; ++i) s += w[i].x * pixels[i];
-            const float mean = sum_sharers(s, log2) * inv_hw;
+            const float about = sum_sharers(s, log2) * inv_hw;
+            s = 0.f;
 #pragma unroll
             for (int i = 0; i < CHUNK_BATCH; ++i) {
-                const float d = pixels[i] > 0.f ? w[i].x - mean : 0.f;         // (the square of a mean past 2^64, times no pixels, is no number)
-                m2 += w[i].y + d * d * pixels[i];
+                const float d = pixels[i] > 0.f ? w[i].x - about : 0.f, e = d * pixels[i];         // (the square of a mean past 2^64, times no pixels, is no number)
+                s += e;
+                m2 += w[i].y + d * e;
             }
+            s = sum_sharers(s, log2);
             m2 = sum_sharers(m2, log2);
-            if (q < n && sl == 0) channel[q] = make_float2(mean, m2);
+            if (q < n && sl == 0) channel[q] = make_float2(fmaf(s, inv_hw, about), m2 - s * (s * inv_hw));
         }
     }
     __syncthreads();
     by_group(range.n, p.cpg, [&](int g, int i, int team, int log2) {
         const float2 *w = channel + g * p.cpg;
-        float a = 0.f, b = 0.f;
+        float a = 0.f, b = 0.f, off = 0.f;
         if (g < range.n)
             for (int j = i; j < p.cpg; j += team) a += w[j].x;
         a = sum_sharers(a, log2) * inv_cpg;
         if (g < range.n)
             for (int j = i; j < p.cpg; j += team) {
                 const float d = w[j].x - a;
+                off += d;
                 b += w[j].y + d * d * (float)p.HW;
             }
-        b = sum_sharers(b, log2) * inv_hw * inv_cpg;
+        off = sum_sharers(off, log2) * inv_cpg;
+        b = fmaf(-off, off, sum_sharers(b, log2) * inv_hw * inv_cpg);
+        a += off;
+        b = b < 0.f ? 0.f : b;                                 // (a NaN stays one)
         if (g < range.n && i == 0) {
             const float2 result = make_float2(a, 1.f / sqrtf(b + p.eps));
             image[g] = result;
@@ -998,16 +1010,19 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
     cluster_wait();
     by_group(s.sg, p.cpg, [&](int g, int i, int team, int log2) {
         const float2 *c = m.channel + (s.g0 + g) * p.cpg - s.v0 * L;
-        float a = 0.f, b = 0.f;
+        float a = 0.f, b = 0.f, off = 0.f;
         if (g < s.sg)
             for (int j = i; j < p.cpg; j += team) a += c[j].x;
         a = sum_sharers(a, log2) * inv_cpg;
         if (g < s.sg)
             for (int j = i; j < p.cpg; j += team) {
                 const float d = c[j].x - a;
+                off += d;
                 b += c[j].y + d * d * (float)s.n;
             }
-        b = sum_sharers(b, log2);
+        off = sum_sharers(off, log2);
+        b = sum_sharers(b, log2) - off * (off * inv_cpg) * (float)s.n;
+        a = fmaf(off, inv_cpg, a);
         if (g < s.sg && i < ranks) push_float2(m.inbox + rank * p.gs + g, i, make_float2(a, b));
     });
     cluster_arrive();
@@ -1015,10 +1030,11 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
     // the ranks' groups to the image's
     const float pixels = (float)max(0, min(p.per, p.HW - (t & 15) * p.per));
     over_ranks(m.inbox, p.gs, s.sg, ranks, [&](int g, float2 w) {
-        const float mean = sum16(w.x * pixels) * inv_hw, d = pixels > 0.f ? w.x - mean : 0.f;
-        const float m2 = sum16(w.y + d * d * pixels * (float)p.cpg);
+        const float about = sum16(w.x * pixels) * inv_hw, d = pixels > 0.f ? w.x - about : 0.f, e = d * pixels;
+        const float off = sum16(e) * inv_hw, mean = about + off;
+        const float v = fmaf(-off, off, sum16(w.y + d * e * (float)p.cpg) * inv_hw * inv_cpg);
         if (g < s.sg && (t & 15) == 0) {
-            const float2 result = make_float2(mean, 1.f / sqrtf(m2 * inv_hw * inv_cpg + p.eps));
+            const float2 result = make_float2(mean, 1.f / sqrtf((v < 0.f ? 0.f : v) + p.eps));
             m.image[g] = result;
             if (rank == 0) ((float2 *)p.stats)[(size_t)blockIdx.z * p.G + s.g0 + g] = result;
         }

@@ -400,3 +400,46 @@ def test_gradients_of_one_sign(cp, H, W, C, G, dtype, act, with_res):
     want = r * (t - m1 - h * m2)
     off = r * (t_off + m1_off + h.abs() * m2_off + h_off * m2.abs() + UNITS * (t.abs() + m1.abs() + (h * m2).abs()))
     close("dx", dx[..., :C].reshape(want.shape), want, STEP[dtype] * want.abs() + off)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,H,W,C,G", [(3, 5, 7, 20, 10), (1, 9, 9, 756, 3), (30, 25, 155, 300, 150), (2, 40, 40, 96, 48), (64, 33, 35, 48, 16), (1, 1, 3, 34, 17), (2, 3, 500, 2056, 4)])
+def test_flat_channels(cp, N, H, W, C, G, dtype):
+    """A value per channel, those of a group 1 % apart or less; groups whose channels are equal.  The deviations are those of a few numbers around a mean that is as good
+    as float32 can be: half a unit of the mean is 0.5 * 2^-23 / 0.01 = 6e-6 of such a deviation, and counts with its square; equal numbers have no deviations."""
+    g = torch.Generator(device="cuda").manual_seed(34)
+    base = torch.rand((G, 1), generator=g, device="cuda") * 300 + 1
+    step = torch.randint(-2, 3, (G, C // G), generator=g, device="cuda") * (2.0 ** -6 if dtype == "bf16" else 2.0 ** -9)
+    step[::3] = 0.0
+    x = torch.zeros((N, H, W, lanes(cp, C, dtype)), dtype=TYPES[dtype], device="cuda")
+    x[..., :C] = (base * (1 + step)).reshape(C)
+    y, stats = cp.cprune_group_norm(x, C, G)
+    v = x[0, 0, 0, :C].double().reshape(G, C // G)
+    mean, var = v.mean(1), v.var(1, correction=0)
+    rstd = 1 / (var + EPS).sqrt()
+    close("mean", stats[..., 0], mean.expand(N, G), 2.0 ** -23 * mean)
+    # what the variance is off by: its own roundings, 24 of 2^-24, and the square of what the mean is off by
+    off = (24 * 2.0 ** -24 * var + (2.0 ** -23 * mean) ** 2) / (var + EPS) / 2 + 2.0 ** -23
+    close("rstd", stats[..., 1], rstd.expand(N, G), off * rstd)
+    flat = (v == v[:, :1]).all(1).repeat_interleave(C // G)
+    assert flat.any() and not y[..., :C][..., flat].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,H,W,C,G", [(1, 31, 33, 16382, 2), (2, 3, 3, 2200, 2), (3, 40, 40, 600, 3), (64, 33, 35, 96, 2), (1, 1, 1, 4104, 1)])
+def test_a_channel_far_from_the_others(cp, N, H, W, C, G, dtype):
+    """The first or the last channel of a group: its distance is rounded to 2^-24 of it, the deviations are that distance over the root of the group's channels."""
+    g = torch.Generator(device="cuda").manual_seed(35)
+    for at in (0, C // G - 1):
+        x = torch.zeros((N, H, W, lanes(cp, C, dtype)), dtype=TYPES[dtype], device="cuda")
+        v = x[..., :C].view(N, H, W, G, C // G)
+        v.copy_(0.25 + torch.rand((N, H, W, G, C // G), generator=g, device="cuda") * 1e-3)
+        v[..., at] = 700.0
+        stats = cp.cprune_group_norm(x, C, G)[1]
+        w = v.double()
+        mean = w.mean((1, 2, 4))
+        rstd = 1 / (w.var((1, 2, 4), correction=0) + EPS).sqrt()
+        close("mean", stats[..., 0], mean, UNITS * (mean.abs() + 1 / rstd))
+        close("rstd", stats[..., 1], rstd, UNITS * rstd)

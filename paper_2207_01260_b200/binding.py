@@ -508,6 +508,7 @@ def cprune_fc(x, in_features, w_packed, b_packed, out_features, activation="none
 # bounds.  What they allocate belongs to the stream that they run on, so that a workspace is not handed out again while it is in use there.
 # A call with nothing but its inputs, which allocates its results and runs on the current stream, is tried by csrc/torch_calls.cpp first: the same
 # steps in compiled code, which gives up (None) where anything is not in order, and raises where the library fails on the way.  What depends on sizes alone is remembered by sizes.
+# None of the calls records anything for autograd: they take tensors that require gradients, as the tasks do, and their results require none.
 TYPE = {torch.bfloat16: 0, torch.float32: 1}
 _BF16, _F32, _U8 = torch.bfloat16, torch.float32, torch.uint8
 _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device

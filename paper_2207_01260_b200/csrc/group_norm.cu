@@ -15,9 +15,9 @@
 //     itself, in the same order, and goes over the data again, last pixels first, so that part of it still comes from the cache.
 // The variance is never a difference of large sums: a thread takes squares of differences from a value near its mean, in runs of a few dozen pixels, and means
 // and deviations of threads, chunks and channels are put together pairwise (Chan, Golub, LeVeque 1979), in float32.
-// What bounds it (us, with buffers that do not stay in the cache): small images the launch and the exchange, 1 x 7x7x352 4.5, 8 x 28x28x91 float32 6.4; large ones
-// the two passes, whose loads, arithmetic and stores wait for one another, 64 x 112x112x44 38 (read once and written: 22 at a copy's rate); gradients instructions
-// too, 64 x 56x56x108 with silu and a shortcut 67 (33), 8 x 14x14x180 7.4.
+// What bounds it (us, with buffers that do not stay in the cache): small images the launch and the exchange, 1 x 7x7x352 4.6, 8 x 28x28x91 float32 6.4; large ones
+// the two passes, whose loads, arithmetic and stores wait for one another, 64 x 112x112x44 38.6 (read once and written: 22 at a copy's rate); gradients instructions
+// too, 64 x 56x56x108 with silu and a shortcut 66.5 (33), 8 x 14x14x180 7.1; few wide images the number of their blocks (see norm_tiling), 1 x 112x112x512 74 (3.9).
 #include <cmath>
 #include <mutex>
 #include <type_traits>
@@ -227,40 +227,40 @@ __device__ __forceinline__ void gradient_one(const NormParams &p, const Column<L
     affine<KIND, RES>(k, x, res, d, z);
     Lanes<KIND>::unpack(dy, dz);
     if constexpr (ACT != CPRUNE_ACT_NONE) {
-    float f[2 * NP], g[2 * NP];
+        float f[2 * NP], g[2 * NP];
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const float2 v = one_by_one(z[i]), w = one_by_one(dz[i]);
-        f[2 * i] = v.x; f[2 * i + 1] = v.y;
-        g[2 * i] = w.x; g[2 * i + 1] = w.y;
-    }
-    if (ACT == CPRUNE_ACT_SILU) {
-#pragma unroll
-        for (int l = 0; l < L; ++l) {
-            const float s = sigmoid(f[l]), t = s * f[l];
-            g[l] *= fmaf(t, 1.f - s, s);
+        for (int i = 0; i < NP; ++i) {
+            const float2 v = one_by_one(z[i]), w = one_by_one(dz[i]);
+            f[2 * i] = v.x; f[2 * i + 1] = v.y;
+            g[2 * i] = w.x; g[2 * i + 1] = w.y;
         }
-    } else {
-        // Where z is next to 0, |(x - mean) a| is next to |beta + residual|; it is off by two roundings of 2^-24, the sums by one each
-        float r[2 * NP];
-        if (RES) unpack_floats<KIND>(res, r);
-        const float near = 4e-7f * k.most, top = 6.f;
-        bool close = false;
+        if (ACT == CPRUNE_ACT_SILU) {
 #pragma unroll
-        for (int l = 0; l < L; ++l) {
-            const float e = RES ? fmaf(4e-7f, fabsf(r[l]), near) : near;
-            close |= fabsf(f[l]) < e || (ACT == CPRUNE_ACT_RELU6 && fabsf(f[l] - top) < e + 2.4e-6f);
+            for (int l = 0; l < L; ++l) {
+                const float s = sigmoid(f[l]), t = s * f[l];
+                g[l] *= fmaf(t, 1.f - s, s);
+            }
+        } else {
+            // Where z is next to 0, |(x - mean) a| is next to |beta + residual|; it is off by two roundings of 2^-24, the sums by one each
+            float r[2 * NP];
+            if (RES) unpack_floats<KIND>(res, r);
+            const float near = 4e-7f * k.most, top = 6.f;
+            bool close = false;
+#pragma unroll
+            for (int l = 0; l < L; ++l) {
+                const float e = RES ? fmaf(4e-7f, fabsf(r[l]), near) : near;
+                close |= fabsf(f[l]) < e || (ACT == CPRUNE_ACT_RELU6 && fabsf(f[l] - top) < e + 2.4e-6f);
+            }
+            if (close) {
+                const uint32_t inside = inside_64<KIND, ACT, RES>(p, x_at, res_at, n, c0);
+#pragma unroll
+                for (int l = 0; l < L; ++l) f[l] = inside >> l & 1 ? 1.f : -1.f;
+            }
+#pragma unroll
+            for (int l = 0; l < L; ++l) g[l] = f[l] > 0.f && (ACT != CPRUNE_ACT_RELU6 || f[l] < top) ? g[l] : 0.f;
         }
-        if (close) {
-            const uint32_t inside = inside_64<KIND, ACT, RES>(p, x_at, res_at, n, c0);
 #pragma unroll
-            for (int l = 0; l < L; ++l) f[l] = inside >> l & 1 ? 1.f : -1.f;
-        }
-#pragma unroll
-        for (int l = 0; l < L; ++l) g[l] = f[l] > 0.f && (ACT != CPRUNE_ACT_RELU6 || f[l] < top) ? g[l] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < NP; ++i) dz[i] = two(g[2 * i], g[2 * i + 1]);
+        for (int i = 0; i < NP; ++i) dz[i] = two(g[2 * i], g[2 * i + 1]);
     }
 }
 
@@ -1070,7 +1070,8 @@ __global__ void __launch_bounds__(NORM_T) norm_cluster_kernel(const __grid_const
 
 // How the on-chip kernel shares out an image; ranks == 0: it does not take it.  It takes what all fits at once, in two blocks to an SM of up to 12 pixels a thread.
 // us there / in two passes:  1 x 7x7x352 4.5 / 6.7, 8 x 28x28x128 5.8 / 7.8, 8 x 56x56x64 7.7 / 10.2, 64 x 14x14x360 9.0 / 17.8, 256 x 7x7x352 9.4 / 16.1,
-// 1 x 112x112x44 7.1 / 7.1;  with four blocks to an SM and 20 pixels 8 x 28x28x128 7.5, 8 x 56x56x64 9.0, 64 x 14x14x360 11.8.
+// 1 x 112x112x44 7.1 / 7.1;  with four blocks to an SM and 20 pixels 8 x 28x28x128 7.5, 8 x 56x56x64 9.0, 64 x 14x14x360 11.8.  (Before the means of means were
+// corrected, which costs 0.1 us here and up to 0.3 there.)
 struct NormCluster {
     int ranks = 0, gs = 0, slices = 0, per = 0, widest = 0;
     size_t data_bytes = 0, smem = 0;
@@ -1180,7 +1181,9 @@ static int norm_kind(int type, int C, uintptr_t addresses) {
 }
 
 // Chunks of pixels: as many blocks as are resident at a time (four to an SM, the gradients' three), so that none waits for a second round, and at most as many
-// an image as the threads of a block of the second pass read at once
+// an image as the threads of a block of the second pass read at once.  That is 8 where a slice touches more than 128 channels, so that few wide images leave most
+// SMs without a block: us 1 x 112x112x512 74, its gradients 191; 1 x 112x112x1280 270 and 735; gradients of 8 x 56x56x256 28, of 8 x 28x28x512 18.5 (floors 3.9, 5.9, 9.8,
+// 14.7, 5.9, 2.9)
 static NormTiling norm_tiling(int kind, int N, int HW, int C, int G, bool backward) {
     NormTiling t;
     const int L = kind == 0 ? 8 : kind == 1 ? 4 : 1;

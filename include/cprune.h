@@ -315,7 +315,7 @@ cprune_status cprune_clip_gradients(const void *const *grads, const unsigned lon
  * (in / 64 + 16) 2^-23 of the sum of their magnitudes (less than float32 additions one by one may be: in 2^-24).  Sums of one sign
  * lose a sixth of that: 4.7e-6 of 25088 channels, 3.3e-4 of a million.
  *   x  bf16 [rows][in_pad], a row per image or pixel;  residual  bf16 [rows][out_pad] or NULL;  act none, relu or relu6 (a NaN stays
- *   one);  y  bf16 [rows][out_pad] (pad lanes zero) or float32 [rows][out] when out_is_f32; it may be residual, not x
+ *   one);  y  bf16 [rows][out_pad] (pad lanes zero) or float32 [rows][out] when out_is_f32; as bf16 it may be residual, never x
  *   workspace  cprune_mx_fc_workspace_bytes, device, 16-byte aligned
  * Results that overlap an input, or one another, in any other way than said are refused (INVALID_ARG).
  * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows of a product, 2^40 of a rounding, more than 2^22 channels or 2^24

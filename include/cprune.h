@@ -287,7 +287,7 @@ cprune_status cprune_group_norm_backward(const void *dy, const void *x, int type
  *   grads   HOST array of n device addresses, counts and types (CPRUNE_TYPE_*) HOST arrays; a tensor is one run of counts[i]
  *           values at any address of its type; no two of them overlap; n and counts may be 0
  *   out     HOST array of n device addresses (types as grads), or NULL: in place.  out[i] is grads[i] or does not overlap any
- *   norm    device float32 [1];   max_norm >= 0;   workspace  cprune_gradient_workspace_bytes(n), device, 16-byte aligned
+ *   norm    device float32 [1], like the workspace apart from all of them;   max_norm >= 0;   workspace  cprune_gradient_workspace_bytes(n), device, 16-byte aligned
  * The arrays are read during the call (the list travels in kernel parameters); enqueue only, two launches for up to 512
  * tensors, two more for every further 512.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^44 values), CUDA. */
 size_t cprune_gradient_workspace_bytes(int n);

@@ -655,9 +655,9 @@ def _gradient_list(where, tensors, device):
     return array("Q", addresses), array("Q", counts), types
 
 
-def _refuse_overlap(where, a, c, t, out=None):
-    """Refuses gradients that share memory, with one another or with results that are not in their own place."""
-    runs = []
+def _refuse_overlap(where, a, c, t, out=None, others=()):
+    """Refuses gradients that share memory, with one another or with results that are not in their own place, or with `others` (addresses and sizes)."""
+    runs = [(at, at + size) for at, size in others]
     for i, (at, n) in enumerate(zip(a, c)):
         if n:
             size = n * (2 if t[i] == TYPE[_BF16] else 4)
@@ -689,9 +689,9 @@ def cprune_gradient_norm(grads, norm=None, workspace=None, stream=None):
     where = "cprune_gradient_norm"
     dev = torch.cuda.current_device()
     a, c, t = _gradient_list(where, list(grads), dev)
-    _refuse_overlap(where, a, c, t)
     norm = _norm_buffer(where, norm, stream, dev)
     pw, size, workspace = _workspace(where, workspace, _gradient_bytes(len(a)), stream, dev, norm)
+    _refuse_overlap(where, a, c, t, None, ((norm.data_ptr(), 4), (pw, size)))
     _check(_lib.cprune_gradient_norm(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), norm.data_ptr(), pw, size, _stream(stream)), where)
     return norm
 
@@ -711,9 +711,9 @@ def cprune_clip_gradients(grads, max_norm, out=None, norm=None, workspace=None, 
         o, oc, ot = _gradient_list(where, list(out), dev)
         if oc != c or ot != t:
             _refuse(where, "out has to have the gradients' sizes and types")
-    _refuse_overlap(where, a, c, t, o)
     norm = _norm_buffer(where, norm, stream, dev)
     pw, size, workspace = _workspace(where, workspace, _gradient_bytes(len(a)), stream, dev, norm)
+    _refuse_overlap(where, a, c, t, o, ((norm.data_ptr(), 4), (pw, size)))
     _check(_lib.cprune_clip_gradients(a.buffer_info()[0], c.buffer_info()[0], t.buffer_info()[0], len(a), max_norm, None if o is None else o.buffer_info()[0],
                                       norm.data_ptr(), pw, size, _stream(stream)), where)
     return norm

@@ -217,3 +217,24 @@ def test_factors_below_the_smallest_normal_number(cp, dtypes):
             w = w * (ctypes.c_float(max_norm).value / max_norm)
             off = (t.cpu().double() - w).abs()
             assert torch.all(off <= (step + 2.0 ** -22) * w.abs() + (2.0 ** -134 + 2.0 ** -149 if t.dtype == torch.bfloat16 else 2.0 ** -149)), scale
+
+
+def test_norm_and_workspace_apart_from_the_list(cp):
+    refuse = cp.binding._refuse_overlap
+    refuse("f", [100, 164], [16, 3], [1, 0], None, ((170, 4), (300, 1000)))
+    for others in (((160, 4), (300, 1000)), ((172, 4), (60, 41)), ((300, 4), (300, 64))):
+        with pytest.raises(cp.CpruneError):
+            refuse("f", [100, 164], [16, 3], [1, 0], None, others)
+
+
+@pytest.mark.gpu
+def test_a_norm_in_the_list_is_refused(cp):
+    flat = torch.ones(4096, device="cuda")
+    for call in (lambda **k: cp.cprune_gradient_norm([flat[:1000]], **k), lambda **k: cp.cprune_clip_gradients([flat[:1000]], 1.0, **k),
+                 lambda **k: cp.cprune_clip_gradients([flat[2000:3000]], 1.0, out=[flat[:1000]], **k)):
+        for bad in (dict(norm=flat[999:1000]), dict(workspace=torch.empty(0, device="cuda", dtype=torch.uint8).set_(flat.untyped_storage()))):
+            with pytest.raises(cp.CpruneError) as e:
+                call(**bad)
+            assert e.value.status in (1, 3) and (flat == 1).all()
+        assert e.value.status == 1
+    assert abs(float(cp.cprune_gradient_norm([flat[:1000]], norm=flat[1000:1001])) - 1000 ** 0.5) <= 1e-5

@@ -703,9 +703,10 @@ __global__ void __launch_bounds__(NORM_T, 4) norm_apply_kernel(const __grid_cons
     x.run([&](size_t at, const Raw *v) { apply_one<KIND, ACT, RES>(p, k, v[0], v[RES ? NORM_T : 0], at); });
 }
 
-// Sums of dz and dz (x - mean) of a thread.  RUNS: of many pixels, run by run; the sums of the runs before are kept in local memory, for which there are no registers
-// left.  In a single run 784 equal values were off by 8e-6 of their sum, 1568 by 1.1e-5.  (us with / without, which is why few pixels do without: 64 x 56x56x108 silu and shortcut, 30
-// pixels a thread, 70.8 / 68.9; 64 x 112x112x44 relu, 50 of them, 71.7 / 70.0; the sums before in registers, with spills, 72.6 and 73.7.)
+// Sums of dz and dz (x - mean) of a thread.  RUNS: of many pixels, run by run; the sums of the runs before are kept in local memory, for which there are no
+// registers left.  In a single run 784 equal values were off by 8e-6 of their sum, 1568 by 1.1e-5.  (us with / without, which is why few pixels do without:
+// 64 x 56x56x108 silu and shortcut, 30 pixels a thread, 70.8 / 68.9; 64 x 112x112x44 relu, 50 of them, 71.7 / 70.0; the sums before in registers, with spills, 72.6
+// and 73.7.)
 constexpr int GRADIENT_RUN = 30, GRADIENT_SINGLE = 64;         // pixels: of a run at least, of a single one at most
 template <int NP, bool RUNS> struct GradientSums {
     f2 a[NP], b[NP], *before;
@@ -1182,8 +1183,8 @@ static int norm_kind(int type, int C, uintptr_t addresses) {
 
 // Chunks of pixels: as many blocks as are resident at a time (four to an SM, the gradients' three), so that none waits for a second round, and at most as many
 // an image as the threads of a block of the second pass read at once.  That is 8 where a slice touches more than 128 channels, so that few wide images leave most
-// SMs without a block: us 1 x 112x112x512 74, its gradients 191; 1 x 112x112x1280 270 and 735; gradients of 8 x 56x56x256 28, of 8 x 28x28x512 18.5 (floors 3.9, 5.9, 9.8,
-// 14.7, 5.9, 2.9)
+// SMs without a block: us 1 x 112x112x512 74, its gradients 191; 1 x 112x112x1280 270 and 735; gradients of 8 x 56x56x256 28, of 8 x 28x28x512 18.5 (floors 3.9, 5.9,
+// 9.8, 14.7, 5.9, 2.9)
 static NormTiling norm_tiling(int kind, int N, int HW, int C, int G, bool backward) {
     NormTiling t;
     const int L = kind == 0 ? 8 : kind == 1 ? 4 : 1;

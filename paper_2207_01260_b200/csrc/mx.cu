@@ -110,7 +110,8 @@ constexpr int MX_T = 256, MX_UNIT = 64;      // rows that a block takes at a tim
 // 16 / E threads take four blocks (128 channels, a tile of scales wide: grid y) of a row, 8 E values each (bf16: sixteen, float32: eight): loads and stores of
 // neighbouring threads adjoin, and the four scales are one word of a tile of scales.  What bounds it is the number of instructions, most of them for a block's scale, whatever the values a thread
 // has; 200704 x 108 with the values written (98 MB): eight values a thread, one row at a time 36 us, four rows under way and bf16 two at a time 26 us, sixteen
-// values 22 us.  Narrow rows leave most of a row's threads without work: a million rows of 16 channels 82 us, 4 million of 3 272 (12.4 and 30 at a copy's rate).  FORM 0: codes and scales (either both or neither), values as x; 1: the values in blocks, bf16 [rows][blocks * 32], in the order
+// values 22 us.  Narrow rows leave most of a row's threads without work: a million rows of 16 channels 82 us, 4 million of 3 272 (12.4 and 30 at a copy's
+// rate).  FORM 0: codes and scales (either both or neither), values as x; 1: the values in blocks, bf16 [rows][blocks * 32], in the order
 // 0 4 1 5 2 6 3 7 of every eight (the order in which mx_pair takes codes apart).
 template <int TYPE, int FORM>
 __global__ void __launch_bounds__(MX_T) mx_quantize_kernel(const void *__restrict__ x, unsigned long long rows, int C, int pitch, int tiles4, uint32_t *__restrict__ codes,
